@@ -408,6 +408,154 @@ int tetra_rotate(const uint16_t* x, const uint8_t* sign_bits, uint16_t* out, int
 int tetra_emb4_gather(const void* q, const uint16_t* scale_off, int rows, int dim, const int* tokens, int n,
                       float* out, hipStream_t stream);
 
+/*
+ * A paged cache of keys and values in 8 bits, for one layer and `seqs`
+ * sequences.  Page j of a sequence holds its tokens j * page_tokens onwards;
+ * `pages` names the page of the pool that it is.  A value is q * scale with q
+ * in -127..127 and one fp32 scale per page and head, keys and values apart:
+ *   k:      device int8 [num_pages][kv_heads][page_tokens][head_dim]
+ *   v:      device int8 [num_pages][kv_heads][page_tokens / 16][head_dim][16]
+ *           (tokens in groups of 16, a group's values transposed)
+ *   scales: device fp32 [num_pages][kv_heads][2] (of the keys, of the values)
+ *   pages:  device int32 [seqs][max_pages]; an entry outside [0, num_pages)
+ *           is no page: nothing is written to it, and its tokens are not seen
+ *   lens:   device int32 [seqs], the tokens of each sequence once the rows of
+ *           the call are in (0 for an idle slot); tokens past max_pages pages
+ *           are not kept
+ * page_tokens is 16, 32, 64 or 128; head_dim 64 or 128 (others:
+ * TETRA_EUNSUPPORTED); k and v 16-byte aligned, scales 8-byte, the others 4.
+ * The pool may be of any size; what it holds before the first append does not
+ * matter.  Sequences may share pages that are full and no longer appended to.
+ */
+typedef struct {
+    int8_t* k;
+    int8_t* v;
+    float* scales;
+    const int* pages;
+    const int* lens;
+    int num_pages, page_tokens, kv_heads, head_dim, seqs, max_pages;
+} tetra_kv_cache;
+
+/*
+ * What tetra_kv_append takes for each row (a new token): heads of head_dim
+ * values one after another, `*_stride` elements from a row to the next.
+ *   q:       device [rows][q_heads][head_dim], or NULL (then q_out is NULL)
+ *   k, v:    device [rows][kv_heads][head_dim]
+ *   half:    0: q, k and v are fp32 (as the products give them), 1: fp16
+ *   q_norm, k_norm: device fp32 [head_dim], the weights of an RMS norm of each
+ *            head of q and of k, or NULL for none:
+ *            x / sqrt(mean(x^2) + eps) * weight
+ *   rope:    device fp32 [rope_rows][head_dim], the cosines of a position's
+ *            head_dim / 2 angles and then their sines, or NULL for no rotation;
+ *            positions past the table take its last row
+ *   q_out:   device fp16 [rows][q_heads][head_dim], normed and rotated
+ * All 16-byte aligned, strides multiples of 8.
+ */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    long long q_stride, k_stride, v_stride;
+    int half;
+    const float* q_norm;
+    const float* k_norm;
+    float eps;
+    const float* rope;
+    int rope_rows;
+    int q_heads;
+    uint16_t* q_out;
+} tetra_kv_input;
+
+/*
+ * Appends keys and values to the cache, and norms and rotates q with them.
+ * Rows starts[s] .. starts[s + 1] - 1 are the new tokens of sequence s, the
+ * last of its lens[s] tokens; a sequence may have none.  Rotation turns the
+ * pairs (i, i + head_dim / 2) by the angles of the token's position:
+ *   (a, b) -> (a cos - b sin, b cos + a sin).
+ * A page's scale is the largest finite |value| over 127 (0 below 1e-30: the
+ * page then holds zeros).  Where a page already holds tokens of the sequence,
+ * its scale can only grow; the old values are then rounded again to the new
+ * one, rint(q * old / new), so a page's contents depend on how its tokens were
+ * split over calls, by a unit of the scale.  NaN is stored as 0, an infinity
+ * as +-127.
+ *   starts:  device int32 [seqs + 1], rising from 0 to `rows` at most (what
+ *            lies outside is ignored)
+ *   max_new: at least the largest count of new rows of a sequence (rows past it
+ *            are ignored), 1..rows
+ * Two sequences of a call must not append to the same page.  No workspace.
+ * Asynchronous; TETRA_EINVAL / TETRA_EALIGN / TETRA_EUNSUPPORTED before any
+ * launch, TETRA_EDEVICE at launch.
+ */
+int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, int rows, int max_new,
+                    hipStream_t stream);
+
+/*
+ * The last `count` tokens of every sequence as the values they stand for,
+ * fl16(q * scale), zeros where a sequence has fewer (or no page there):
+ *   k_out, v_out: device fp16 [seqs][count][kv_heads][head_dim], 16-byte aligned
+ * Asynchronous; errors as for tetra_kv_append.
+ */
+int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint16_t* v_out, hipStream_t stream);
+
+/*
+ * Attention of rows of q over the cache, which holds their own tokens already.
+ * Row i of sequence s (rows as for tetra_kv_append) is at position
+ * p = lens[s] - (starts[s + 1] - starts[s]) + i and sees the tokens j with
+ * j <= p and, if window > 0, j > p - window:
+ *   out = sum_j exp(scale q . k_j) v_j / sum_j exp(scale q . k_j),
+ * zeros where a row sees none.  Head h reads the cache's head
+ * h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.  Scores, maxima
+ * and sums are fp32, a weight is rounded to fp16 before it meets the values.
+ *   q:   device fp16, q_stride elements from a row to the next, 16-byte aligned
+ *   out: device fp16, out_stride elements apart, 16-byte aligned; rows of no
+ *        sequence are not written
+ *   workspace: device memory of the caller, 256-byte aligned, at least
+ *        tetra_kv_attend_workspace_bytes() (what it holds before a call does not
+ *        matter).  Calls that may run at the same time need different ones.
+ * Strides are multiples of 8.  The result does not change from run to run.
+ * Asynchronous; errors as for tetra_kv_append.
+ */
+int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                    int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
+                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of tetra_kv_attend on the current device (host only; 0 when
+ * the device cannot be queried). */
+size_t tetra_kv_attend_workspace_bytes(void);
+
+/*
+ * A token for every row of logits, from given random numbers.  With T the
+ * row's temperature and `top` its largest logit, a token has the weight
+ * floor(2^40 * 2^t), t = (x - top) * fl(log2(e) / T), where 2^t is a fixed
+ * sequence of fp32 operations (csrc/sample.h), so that sums of weights are
+ * exact and the token is fixed by the inputs.  In this order:
+ *   top_k: the k largest logits are left (equal ones: the lowest indices
+ *          first); k <= 0 or k >= vocab leaves all
+ *   top_p: of those, by falling logit, the shortest run whose weight reaches
+ *          ceil(p * W), W the weight of all of them, and one at least; p >= 1
+ *          leaves all
+ *   min_p: a token needs min_p times the likeliest's weight; min_p <= 0
+ *          leaves all
+ *   u:     the token is the first by index at which the sum of the weights
+ *          left exceeds floor(u * W'), W' the sum of all of them; u in [0, 1)
+ * T <= 0 gives the largest logit's token (the first of equal ones).  NaN counts
+ * as -inf; a row of nothing but -inf gives -1.
+ *   logits: device fp32, `stride` elements from a row to the next
+ *   temperature, top_p, min_p, u: device fp32 [rows]; top_k: device int32 [rows]
+ *   tokens: device int32 [rows]
+ *   workspace: device memory of the caller, 256-byte aligned, at least
+ *           tetra_sample_workspace_bytes(rows, vocab), as for tetra_kv_attend
+ * vocab is at most 2^22.  Asynchronous; TETRA_EINVAL / TETRA_EALIGN /
+ * TETRA_EDEVICE as for tetra_gemv.
+ */
+int tetra_sample(const float* logits, long long stride, int rows, int vocab, const float* temperature,
+                 const int* top_k, const float* top_p, const float* min_p, const float* u, int* tokens,
+                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of tetra_sample for these sizes (host only, pure; 0 if
+ * rows < 1 or vocab is out of range). */
+size_t tetra_sample_workspace_bytes(int rows, int vocab);
+
 #ifdef __cplusplus
 }
 #endif

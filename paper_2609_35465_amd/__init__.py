@@ -25,6 +25,7 @@ ENCODE_MAX_RADIUS = 25.0
 ENCODE_RADII = (13.0, 15.0)        # trial radii of the encoder: the best integer pair on Gaussian blocks
 
 _vp, _sz, _int = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+_i64, _f32 = ctypes.c_longlong, ctypes.c_float
 
 # name: (restype, argtypes)
 _SIGNATURES = {
@@ -49,6 +50,12 @@ _SIGNATURES = {
     "tetra_gemm_noalloc": (_int, [_vp, _vp, _vp, _vp, _int, _int, _int, _vp]),
     "tetra_release_stream": (_int, [_vp]),
     "tetra_emb4_gather": (_int, [_vp, _vp, _int, _int, _vp, _int, _vp, _vp]),
+    "tetra_kv_append": (_int, [_vp, _vp, _vp, _int, _int, _vp]),
+    "tetra_kv_read": (_int, [_vp, _int, _vp, _vp, _vp]),
+    "tetra_kv_attend": (_int, [_vp, _vp, _i64, _vp, _int, _int, _int, _f32, _int, _vp, _i64, _vp, _sz, _vp]),
+    "tetra_kv_attend_workspace_bytes": (_sz, []),
+    "tetra_sample": (_int, [_vp, _i64, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "tetra_sample_workspace_bytes": (_sz, [_int, _int]),
     "tetra_encode": (_int, [_vp, _vp, _sz, ctypes.c_double, ctypes.c_double, _vp, _vp]),
 }
 EXPORTED = tuple(_SIGNATURES)
@@ -305,3 +312,148 @@ def emb4_gather(q, scale_off, rows: int, dim: int, tokens, out, stream=None):
     embedding table q uint8 [rows, dim/2], scale_off fp16 [rows, dim/64, 2]."""
     _check(_call("tetra_emb4_gather", _ptr(q), _ptr(scale_off), rows, dim, _ptr(tokens),
                  int(tokens.numel()), _ptr(out), _stream(stream)), "tetra_emb4_gather")
+
+
+# ------------------------------------------------ cache, attention, sampling
+
+def _expect(ok, what):
+    if not ok:
+        raise TetraError(EINVAL, what)
+
+
+class KVCache(ctypes.Structure):
+    """tetra_kv_cache; keeps the tensors it was made of in `tensors`."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("seqs", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
+class KVInput(ctypes.Structure):
+    """tetra_kv_input"""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_longlong), ("k_stride", ctypes.c_longlong), ("v_stride", ctypes.c_longlong),
+                ("half", ctypes.c_int), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rope", ctypes.c_void_p), ("rope_rows", ctypes.c_int),
+                ("q_heads", ctypes.c_int), ("q_out", ctypes.c_void_p)]
+
+
+def make_kv_cache(k, v, scales, pages, lens) -> KVCache:
+    """A paged 8-bit cache of one layer from its device tensors: k int8 [num_pages, kv_heads, page_tokens,
+    head_dim], v int8 [num_pages, kv_heads, page_tokens // 16, head_dim, 16], scales fp32 [num_pages,
+    kv_heads, 2], pages int32 [seqs, max_pages], lens int32 [seqs], all contiguous.  Calls read what pages
+    and lens hold when they run."""
+    import torch
+    n, heads, page, dim = k.shape
+    _expect(k.dtype == v.dtype == torch.int8 and scales.dtype == torch.float32
+            and pages.dtype == lens.dtype == torch.int32
+            and tuple(v.shape) == (n, heads, page // 16, dim, 16) and tuple(scales.shape) == (n, heads, 2)
+            and pages.dim() == 2 and tuple(lens.shape) == (pages.shape[0],)
+            and all(t.is_contiguous() for t in (k, v, scales, pages, lens)), "make_kv_cache")
+    cache = KVCache(_ptr(k), _ptr(v), _ptr(scales), _ptr(pages), _ptr(lens), n, page, heads, dim, *pages.shape)
+    cache.tensors = (k, v, scales, pages, lens)
+    return cache
+
+
+def rope_table(positions: int, head_dim: int, base: float = 1e6):
+    """cos and sin of the rotation's angles, position * base^(-2 i / head_dim), as kv_append takes them:
+    a device fp32 tensor [positions, head_dim], the cosines of a position before its sines."""
+    import torch
+    angle = np.outer(np.arange(positions), base ** (-np.arange(0, head_dim, 2) / head_dim))
+    return torch.from_numpy(np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).cuda()
+
+
+def _rows_of(t, heads, dim, what):
+    """Elements from a row to the next of t [rows, heads, dim] or [rows, heads * dim] (heads side by side)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        _expect(shape[1:] == (heads, dim) and stride[2] == 1 and (heads == 1 or stride[1] == dim), what)
+    else:
+        _expect(len(shape) == 2 and shape[1] == heads * dim and stride[1] == 1, what)
+    return stride[0] if shape[0] > 1 else heads * dim
+
+
+def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm=None, k_norm=None,
+              eps: float = 1e-6, stream=None):
+    """Appends the rows k, v [rows, kv_heads, head_dim] (fp32 or fp16; rows starts[s] .. starts[s + 1] - 1
+    are sequence s's last tokens) to the cache, keys normed (k_norm fp32 [head_dim], optional) and rotated
+    (rope from rope_table(), or None); q [rows, q_heads, head_dim] goes the same way into q_out (fp16,
+    contiguous).  q and q_out may be None.  max_new: at least the largest count of rows of a sequence."""
+    import torch
+    heads, dim, kind = cache.kv_heads, cache.head_dim, k.dtype
+    _expect(kind in (torch.float32, torch.float16) and v.dtype == kind and starts.dtype == torch.int32
+            and starts.shape[0] == cache.seqs + 1 and v.shape[0] == k.shape[0], "tetra_kv_append")
+    a = KVInput(k=_ptr(k), v=_ptr(v), k_stride=_rows_of(k, heads, dim, "tetra_kv_append"),
+                v_stride=_rows_of(v, heads, dim, "tetra_kv_append"), half=int(kind == torch.float16), eps=eps,
+                q_norm=_ptr(q_norm), k_norm=_ptr(k_norm), rope=_ptr(rope), q_out=_ptr(q_out))
+    for w in (q_norm, k_norm):
+        _expect(w is None or (w.dtype == torch.float32 and w.shape == (dim,) and w.is_contiguous()), "tetra_kv_append")
+    if rope is not None:
+        _expect(rope.dtype == torch.float32 and rope.shape[1:] == (dim,) and rope.is_contiguous(), "tetra_kv_append")
+        a.rope_rows = rope.shape[0]
+    if q is not None:
+        _expect(q.dtype == kind and q_out is not None and q_out.dtype == torch.float16 and q_out.is_contiguous()
+                and q.shape[0] == k.shape[0] and q_out.numel() == q.numel(), "tetra_kv_append")
+        a.q, a.q_heads = _ptr(q), q.numel() // (q.shape[0] * dim) if q.shape[0] else 0
+        a.q_stride = _rows_of(q, a.q_heads, dim, "tetra_kv_append")
+    _check(_call("tetra_kv_append", ctypes.addressof(cache), ctypes.addressof(a), _ptr(starts), k.shape[0], max_new,
+                 _stream(stream)), "tetra_kv_append")
+
+
+def kv_read(cache: KVCache, count: int, k_out, v_out, stream=None):
+    """k_out, v_out fp16 [seqs, count, kv_heads, head_dim]: the last count tokens of every sequence."""
+    import torch
+    shape = (cache.seqs, count, cache.kv_heads, cache.head_dim)
+    for t in (k_out, v_out):
+        _expect(tuple(t.shape) == shape and t.dtype == torch.float16 and t.is_contiguous(), "tetra_kv_read")
+    _check(_call("tetra_kv_read", ctypes.addressof(cache), count, _ptr(k_out), _ptr(v_out), _stream(stream)),
+           "tetra_kv_read")
+
+
+def kv_attend_workspace():
+    """A workspace for tetra_kv_attend on the current device (a torch uint8 tensor)."""
+    import torch
+    n = int(_call("tetra_kv_attend_workspace_bytes"))
+    if n == 0:
+        raise TetraError(EDEVICE, "tetra_kv_attend_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def kv_attend(cache: KVCache, q, starts, max_new: int, out, workspace, scale: float = None, window: int = 0,
+              stream=None):
+    """out (fp16, as q) = attention of q fp16 [rows, q_heads, head_dim] over the cache, which holds the rows'
+    own tokens already (rows as in kv_append); scale: 1 / sqrt(head_dim) if None; window: how many tokens a
+    row sees at most, its own among them (0: all); workspace from kv_attend_workspace(), one per stream."""
+    import torch
+    dim = cache.head_dim
+    _expect(q.dtype == out.dtype == torch.float16 and q.shape == out.shape and q.shape[0] > 0
+            and starts.dtype == torch.int32 and starts.shape[0] == cache.seqs + 1, "tetra_kv_attend")
+    heads = q.numel() // (q.shape[0] * dim)
+    _check(_call("tetra_kv_attend", ctypes.addressof(cache), _ptr(q), _rows_of(q, heads, dim, "tetra_kv_attend"),
+                 _ptr(starts), q.shape[0], max_new, heads, dim ** -0.5 if scale is None else scale, window, _ptr(out),
+                 _rows_of(out, heads, dim, "tetra_kv_attend"), _ptr(workspace), workspace.numel(), _stream(stream)),
+           "tetra_kv_attend")
+
+
+def sample_workspace(rows: int, vocab: int):
+    """A workspace for tetra_sample over rows of vocab logits (a torch uint8 tensor)."""
+    import torch
+    n = int(_call("tetra_sample_workspace_bytes", rows, vocab))
+    if n == 0:
+        raise TetraError(EINVAL, "tetra_sample_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def sample(logits, temperature, top_k, top_p, min_p, u, tokens, workspace, stream=None):
+    """tokens int32 [rows] drawn from logits fp32 [rows, vocab] with the rows' temperature, top_p, min_p and
+    random numbers u (fp32 [rows]) and top_k (int32 [rows]); workspace from sample_workspace()."""
+    import torch
+    rows, vocab = logits.shape
+    f32 = (temperature, top_p, min_p, u)
+    _expect(logits.dtype == torch.float32 and logits.stride(1) == 1
+            and all(t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous() for t in f32)
+            and all(t.dtype == torch.int32 and t.shape == (rows,) and t.is_contiguous() for t in (top_k, tokens)),
+            "tetra_sample")
+    _check(_call("tetra_sample", _ptr(logits), logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(temperature),
+                 _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(tokens), _ptr(workspace), workspace.numel(),
+                 _stream(stream)), "tetra_sample")

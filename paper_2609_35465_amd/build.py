@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetra.so")
 
-SOURCES = ["tables.cpp", "tetra.hip"]
+SOURCES = ["tables.cpp", "tetra.hip", "serve.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950",

@@ -1,0 +1,166 @@
+// The serving operators around the projections for MI355X (gfx950): the paged
+// 8-bit cache of keys and values, the attention over it and sampling.  The
+// entry points of include/tetra.h: host code here validates arguments and
+// launches the kernels of kv_cache.h, attend.h and sample.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "../../include/tetra.h"
+#include "attend.h"
+#include "kv_cache.h"
+#include "sample.h"
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int launch_status() { return hipGetLastError() == hipSuccess ? TETRA_OK : TETRA_EDEVICE; }
+
+// a cache's sizes and pointers, as the kernels take them
+int cache_of(const tetra_kv_cache* c, tetra_dev::KvCache* out) {
+    if (!c || !c->k || !c->v || !c->scales || !c->pages || !c->lens) return TETRA_EINVAL;
+    if (c->num_pages < 1 || c->kv_heads < 1 || c->seqs < 1 || c->max_pages < 1) return TETRA_EINVAL;
+    int shift = 4;
+    while (shift < 7 && 1 << shift != c->page_tokens) ++shift;
+    if (1 << shift != c->page_tokens) return TETRA_EINVAL;
+    if (c->head_dim != 64 && c->head_dim != 128) return c->head_dim < 1 ? TETRA_EINVAL : TETRA_EUNSUPPORTED;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->scales, 8) || !aligned(c->pages, 4) ||
+        !aligned(c->lens, 4))
+        return TETRA_EALIGN;
+    *out = {c->k, c->v, c->scales, c->pages, c->lens, c->num_pages, c->page_tokens, shift, c->kv_heads, c->seqs,
+            c->max_pages};
+    return TETRA_OK;
+}
+
+constexpr long long kMaxGrid = 0x7FFFFFFFll;
+constexpr int kMaxVocab = 1 << 22;     // so that a row's sum of weights, 2^62 at most, fits 64 bits
+
+}  // namespace
+
+extern "C" {
+
+int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, int rows, int max_new,
+                    hipStream_t stream) {
+    tetra_dev::AppendArgs a;
+    if (int st = cache_of(cache, &a.c)) return st;
+    if (!in || !in->k || !in->v || !starts || rows < 1 || max_new < 1 || max_new > rows) return TETRA_EINVAL;
+    if (!in->q != !in->q_out || (in->q && in->q_heads < 1)) return TETRA_EINVAL;
+    if ((in->half != 0 && in->half != 1) || (in->rope && in->rope_rows < 1)) return TETRA_EINVAL;
+    if (!(in->eps >= 0.f) || std::isinf(in->eps)) return TETRA_EINVAL;
+    const int D = cache->head_dim;
+    const long long kv_width = static_cast<long long>(a.c.kv_heads) * D, q_width = static_cast<long long>(in->q_heads) * D;
+    if (in->k_stride < kv_width || in->v_stride < kv_width || (in->q && in->q_stride < q_width)) return TETRA_EINVAL;
+    if (!aligned(in->k, 16) || !aligned(in->v, 16) || in->k_stride % 8 || in->v_stride % 8 || !aligned(starts, 4) ||
+        (in->q && (!aligned(in->q, 16) || in->q_stride % 8 || !aligned(in->q_out, 16))) || !aligned(in->q_norm, 16) ||
+        !aligned(in->k_norm, 16) || !aligned(in->rope, 16))
+        return TETRA_EALIGN;
+    a.q = in->q;
+    a.k = in->k;
+    a.v = in->v;
+    a.q_stride = in->q_stride;
+    a.k_stride = in->k_stride;
+    a.v_stride = in->v_stride;
+    a.q_norm = in->q_norm;
+    a.k_norm = in->k_norm;
+    a.rope = in->rope;
+    a.starts = starts;
+    a.q_out = in->q_out;
+    a.eps = in->eps;
+    a.rope_rows = in->rope_rows;
+    a.rows = rows;
+    a.max_new = max_new;
+    a.q_heads = in->q ? in->q_heads : 0;
+    const int waves = a.c.page_tokens / tetra_dev::kGroupTokens;
+    const long long items =
+        max_new == 1 ? a.c.seqs : ((rows + ((1ll << a.c.page_shift) - 2) * a.c.seqs) >> a.c.page_shift) + a.c.seqs;
+    const long long kv_blocks = items * a.c.kv_heads * 2;
+    // 16 heads of a row per wave where that still leaves waves enough, so that a
+    // lane's part of the rotation table is read once for several heads
+    a.q_chunk = static_cast<long long>(rows) * a.q_heads >= 65536 ? 16 : 512 / D;
+    const long long q_units = a.q_heads ? static_cast<long long>(rows) * ((a.q_heads + a.q_chunk - 1) / a.q_chunk) : 0;
+    const long long grid = kv_blocks + (q_units + waves - 1) / waves;
+    if (kv_blocks > kMaxGrid || q_units > kMaxGrid - 8 || grid > kMaxGrid) return TETRA_EINVAL;
+    a.items = static_cast<int>(items);
+    const dim3 g(static_cast<unsigned>(grid)), b(static_cast<unsigned>(waves * 64));
+#define TETRA_APPEND(D_, H) hipLaunchKernelGGL((tetra_dev::append_kernel<D_, H>), g, b, 0, stream, a)
+    if (D == 64) {
+        if (in->half) TETRA_APPEND(64, true);
+        else TETRA_APPEND(64, false);
+    } else {
+        if (in->half) TETRA_APPEND(128, true);
+        else TETRA_APPEND(128, false);
+    }
+#undef TETRA_APPEND
+    return launch_status();
+}
+
+int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint16_t* v_out, hipStream_t stream) {
+    tetra_dev::KvCache c;
+    if (int st = cache_of(cache, &c)) return st;
+    if (count < 1 || !k_out || !v_out) return TETRA_EINVAL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return TETRA_EALIGN;
+    const long long rows = static_cast<long long>(c.seqs) * count;
+    if (rows > (1ll << 40) / (static_cast<long long>(c.kv_heads) * cache->head_dim)) return TETRA_EINVAL;
+    const long long grid = (rows * c.kv_heads * (cache->head_dim / 8) + 255) / 256;
+    if (grid > kMaxGrid) return TETRA_EINVAL;
+    const dim3 g(static_cast<unsigned>(grid)), b(256);
+    if (cache->head_dim == 64)
+        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<64>), g, b, 0, stream, c, count, k_out, v_out);
+    else
+        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<128>), g, b, 0, stream, c, count, k_out, v_out);
+    return launch_status();
+}
+
+size_t tetra_kv_attend_workspace_bytes(void) { return 256; }
+
+int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                    int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
+                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    tetra_dev::AttendArgs a;
+    if (int st = cache_of(cache, &a.c)) return st;
+    if (!q || !starts || !out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
+    if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale)) return TETRA_EINVAL;
+    const long long width = static_cast<long long>(q_heads) * cache->head_dim;
+    if (q_stride < width || out_stride < width || workspace_bytes < tetra_kv_attend_workspace_bytes()) return TETRA_EINVAL;
+    if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 || out_stride % 8 || !aligned(starts, 4) ||
+        !aligned(workspace, 256))
+        return TETRA_EALIGN;
+    a.q = q;
+    a.starts = starts;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.scale = scale * 1.44269504f;
+    a.rows = rows;
+    a.max_new = max_new;
+    a.q_heads = q_heads;
+    a.window = window;
+    const long long grid = static_cast<long long>(rows) * q_heads;
+    if (grid > kMaxGrid) return TETRA_EINVAL;
+    const dim3 g(static_cast<unsigned>(grid)), b(64);
+    if (cache->head_dim == 64) hipLaunchKernelGGL((tetra_dev::attend_kernel<64>), g, b, 0, stream, a);
+    else hipLaunchKernelGGL((tetra_dev::attend_kernel<128>), g, b, 0, stream, a);
+    return launch_status();
+}
+
+size_t tetra_sample_workspace_bytes(int rows, int vocab) { return rows < 1 || vocab < 1 || vocab > kMaxVocab ? 0 : 256; }
+
+int tetra_sample(const float* logits, long long stride, int rows, int vocab, const float* temperature,
+                 const int* top_k, const float* top_p, const float* min_p, const float* u, int* tokens,
+                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!logits || !temperature || !top_k || !top_p || !min_p || !u || !tokens || !workspace) return TETRA_EINVAL;
+    if (rows < 1 || vocab < 1 || vocab > kMaxVocab || stride < vocab) return TETRA_EINVAL;
+    if (workspace_bytes < tetra_sample_workspace_bytes(rows, vocab)) return TETRA_EINVAL;
+    if (!aligned(logits, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) ||
+        !aligned(min_p, 4) || !aligned(u, 4) || !aligned(tokens, 4) || !aligned(workspace, 256))
+        return TETRA_EALIGN;
+    const tetra_dev::SampleArgs a{logits, stride, temperature, top_p, min_p, u, top_k, tokens, vocab};
+    hipLaunchKernelGGL(tetra_dev::sample_kernel, dim3(static_cast<unsigned>(rows)), dim3(tetra_dev::kSampleThreads), 0,
+                       stream, a);
+    return launch_status();
+}
+
+}  // extern "C"
