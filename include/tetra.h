@@ -422,7 +422,7 @@ int tetra_emb4_gather(const void* q, const uint16_t* scale_off, int rows, int di
  *   lens:   device int32 [seqs], the tokens of each sequence once the rows of
  *           the call are in (0 for an idle slot); tokens past max_pages pages
  *           are not kept
- * page_tokens is 16, 32, 64 or 128; head_dim 64 or 128 (others:
+ * page_tokens is 16, 32, 64 or 128, max_pages * page_tokens at most 2^30; head_dim 64 or 128 (others:
  * TETRA_EUNSUPPORTED); k and v 16-byte aligned, scales 8-byte, the others 4.
  * The pool may be of any size; what it holds before the first append does not
  * matter.  Sequences may share pages that are full and no longer appended to.

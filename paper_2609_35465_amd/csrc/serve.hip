@@ -19,6 +19,8 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 
 int launch_status() { return hipGetLastError() == hipSuccess ? TETRA_OK : TETRA_EDEVICE; }
 
+constexpr int kMaxTokens = 1 << 30;    // of a sequence, so that token numbers have room above them in an int
+
 // a cache's sizes and pointers, as the kernels take them
 int cache_of(const tetra_kv_cache* c, tetra_dev::KvCache* out) {
     if (!c || !c->k || !c->v || !c->scales || !c->pages || !c->lens) return TETRA_EINVAL;
@@ -26,6 +28,7 @@ int cache_of(const tetra_kv_cache* c, tetra_dev::KvCache* out) {
     int shift = 4;
     while (shift < 7 && 1 << shift != c->page_tokens) ++shift;
     if (1 << shift != c->page_tokens) return TETRA_EINVAL;
+    if (c->max_pages > kMaxTokens >> shift) return TETRA_EINVAL;
     if (c->head_dim != 64 && c->head_dim != 128) return c->head_dim < 1 ? TETRA_EINVAL : TETRA_EUNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->scales, 8) || !aligned(c->pages, 4) ||
         !aligned(c->lens, 4))
@@ -33,6 +36,28 @@ int cache_of(const tetra_kv_cache* c, tetra_dev::KvCache* out) {
     *out = {c->k, c->v, c->scales, c->pages, c->lens, c->num_pages, c->page_tokens, shift, c->kv_heads, c->seqs,
             c->max_pages};
     return TETRA_OK;
+}
+
+// compute units of the current device, asked for once per device
+int device_cus(int* cus) {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return TETRA_EDEVICE;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return TETRA_EDEVICE;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    *cus = n;
+    return TETRA_OK;
+}
+
+constexpr int kFewGroupsPerCU = 2;
+constexpr size_t kMinAttendWorkspace = 4096;
+
+// parts of attend_few_kernel's workgroups
+size_t few_workspace(int cus) {
+    return static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128> * sizeof(float);
 }
 
 constexpr long long kMaxGrid = 0x7FFFFFFFll;
@@ -114,7 +139,11 @@ int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint1
     return launch_status();
 }
 
-size_t tetra_kv_attend_workspace_bytes(void) { return 256; }
+size_t tetra_kv_attend_workspace_bytes(void) {
+    int cus = 0;
+    if (device_cus(&cus)) return 0;
+    return few_workspace(cus);
+}
 
 int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
                     int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
@@ -124,25 +153,44 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     if (!q || !starts || !out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
     if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale)) return TETRA_EINVAL;
     const long long width = static_cast<long long>(q_heads) * cache->head_dim;
-    if (q_stride < width || out_stride < width || workspace_bytes < tetra_kv_attend_workspace_bytes()) return TETRA_EINVAL;
+    if (q_stride < width || out_stride < width || rows > kMaxGrid / q_heads) return TETRA_EINVAL;
     if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 || out_stride % 8 || !aligned(starts, 4) ||
         !aligned(workspace, 256))
         return TETRA_EALIGN;
+    int cus = 0;
+    if (workspace_bytes < kMinAttendWorkspace) return TETRA_EINVAL;
+    if (int st = device_cus(&cus)) return st;
+    if (workspace_bytes < few_workspace(cus)) return TETRA_EINVAL;
     a.q = q;
     a.starts = starts;
     a.out = out;
+    a.partials = static_cast<float*>(workspace);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    a.scale = scale * 1.44269504f;
+    a.scale = std::fabs(scale) * 1.44269504f;
+    a.q_flip = scale < 0.f ? 0x80008000u : 0u;
     a.rows = rows;
     a.max_new = max_new;
     a.q_heads = q_heads;
+    a.group = q_heads / a.c.kv_heads;
     a.window = window;
-    const long long grid = static_cast<long long>(rows) * q_heads;
-    if (grid > kMaxGrid) return TETRA_EINVAL;
-    const dim3 g(static_cast<unsigned>(grid)), b(64);
-    if (cache->head_dim == 64) hipLaunchKernelGGL((tetra_dev::attend_kernel<64>), g, b, 0, stream, a);
-    else hipLaunchKernelGGL((tetra_dev::attend_kernel<128>), g, b, 0, stream, a);
+    const int workers = cus * kFewGroupsPerCU;
+    const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
+    const long long reach = window > 0 ? std::min<long long>(kept, static_cast<long long>(window) + max_new + 64) : kept;
+    const long long row_tiles = (static_cast<long long>(max_new) * a.group + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
+    const long long units = row_tiles * a.c.kv_heads * a.c.seqs, tiles = (reach + tetra_dev::kFewTile - 1) / tetra_dev::kFewTile;
+    if (units > kMaxGrid / tiles) return TETRA_EINVAL;
+    const dim3 g(static_cast<unsigned>(workers)), join(static_cast<unsigned>(units)), b(256);
+#define TETRA_ATTEND(D)                                                                                       \
+    hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), g, b, 0, stream, a);                                \
+    if (tiles > 1)                                                                                            \
+        hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), join, b, 0, stream, a, workers, static_cast<int>(row_tiles))
+    if (cache->head_dim == 64) {
+        TETRA_ATTEND(64);
+    } else {
+        TETRA_ATTEND(128);
+    }
+#undef TETRA_ATTEND
     return launch_status();
 }
 
