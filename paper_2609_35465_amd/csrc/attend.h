@@ -24,6 +24,7 @@ struct AttendArgs {
     float scale;      // |scale| log2(e)
     uint32_t q_flip;  // 0x80008000 if the scale is negative: turns q instead
     int rows, max_new, q_heads, group, window;
+    int few_most;     // sequences of up to so many rows (token, q head of a group) go through attend_few_kernel
 };
 
 constexpr float kNoScore = -3e38f;   // a maximum over no score
@@ -101,10 +102,15 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs& a, const Span& s) {
 // written) and its units
 __device__ __forceinline__ int few_tiles(const Reach& r) { return max(1, (r.end - r.begin + kFewTile - 1) / kFewTile); }
 
+// row tiles of a sequence: none if it goes through attend_many_kernel
+__device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Span& s) {
+    const int rows = s.n * a.group;
+    return rows > a.few_most ? 0 : (rows + kFewRows - 1) / kFewRows;
+}
+
 __device__ __forceinline__ int few_work(const AttendArgs& a, int seq) {
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int units = (s.n * a.group + kFewRows - 1) / kFewRows * a.c.kv_heads;
-    return units * few_tiles(reach_of(a, s));
+    return few_row_tiles(a, s) * a.c.kv_heads * few_tiles(reach_of(a, s));
 }
 
 // sum over the workgroup's four waves, in every thread
@@ -117,11 +123,22 @@ __device__ __forceinline__ int few_sum(int v, int* lds) {
     return lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// the workgroups that take part, a tile each at least, and the first tile of one
-__device__ __forceinline__ int few_workers(long long total, int launched) {
-    return static_cast<int>(min(total, static_cast<long long>(launched)));
-}
-__device__ __forceinline__ long long few_from(int w, long long total, int workers) { return w * total / workers; }
+// The workgroups that take part, a tile each at least, the first tile of one and
+// the one that has a tile.
+struct FewPlan {
+    int workers, share, more;      // `more` workgroups take share + 1 tiles, the others share
+
+    __device__ __forceinline__ FewPlan(int total, int launched) {
+        workers = min(total, launched);
+        share = total / max(workers, 1);
+        more = total - share * workers;
+    }
+    __device__ __forceinline__ int from(int w) const { return w * share + min(w, more); }
+    __device__ __forceinline__ int owner(int tile) const {
+        const int big = more * (share + 1);
+        return tile < big ? tile / (share + 1) : more + (tile - big) / share;
+    }
+};
 
 template <int D>
 struct FewState {
@@ -238,16 +255,9 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
     __shared__ int lds[4], found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4, w = blockIdx.x;
-    int mine = 0;
-    for (int s = tid; s < a.c.seqs; s += 256) mine += few_work(a, s);
-    const long long total = few_sum(mine, lds);
-    const int W = few_workers(total, gridDim.x);
-    if (w >= W) return;
-    const int from = __builtin_amdgcn_readfirstlane(static_cast<int>(few_from(w, total, W)));
-    const int to = __builtin_amdgcn_readfirstlane(static_cast<int>(few_from(w + 1, total, W)));
-    // the sequence that holds tile `from`, and the tiles before it
-    for (int s0 = 0, before = 0; s0 < a.c.seqs; s0 += 256) {
-        const int n = s0 + tid < a.c.seqs ? few_work(a, s0 + tid) : 0;
+    // The total, and the sequence that holds this workgroup's first tile with the
+    // tiles before it.  Up to 256 sequences are one scan, more take two passes.
+    auto scan = [&](int n, int& all) {
         int upto = n;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -257,18 +267,33 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
         __syncthreads();
         if (lane == 63) lds[wave] = upto;
         __syncthreads();
-        int all = 0;
+        all = 0;
         for (int i = 0; i < kFewWaves; ++i) {
             if (i < wave) upto += lds[i];
             all += lds[i];
         }
-        upto += before;
+        return upto;
+    };
+    const int n0 = tid < a.c.seqs ? few_work(a, tid) : 0;
+    int all, upto = scan(n0, all), total = all;
+    if (a.c.seqs > 256) {
+        int more = 0;
+        for (int i = tid + 256; i < a.c.seqs; i += 256) more += few_work(a, i);
+        total += few_sum(more, lds);
+    }
+    const FewPlan plan(__builtin_amdgcn_readfirstlane(total), gridDim.x);
+    if (w >= plan.workers) return;
+    const int from = plan.from(w), to = plan.from(w + 1);
+    for (int s0 = 0, n = n0, before = 0;;) {
         if (upto > from && upto - n <= from) {
             found[0] = s0 + tid;
             found[1] = upto - n;
         }
         before += all;
-        if (before > from) break;
+        s0 += 256;
+        if (before > from || s0 >= a.c.seqs) break;
+        n = s0 + tid < a.c.seqs ? few_work(a, s0 + tid) : 0;
+        upto = scan(n, all) + before;
     }
     __syncthreads();
     int seq = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
@@ -277,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
         const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
         const Reach reach = reach_of(a, s);
         const int tiles = few_tiles(reach), rows = s.n * a.group;
-        const int row_tiles = (rows + kFewRows - 1) / kFewRows, units = row_tiles * a.c.kv_heads;
+        const int row_tiles = few_row_tiles(a, s), units = row_tiles * a.c.kv_heads;
         const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
         for (int unit = (x - base) / tiles; unit < units && x < to; ++unit) {
             const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
@@ -350,48 +375,489 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
 }
 
 // Joins the parts of the units that span workgroups of attend_few_kernel
-// (`launched` of them): a workgroup per unit, a wave per row.
+// (`launched` of them): a workgroup per unit and row, D / 4 lanes for the
+// dimensions and as many teams of them as fit for the parts.
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int launched, int row_tiles_most) {
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int launched, int row_tiles_most, int rows_most) {
+    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
     __shared__ int lds[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ float sums[kTeams][D + 1];
+    const int tid = threadIdx.x;
+    const int r = blockIdx.x % rows_most, rest = blockIdx.x / rows_most;
     const int per_seq = a.c.kv_heads * row_tiles_most;
-    const int seq = blockIdx.x / per_seq, unit = blockIdx.x - seq * per_seq;
+    const int seq = rest / per_seq, unit = rest - seq * per_seq;
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int rows = s.n * a.group, row_tiles = (rows + kFewRows - 1) / kFewRows;
+    const int rows = s.n * a.group, row_tiles = few_row_tiles(a, s);
     if (unit >= row_tiles * a.c.kv_heads) return;
+    const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
     const int tiles = few_tiles(reach_of(a, s));
-    if (tiles == 1) return;
+    if (tiles == 1 || row0 + r >= rows) return;
     int all = 0, mine = 0;
     for (int i = tid; i < a.c.seqs; i += 256) {
         const int n = few_work(a, i);
         all += n;
         if (i < seq) mine += n;
     }
-    const long long total = few_sum(all, lds);
-    const int workers = few_workers(total, launched);
-    const long long u0 = few_sum(mine, lds) + static_cast<long long>(unit) * tiles, u1 = u0 + tiles;
-    const int w0 = static_cast<int>(((u0 + 1) * workers - 1) / total), w1 = static_cast<int>((u1 * workers - 1) / total);
+    const FewPlan plan(few_sum(all, lds), launched);
+    const int u0 = few_sum(mine, lds) + unit * tiles, w0 = plan.owner(u0), w1 = plan.owner(u0 + tiles - 1);
     if (w0 == w1) return;
-    const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
-    const int slot0 = 2 * w0 + (few_from(w0, total, workers) >= u0 ? 0 : 1);
-    auto slot = [&](int w) { return a.partials + static_cast<size_t>(w == w0 ? slot0 : 2 * w) * kFewSlot<D>; };
-    for (int r = wave; r < min(kFewRows, rows - row0); r += kFewWaves) {
-        float m = kNoScore;
-        for (int w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, slot(w)[r]);
+    // the unit's first workgroup may have begun with another unit
+    const float* part0 = a.partials + (2 * static_cast<size_t>(w0) + (plan.from(w0) == u0 ? 0 : 1)) * kFewSlot<D>;
+    auto part = [&](int w) { return w == w0 ? part0 : a.partials + 2 * static_cast<size_t>(w) * kFewSlot<D>; };
+    const int team = tid / kLanes, d = tid % kLanes * 4;
+    float m = kNoScore, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = w0 + team; w <= w1; w += kTeams) {
+        const float* p = part(w);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(p + 2 * kFewRows + r * D + d);
+        const float pm = p[r], mnew = fmaxf(m, pm), fo = fast_exp2(m - mnew), fp = fast_exp2(pm - mnew);
+        l = l * fo + p[kFewRows + r] * fp;
+        o = o * fo + x * fp;
+        m = mnew;
+    }
+    // the teams': m and l, then the sums
+    __shared__ float stat[kTeams][2];
+    if (d == 0) {
+        stat[team][0] = m;
+        stat[team][1] = l;
+    }
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    for (int i = 0; i < 4; ++i) sums[team][d + i] = o[i];
+    __syncthreads();
+    if (tid < D) {
+        for (int i = 0; i < kTeams; ++i) m = fmaxf(m, stat[i][0]);
+        float sum = 0.f, x = 0.f;
+        for (int i = 0; i < kTeams; ++i) {
+            const float f = fast_exp2(stat[i][0] - m);
+            sum += f * stat[i][1];
+            x += f * sums[i][tid];
+        }
+        const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
+        reinterpret_cast<_Float16*>(a.out)[(s.row0 + t) * a.out_stride + h * D + tid] =
+            static_cast<_Float16>(sum > 0.f ? x / sum : 0.f);
+    }
+}
+
+// ---------------------------------------------------------------- many rows
+//
+// Sequences with many rows (prompts): bound by the matrix cores and by the
+// exponentials.  A workgroup takes a unit of 32 NW rows of a sequence and
+// cache head, a wave 32 of them, and goes through the unit's keys 64 at a
+// time: each tile is turned into fp16 once, in LDS, for all waves.  Two buffers,
+// one barrier a tile; the next tile is written while the present one is in use,
+// and the one after it is on its way from memory.
+//
+// Products on v_mfma_f32_32x32x16_f16, transposed as above: S^T = K Q^T leaves
+// a lane (row lane % 32, half h = lane / 32) with the scores of tokens 8 (i /
+// 4) + 4 h + i % 4 of each 32, which as they stand are its operand of O^T = V^T
+// P^T, a product of 16 tokens in the order 0-3, 8-11 | 4-7, 12-15; the values
+// are written to LDS in that order.
+//
+// The scale of a page's values enters through the exponent, 2^(s - m + 15 +
+// log2(scale / largest so far)), and leaves the sum l again once for 16 tokens.
+// m follows the maximum only when a score passes it by 2^kSlack or more.
+
+constexpr int kManyTile = 64;
+constexpr float kSlack = 8.f;
+constexpr float kNoLog = -1e30f;        // log2 of a scale of zero
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// How the device spreads the many-row units, found by every wave for itself: the
+// row tiles of all sequences, and the pieces that a unit's keys are cut into.
+// Units that do not fill the chip (`slots` workgroups at once) are cut, if their
+// keys are many: a cut costs the pieces' sums a way through memory and a join.
+// 128 rows a workgroup, us: 203 tokens after 3,893 of 32 heads 105 whole and 41 in
+// 8 pieces, 100 after 900 34 and 23 in 4; but 1,024 from the start 35 whole and 42
+// in 2, 512 from the start 22 and 27.
+struct ManyPlan {
+    int row_tiles, splits;
+};
+
+template <int NW>
+__device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s) {
+    const int rows = s.n * a.group;
+    return rows > a.few_most ? (rows + 32 * NW - 1) / (32 * NW) : 0;
+}
+
+template <int NW>
+__device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
+    int row_tiles = 0, most = 0;
+    for (int i = threadIdx.x & 63; i < a.c.seqs; i += 64) {
+        const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, i);
+        const int t = many_row_tiles<NW>(a, s);
+        const Reach r = reach_of(a, s);
+        row_tiles += t;
+        if (t) most = max(most, (r.end - r.begin + kManyTile - 1) / kManyTile);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        row_tiles += __shfl_xor(row_tiles, o, 64);
+        most = max(most, __shfl_xor(most, o, 64));
+    }
+    ManyPlan p;
+    p.row_tiles = __builtin_amdgcn_readfirstlane(row_tiles);
+    most = __builtin_amdgcn_readfirstlane(most);
+    p.splits = 1;
+    const int units = p.row_tiles * a.c.kv_heads;
+    if (units > 0 && units <= slots / 2 && most >= 12) {
+        const int splits = min(slots / units, most / 4);
+        if (most >= 32 || splits * units <= slots / 4) p.splits = splits;
+    }
+    return p;
+}
+
+// the sequence of row tile `rank` of all, and its first one
+template <int NW>
+__device__ __forceinline__ void many_find(const AttendArgs& a, int rank, int& seq, int& first) {
+    const int lane = threadIdx.x & 63;
+    for (int i = 0, before = 0; i < a.c.seqs; i += 64) {
+        const int n = i + lane < a.c.seqs ? many_row_tiles<NW>(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i + lane)) : 0;
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += u;
+        }
+        upto += before;
+        const unsigned long long has = __ballot(upto > rank);
+        if (has) {
+            const int l = __builtin_ctzll(has);
+            seq = i + l;
+            first = __builtin_amdgcn_readlane(upto - n, l);
+            return;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    seq = first = -1;
+}
+
+// the first of a unit's tiles that piece `split` of it takes
+__device__ __forceinline__ int split_from(int split, int tiles, int splits) {
+    return tiles / splits * split + min(split, tiles % splits);
+}
+
+// a piece's part: m and l of its rows, then their sums
+template <int D, int NW>
+constexpr int kManySlot = 32 * NW * (D + 2);
+
+template <int D, int NW, bool ONE>
+__global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, int slots) {
+    constexpr int kRows = 32 * NW, kThreads = 64 * NW;
+    constexpr int kKeys = 4 * D, kPer = 8 * D / kThreads;       // 16-byte pieces of a tile's keys; a thread's pieces of both
+    constexpr int kGroups = ONE ? 1 : 4, kWindow = 64 / kGroups;   // scales of a tile; tiles whose scales 64 lanes hold
+    static_assert(8 * D % kThreads == 0, "whole pieces a thread");
+    __shared__ __align__(16) _Float16 kt[2][D / 8][kManyTile][8];   // [8 dimensions][token]
+    __shared__ __align__(16) _Float16 vt[2][4][2][D][8];            // [16 tokens][half][dimension][8 tokens]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const ManyPlan plan = many_plan<NW>(a, slots);
+    // the last row tiles first: those have the most keys
+    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, splits = plan.splits;
+    const int rank = plan.row_tiles - 1 - rest / splits, split = rest % splits;
+    if (rank < 0) return;
+    int seq, first;
+    many_find<NW>(a, rank, seq, first);
+    if (seq < 0) return;
+    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+    const int rows = s.n * a.group, row0 = (rank - first) * kRows;
+    const Reach reach = reach_of(a, s);
+    const int token0 = s.first + row0 / a.group, token1 = s.first + (min(row0 + kRows, rows) - 1) / a.group;
+    const int reach_end = min(token1 + 1, reach.end), reach_begin = a.window > 0 ? max(0, token0 - a.window + 1) & ~63 : 0;
+    const int unit_tiles = max(0, reach_end - reach_begin + kManyTile - 1) / kManyTile;
+    const int tile0 = split_from(split, unit_tiles, splits), n = split_from(split + 1, unit_tiles, splits) - tile0;
+    const int begin = reach_begin + tile0 * kManyTile, end = min(reach_end, begin + n * kManyTile);
+    const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
+    const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
+
+    // the lane's row, and what the wave's rows see: all of [all_begin, all_end), none outside [any_begin, any_end)
+    const int wrow = row0 + 32 * wave, row = wrow + (lane & 31), half = lane >> 5;
+    const int rtoken = row / a.group, h = head * a.group + row - rtoken * a.group;
+    const bool there = row < rows;
+    const int position = s.first + rtoken;
+    const int row_end = there ? min(position + 1, end) : 0, row_begin = a.window > 0 ? position - a.window + 1 : 0;
+    const int wfirst = s.first + wrow / a.group, wlast = s.first + (min(wrow + 32, rows) - 1) / a.group;
+    const int all_end = min(wfirst + 1, end), all_begin = a.window > 0 ? wlast - a.window + 1 : 0;
+    const int any_end = wrow < rows ? min(wlast + 1, end) : 0, any_begin = a.window > 0 ? wfirst - a.window + 1 : 0;
+
+    f16x8 q[D / 16];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        u32x4 v = {0, 0, 0, 0};
+        if (there) v = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + rtoken) * a.q_stride + h * D + 16 * c + 8 * half);
+        q[c] = __builtin_bit_cast(f16x8, v ^ a.q_flip);
+    }
+
+    // Pages and scales of kWindow tiles, a lane each (of 16 tokens or of a tile): this window's and the next's.
+    // A negative page is none; sg is the factor of the scores, lv log2 of the values' scale.
+    struct Window {
+        int page;
+        float sg, lv;
+    } win, next;
+    auto load_pages = [&](Window& w, int first) {
+        const int t = begin + (first * kGroups + lane) * (kManyTile / kGroups);
+        const int id = t < end ? table[t >> a.c.page_shift] : -1;
+        w.page = id < a.c.num_pages ? id : -1;
+    };
+    auto load_scales = [&](Window& w) {
+        const f32x2 x = *reinterpret_cast<const f32x2*>(a.c.scales + 2 * (static_cast<size_t>(max(w.page, 0)) * a.c.kv_heads + head));
+        w.sg = fmaxf(x[0] * a.scale, 1e-30f);
+        w.lv = x[1] > 0.f ? __builtin_amdgcn_logf(x[1]) : kNoLog;
+    };
+    auto of_lane = [&](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+    // page of the tokens 16 g .. of tile j, which lies in the present window or the next
+    int window0 = 0;
+    auto page_at = [&](int j, int g) {
+        const int v = j - window0 < kWindow ? win.page : next.page;
+        return of_lane(v, (j % kWindow) * kGroups + (ONE ? 0 : g));
+    };
+
+    // pieces of a tile: the first kKeys are keys (token, 16 dimensions), the others values (16 tokens, a dimension)
+    u32x4 raw[kPer];
+    auto is_key = [&](int u) { return (u + 1) * kThreads <= kKeys || (u * kThreads < kKeys && tid + u * kThreads < kKeys); };
+    auto load_piece = [&](int u, int jk, int jv) {
+        const int p = tid + u * kThreads;
+        if (is_key(u)) {
+            const int t = begin + jk * kManyTile + (ONE ? 0 : p & 48);
+            int page;
+            if constexpr (ONE) page = page_at(jk, 0);
+            else page = __shfl(jk - window0 < kWindow ? win.page : next.page, (jk % kWindow) * 4 + ((p & 63) >> 4), 64);
+            const int8_t* at = a.c.k + (static_cast<size_t>(max(page, 0)) * a.c.kv_heads + head) * stride +
+                               static_cast<size_t>(t & (a.c.page_tokens - 1)) * D;
+            raw[u] = *reinterpret_cast<const u32x4*>(at + (ONE ? p & 63 : p & 15) * D + (p >> 6) * 16);
+        } else {
+            const int g = __builtin_amdgcn_readfirstlane((p - kKeys) / D);
+            const int t = begin + jv * kManyTile + 16 * g;
+            const int8_t* at = a.c.v + (static_cast<size_t>(max(page_at(jv, g), 0)) * a.c.kv_heads + head) * stride +
+                               static_cast<size_t>(t & (a.c.page_tokens - 1)) * D;
+            raw[u] = *reinterpret_cast<const u32x4*>(at + (p - kKeys) % D * 16);
+        }
+    };
+    auto write_piece = [&](int u, int bk, int bv) {
+        const int p = tid + u * kThreads;
+        const u32x4 x = raw[u];
+        if (is_key(u)) {
+            *reinterpret_cast<f16x8*>(kt[bk][(p >> 6) * 2][p & 63]) = to_half8(x[0], x[1]);
+            *reinterpret_cast<f16x8*>(kt[bk][(p >> 6) * 2 + 1][p & 63]) = to_half8(x[2], x[3]);
+        } else {
+            const int v = p - kKeys;
+            *reinterpret_cast<f16x8*>(vt[bv][v / D][0][v % D]) = to_half8(x[0], x[2]);
+            *reinterpret_cast<f16x8*>(vt[bv][v / D][1][v % D]) = to_half8(x[1], x[3]);
+        }
+    };
+    // keys of tile jk and values of tile jv, from memory and into LDS (tiles past the last: the last again)
+    auto load_tiles = [&](int jk, int jv) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) load_piece(u, min(jk, n - 1), min(jv, n - 1));
+    };
+    auto write_tiles = [&](int bk, int bv) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) write_piece(u, bk, bv);
+    };
+
+    f32x16 o[D / 32], sc[2];
+    for (f32x16& x : o)
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    auto scores = [&](f32x16 (&x)[2], int b) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    *reinterpret_cast<const f16x8*>(kt[b][2 * c + half][32 * t + (lane & 31)]), q[c], x[t], 0, 0, 0);
+    };
+    float m = kNoScore, l = 0.f, lref = kNoLog;
+    if (n > 0) {
+        load_pages(win, 0);
+        load_scales(win);
+        load_pages(next, kWindow);
+        next.sg = next.lv = 0.f;
+        u32x4 first_raw[kPer];
+        load_tiles(0, 0);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) first_raw[u] = raw[u];
+        load_tiles(1, 0);
+        u32x4 second_raw[kPer];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) second_raw[u] = raw[u];
+        load_tiles(2, 1);
+        u32x4 third_raw[kPer];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            third_raw[u] = raw[u];
+            raw[u] = first_raw[u];
+        }
+        write_tiles(0, 0);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) raw[u] = second_raw[u];
+        write_tiles(1, 0);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) raw[u] = third_raw[u];
+        __syncthreads();
+        scores(sc, 0);
+    }
+    // tile j, whose scores are in `cur`; those of tile j + 1 go into `ahead`
+    auto tile = [&](int j, int b, f32x16 (&cur)[2], f32x16 (&ahead)[2]) {
+        const int t0 = begin + j * kManyTile;
+        if (j == window0 + kWindow) {
+            win = next;
+            window0 = j;
+            load_pages(next, j + kWindow);
+        }
+        if (j == window0 + kWindow / 2) load_scales(next);
+        __syncthreads();
+        // a wave also goes through the tile before its first, for that one's scores
+        if (t0 < any_end && t0 + 2 * kManyTile > any_begin) {
+            float sg[kGroups], rel[kGroups], lnew = lref;
+            bool none[kGroups], holes = false;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int at = (j - window0) * kGroups + g;
+                sg[g] = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, win.sg), at));
+                rel[g] = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, win.lv), at));
+                none[g] = of_lane(win.page, at) < 0;
+                lnew = fmaxf(lnew, rel[g]);
+                holes |= none[g];
+            }
+#pragma unroll
+            for (float& x : rel) x = x > kNoLog ? fmaxf(x - lnew, -100.f) : 0.f;
+            if (holes || t0 < all_begin || t0 + kManyTile > all_end) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int token = t0 + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+                        if (none[ONE ? 0 : 2 * t + i / 8] || token < row_begin || token >= row_end) cur[t][i] = -INFINITY;
+                    }
+            }
+            // exponents with the maximum so far, and what they say of the new one
+            const float from = m > kNoScore ? m : 0.f;
+            float top = kNoScore;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float c = kWeightShift - kSlack + rel[ONE ? 0 : g] - from;
+                float x = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __builtin_fmaf(cur[g / 2][8 * (g % 2) + i], sg[ONE ? 0 : g], c);
+                    cur[g / 2][8 * (g % 2) + i] = e;
+                    x = fmaxf(x, e);
+                }
+                top = fmaxf(top, x - c);
+            }
+            const uint32_t ut = __builtin_bit_cast(uint32_t, top);
+            const auto sw = __builtin_amdgcn_permlane32_swap(ut, ut, false, false);
+            top = fmaxf(__builtin_bit_cast(float, static_cast<uint32_t>(sw[0])), __builtin_bit_cast(float, static_cast<uint32_t>(sw[1])));
+            if (__any(top > m + kSlack) || lnew != lref) {
+                const float mnew = fmaxf(m, top), alpha = fast_exp2(m - mnew), beta = alpha * fast_exp2(lref - lnew);
+                l *= alpha;
+#pragma unroll
+                for (f32x16& x : o) x *= beta;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) cur[t] += from - mnew;
+                m = mnew;
+                lref = lnew;
+            }
+            __builtin_amdgcn_s_setprio(1);
+            scores(ahead, b ^ 1);
+            f16x8 p[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = fast_exp2(cur[g / 2][8 * (g % 2) + i]);
+                    sum += w;
+                    p[g][i] = static_cast<_Float16>(w);
+                }
+                l += sum * fast_exp2(-rel[ONE ? 0 : g]);
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        *reinterpret_cast<const f16x8*>(vt[b][g][half][32 * d + (lane & 31)]), p[g], o[d], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
+        }
+        // keys of tile j + 2 and values of tile j + 1 go where those of tiles j and j - 1 were
+        write_tiles(b, b ^ 1);
+        load_tiles(j + 3, j + 2);
+    };
+    f32x16 sc2[2];
+    for (int t = 0; t < 2; ++t)
+        for (int i = 0; i < 16; ++i) sc2[t][i] = 0.f;
+    for (int j = 0; j < n; j += 2) {
+        tile(j, 0, sc, sc2);
+        if (j + 1 < n) tile(j + 1, 1, sc2, sc);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (!there) return;
+    if (splits > 1) {
+        float* slot = a.partials + static_cast<size_t>(blockIdx.x) * kManySlot<D, NW>;
+        const int r = 32 * wave + (lane & 31);
+        if (half == 0) {
+            slot[r] = m;
+            slot[kRows + r] = l;
+        }
+        const float unit = fast_exp2(fmaxf(lref, -120.f));
+        float* out = slot + 2 * kRows + r * D + 4 * half;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(out + 32 * d + 2 * i) =
+                    f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * unit;
+        return;
+    }
+    const float inv = l > 0.f ? fast_exp2(fmaxf(lref, -120.f)) / l : 0.f;
+    uint16_t* out = a.out + (s.row0 + rtoken) * a.out_stride + h * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            f16x4 v;
+            for (int j = 0; j < 4; ++j) v[j] = static_cast<_Float16>(o[d][i + j] * inv);
+            *reinterpret_cast<f16x4*>(out + 32 * d + 2 * i) = v;
+        }
+}
+
+// Joins the pieces of attend_many_kernel's units: a workgroup per 32 rows of a
+// unit, eight of them a wave.
+template <int D, int NW>
+__global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots) {
+    constexpr int kRows = 32 * NW;
+    const ManyPlan plan = many_plan<NW>(a, slots);
+    if (plan.splits == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int part = blockIdx.x % NW, rest = blockIdx.x / NW, head = rest % a.c.kv_heads;
+    const int rank = plan.row_tiles - 1 - rest / a.c.kv_heads;
+    if (rank < 0) return;
+    int seq, first;
+    many_find<NW>(a, rank, seq, first);
+    if (seq < 0) return;
+    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+    const int rows = s.n * a.group, row0 = (rank - first) * kRows;
+    const float* unit = a.partials +
+                        (static_cast<size_t>(rest / a.c.kv_heads) * plan.splits * a.c.kv_heads + head) * kManySlot<D, NW>;
+    const size_t step = static_cast<size_t>(a.c.kv_heads) * kManySlot<D, NW>;
+    for (int r = 32 * part + 8 * wave; r < min(rows - row0, 32 * part + 8 * wave + 8); ++r) {
+        float m = kNoScore;
+        for (int i = 0; i < plan.splits; ++i) m = fmaxf(m, unit[i * step + r]);
         float l = 0.f, o[D / 64] = {};
-        for (int w = w0; w <= w1; ++w) {
-            const float* p = slot(w);
+#pragma unroll 4
+        for (int i = 0; i < plan.splits; ++i) {
+            const float* p = unit + i * step;
             const float f = fast_exp2(p[r] - m);
-            l += f * p[kFewRows + r];
-            for (int i = 0; i < D / 64; ++i) o[i] += f * p[2 * kFewRows + r * D + lane + 64 * i];
+            l += f * p[kRows + r];
+            for (int j = 0; j < D / 64; ++j) o[j] += f * p[2 * kRows + r * D + lane + 64 * j];
         }
         const float inv = l > 0.f ? 1.f / l : 0.f;
         const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
         _Float16* out = reinterpret_cast<_Float16*>(a.out) + (s.row0 + t) * a.out_stride + h * D;
-        for (int i = 0; i < D / 64; ++i) out[lane + 64 * i] = static_cast<_Float16>(o[i] * inv);
+        for (int j = 0; j < D / 64; ++j) out[lane + 64 * j] = static_cast<_Float16>(o[j] * inv);
     }
 }
 

@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 
 #include "../../include/tetra.h"
 #include "attend.h"
@@ -55,13 +56,89 @@ int device_cus(int* cus) {
 constexpr int kFewGroupsPerCU = 2;
 constexpr size_t kMinAttendWorkspace = 4096;
 
-// parts of attend_few_kernel's workgroups
-size_t few_workspace(int cus) {
-    return static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128> * sizeof(float);
+// the parts of attend_few_kernel's workgroups, or the pieces of
+// attend_many_kernel's units (as many of 128 rows as of 256 in twice the room);
+// the kernels of a call run one after another
+size_t attend_workspace(int cus) {
+    const size_t few = static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128>;
+    const size_t many = static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 8>;
+    return (std::max(few, many) * sizeof(float) + 255) / 256 * 256;
 }
 
 constexpr long long kMaxGrid = 0x7FFFFFFFll;
 constexpr int kMaxVocab = 1 << 22;     // so that a row's sum of weights, 2^62 at most, fits 64 bits
+
+// How a call of tetra_kv_attend is spread; the lengths, and with them the
+// pieces, are the device's own matter.
+struct AttendPlan {
+    long long few_grid = 0, join_grid = 0;            // attend_few_kernel, 0: none
+    int row_tiles = 0, rows_most = 0;                 // of a sequence in it: row tiles; rows of one
+    long long many_grid = 0, many_join_grid = 0;      // attend_many_kernel, 0: none
+    int waves = 0, slots = 0;
+};
+
+AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
+    AttendPlan p;
+    const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
+    const long long reach = a.window > 0 ? std::min<long long>(kept, static_cast<long long>(a.window) + a.max_new + 64) : kept;
+    const long long tiles = (reach + tetra_dev::kFewTile - 1) / tetra_dev::kFewTile;
+    const long long most = static_cast<long long>(a.max_new) * a.group;      // rows of a sequence
+    const long long most_tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
+    const long long few_groups = static_cast<long long>(cus) * kFewGroupsPerCU;
+    const int few_rows = getenv("FEW") ? atoi(getenv("FEW")) : 64;
+    const bool all_few = most <= few_rows || (tiles == 1 && most_tiles * a.c.kv_heads * a.c.seqs <= few_groups);
+    a.few_most = static_cast<int>(all_few ? most : few_rows);
+    if (!all_few) {
+        // sequences of the most rows that the rows would make, and their units
+        const long long full = (a.rows + a.max_new - 1) / a.max_new;
+        const long long units8 = full * ((most + 255) / 256) * a.c.kv_heads;
+        p.waves = units8 < cus ? 4 : 8;
+        p.slots = p.waves == 8 ? cus : 2 * cus;
+        const long long rows = 32 * p.waves, all = static_cast<long long>(a.rows) * a.group;
+        const long long sequences = std::min<long long>(a.c.seqs, all / (few_rows + 1));
+        const long long units = (all / rows + sequences) * a.c.kv_heads;     // at most
+        p.many_grid = std::max<long long>(units, p.slots);
+        // no unit is cut where units, at least all / rows of them, fill the chip, or none can have 12 tiles
+        if (all / rows * a.c.kv_heads <= p.slots / 2 && reach > 11 * tetra_dev::kManyTile)
+            p.many_join_grid = std::min<long long>(units, p.slots / 2) * p.waves;
+        // every sequence has the most rows: none is left for the other kernel
+        if (static_cast<long long>(a.c.seqs) * a.max_new == a.rows) return p;
+    }
+    p.row_tiles = (a.few_most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
+    p.rows_most = std::min(a.few_most, tetra_dev::kFewRows);
+    p.few_grid = few_groups;
+    const long long units = static_cast<long long>(p.row_tiles) * a.c.kv_heads * a.c.seqs;
+    if (units > kMaxGrid / tiles) p.few_grid = kMaxGrid + 1;
+    if (tiles > 1) p.join_grid = units * p.rows_most;
+    return p;
+}
+
+template <int D, int NW>
+void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+    const dim3 g(static_cast<unsigned>(p.many_grid)), b(64 * NW), j(static_cast<unsigned>(p.many_join_grid));
+    if (a.c.page_tokens >= tetra_dev::kManyTile)
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, true>), g, b, 0, stream, a, p.slots);
+    else
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, false>), g, b, 0, stream, a, p.slots);
+    if (p.many_join_grid)
+        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, NW>), j, dim3(256), 0, stream, a, p.slots);
+}
+
+template <int D>
+int attend_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+    if (p.many_grid) {
+        if (p.waves == 8) attend_many_launch<D, 8>(a, p, stream);
+        else attend_many_launch<D, 4>(a, p, stream);
+        if (int st = launch_status()) return st;
+    }
+    if (p.few_grid) {
+        hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), dim3(static_cast<unsigned>(p.few_grid)), dim3(256), 0, stream, a);
+        if (p.join_grid)
+            hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), dim3(static_cast<unsigned>(p.join_grid)), dim3(256), 0,
+                               stream, a, static_cast<int>(p.few_grid), p.row_tiles, p.rows_most);
+    }
+    return launch_status();
+}
 
 }  // namespace
 
@@ -142,7 +219,7 @@ int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint1
 size_t tetra_kv_attend_workspace_bytes(void) {
     int cus = 0;
     if (device_cus(&cus)) return 0;
-    return few_workspace(cus);
+    return attend_workspace(cus);
 }
 
 int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
@@ -160,7 +237,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     int cus = 0;
     if (workspace_bytes < kMinAttendWorkspace) return TETRA_EINVAL;
     if (int st = device_cus(&cus)) return st;
-    if (workspace_bytes < few_workspace(cus)) return TETRA_EINVAL;
+    if (workspace_bytes < attend_workspace(cus)) return TETRA_EINVAL;
     a.q = q;
     a.starts = starts;
     a.out = out;
@@ -174,24 +251,10 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     a.q_heads = q_heads;
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
-    const int workers = cus * kFewGroupsPerCU;
-    const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
-    const long long reach = window > 0 ? std::min<long long>(kept, static_cast<long long>(window) + max_new + 64) : kept;
-    const long long row_tiles = (static_cast<long long>(max_new) * a.group + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
-    const long long units = row_tiles * a.c.kv_heads * a.c.seqs, tiles = (reach + tetra_dev::kFewTile - 1) / tetra_dev::kFewTile;
-    if (units > kMaxGrid / tiles) return TETRA_EINVAL;
-    const dim3 g(static_cast<unsigned>(workers)), join(static_cast<unsigned>(units)), b(256);
-#define TETRA_ATTEND(D)                                                                                       \
-    hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), g, b, 0, stream, a);                                \
-    if (tiles > 1)                                                                                            \
-        hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), join, b, 0, stream, a, workers, static_cast<int>(row_tiles))
-    if (cache->head_dim == 64) {
-        TETRA_ATTEND(64);
-    } else {
-        TETRA_ATTEND(128);
-    }
-#undef TETRA_ATTEND
-    return launch_status();
+    const AttendPlan p = attend_plan(a, cus);
+    if (p.few_grid > kMaxGrid || p.join_grid > kMaxGrid || p.many_grid > kMaxGrid || p.many_join_grid > kMaxGrid)
+        return TETRA_EINVAL;
+    return cache->head_dim == 64 ? attend_launch<64>(a, p, stream) : attend_launch<128>(a, p, stream);
 }
 
 size_t tetra_sample_workspace_bytes(int rows, int vocab) { return rows < 1 || vocab < 1 || vocab > kMaxVocab ? 0 : 256; }
