@@ -465,14 +465,24 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // How the device spreads the many-row units, found by every wave for itself: the
 // row tiles of all sequences, and the pieces that a unit's keys are cut into.
-// Units that do not fill the chip (`slots` workgroups at once) are cut, if their
-// keys are many: a cut costs the pieces' sums a way through memory and a join.
-// 128 rows a workgroup, us: 203 tokens after 3,893 of 32 heads 105 whole and 41 in
-// 8 pieces, 100 after 900 34 and 23 in 4; but 1,024 from the start 35 whole and 42
-// in 2, 512 from the start 22 and 27.
 struct ManyPlan {
     int row_tiles, splits;
 };
+
+// Units that do not fill the chip (`slots` workgroups at once) are cut along
+// their keys where that pays: a tile takes a workgroup 1.4 us, a piece's sums on
+// their way through memory D / 4096 us (128 rows; all pieces' together), the
+// join's launch 6 us.  Measured, 128 rows a workgroup, 32 heads of 128, us: 203
+// tokens after 3,893 105 whole and 41 in 8 pieces, 100 after 900 34 and 23 in 4;
+// 1,024 from the start 35 whole and 42 in 2, 512 from the start 22 and 27.
+template <int D, int NW>
+__host__ __device__ __forceinline__ int many_splits(int units, int tiles, int slots) {
+    if (units < 1 || 2 * units > slots || tiles < 8) return 1;
+    const float work = 1.4f * tiles, part = units * (D * NW / 16384.f);
+    float s = sqrtf(work / part);
+    s = fminf(s, fminf(static_cast<float>(slots / units), static_cast<float>(tiles / 4)));
+    return s >= 2.f && work * (1.f - 1.f / s) > 6.f + part * s ? static_cast<int>(s) : 1;
+}
 
 template <int NW>
 __device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s) {
@@ -480,7 +490,8 @@ __device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s
     return rows > a.few_most ? (rows + 32 * NW - 1) / (32 * NW) : 0;
 }
 
-template <int NW>
+// slots 0: no unit is cut
+template <int D, int NW>
 __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
     int row_tiles = 0, most = 0;
     for (int i = threadIdx.x & 63; i < a.c.seqs; i += 64) {
@@ -498,12 +509,7 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
     ManyPlan p;
     p.row_tiles = __builtin_amdgcn_readfirstlane(row_tiles);
     most = __builtin_amdgcn_readfirstlane(most);
-    p.splits = 1;
-    const int units = p.row_tiles * a.c.kv_heads;
-    if (units > 0 && units <= slots / 2 && most >= 12) {
-        const int splits = min(slots / units, most / 4);
-        if (most >= 32 || splits * units <= slots / 4) p.splits = splits;
-    }
+    p.splits = many_splits<D, NW>(p.row_tiles * a.c.kv_heads, most, slots);
     return p;
 }
 
@@ -550,7 +556,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     __shared__ __align__(16) _Float16 kt[2][D / 8][kManyTile][8];   // [8 dimensions][token]
     __shared__ __align__(16) _Float16 vt[2][4][2][D][8];            // [16 tokens][half][dimension][8 tokens]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const ManyPlan plan = many_plan<NW>(a, slots);
+    const ManyPlan plan = many_plan<D, NW>(a, slots);
     // the last row tiles first: those have the most keys
     const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, splits = plan.splits;
     const int rank = plan.row_tiles - 1 - rest / splits, split = rest % splits;
@@ -824,41 +830,46 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         }
 }
 
-// Joins the pieces of attend_many_kernel's units: a workgroup per 32 rows of a
-// unit, eight of them a wave.
+// Joins the pieces of attend_many_kernel's units: a workgroup per 1024 / D rows
+// of a unit, D / 4 lanes a row.
+template <int D>
+constexpr int kJoinRows = 1024 / D;
+
 template <int D, int NW>
 __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots) {
-    constexpr int kRows = 32 * NW;
-    const ManyPlan plan = many_plan<NW>(a, slots);
+    constexpr int kRows = 32 * NW, kParts = kRows / kJoinRows<D>;
+    const ManyPlan plan = many_plan<D, NW>(a, slots);
     if (plan.splits == 1) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int part = blockIdx.x % NW, rest = blockIdx.x / NW, head = rest % a.c.kv_heads;
+    const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts, head = rest % a.c.kv_heads;
     const int rank = plan.row_tiles - 1 - rest / a.c.kv_heads;
     if (rank < 0) return;
     int seq, first;
     many_find<NW>(a, rank, seq, first);
     if (seq < 0) return;
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int rows = s.n * a.group, row0 = (rank - first) * kRows;
+    const int row0 = (rank - first) * kRows, r = part * kJoinRows<D> + static_cast<int>(threadIdx.x) / (D / 4);
+    if (row0 + r >= s.n * a.group) return;
     const float* unit = a.partials +
                         (static_cast<size_t>(rest / a.c.kv_heads) * plan.splits * a.c.kv_heads + head) * kManySlot<D, NW>;
     const size_t step = static_cast<size_t>(a.c.kv_heads) * kManySlot<D, NW>;
-    for (int r = 32 * part + 8 * wave; r < min(rows - row0, 32 * part + 8 * wave + 8); ++r) {
-        float m = kNoScore;
-        for (int i = 0; i < plan.splits; ++i) m = fmaxf(m, unit[i * step + r]);
-        float l = 0.f, o[D / 64] = {};
+    const int d = static_cast<int>(threadIdx.x) % (D / 4) * 4;
+    float m = kNoScore;
 #pragma unroll 4
-        for (int i = 0; i < plan.splits; ++i) {
-            const float* p = unit + i * step;
-            const float f = fast_exp2(p[r] - m);
-            l += f * p[kRows + r];
-            for (int j = 0; j < D / 64; ++j) o[j] += f * p[2 * kRows + r * D + lane + 64 * j];
-        }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
-        _Float16* out = reinterpret_cast<_Float16*>(a.out) + (s.row0 + t) * a.out_stride + h * D;
-        for (int j = 0; j < D / 64; ++j) out[lane + 64 * j] = static_cast<_Float16>(o[j] * inv);
+    for (int i = 0; i < plan.splits; ++i) m = fmaxf(m, unit[i * step + r]);
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < plan.splits; ++i) {
+        const float* p = unit + i * step;
+        const float f = fast_exp2(p[r] - m);
+        l += f * p[kRows + r];
+        o += f * *reinterpret_cast<const f32x4*>(p + 2 * kRows + r * D + d);
     }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
+    f16x4 v;
+    for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
+    *reinterpret_cast<f16x4*>(a.out + (s.row0 + t) * a.out_stride + h * D + d) = v;
 }
 
 }  // namespace tetra_dev

@@ -7,7 +7,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cstdlib>
 
 #include "../../include/tetra.h"
 #include "attend.h"
@@ -77,6 +76,7 @@ struct AttendPlan {
     int waves = 0, slots = 0;
 };
 
+template <int D>
 AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     AttendPlan p;
     const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
@@ -85,22 +85,35 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     const long long most = static_cast<long long>(a.max_new) * a.group;      // rows of a sequence
     const long long most_tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
     const long long few_groups = static_cast<long long>(cus) * kFewGroupsPerCU;
-    const int few_rows = getenv("FEW") ? atoi(getenv("FEW")) : 64;
+    // attend_few_kernel reads the keys once for 16 rows.  Up to there it is ahead (64 sequences of 1,000 tokens, 8
+    // heads by 16 rows: 44 us against 64); with several row tiles only where few sequences leave the other kernel
+    // short of units (32 rows: 1 sequence of 4,096 14 us against 22, 8 of them 37 and 37, 32 of 1,000 43 and 36;
+    // 64 rows: 17 and 24, 58 and 43, 72 and 34).
+    const int few_rows = static_cast<int>(std::min<long long>(64, std::max<long long>(16, 2048 / (static_cast<long long>(a.c.seqs) * a.c.kv_heads))));
     const bool all_few = most <= few_rows || (tiles == 1 && most_tiles * a.c.kv_heads * a.c.seqs <= few_groups);
     a.few_most = static_cast<int>(all_few ? most : few_rows);
     if (!all_few) {
         // sequences of the most rows that the rows would make, and their units
         const long long full = (a.rows + a.max_new - 1) / a.max_new;
         const long long units8 = full * ((most + 255) / 256) * a.c.kv_heads;
+        // 128 rows a workgroup, two of them a CU, while those are one round of the chip (32 heads, 1,024 tokens 35 us
+        // against 41, 2,048 69 and 71), else 256 rows, whose tiles are turned into fp16 for twice as many (4,096 tokens
+        // 174 against 154)
         p.waves = units8 < cus ? 4 : 8;
-        p.slots = p.waves == 8 ? cus : 2 * cus;
+        const int slots = p.waves == 8 ? cus : 2 * cus;
         const long long rows = 32 * p.waves, all = static_cast<long long>(a.rows) * a.group;
         const long long sequences = std::min<long long>(a.c.seqs, all / (few_rows + 1));
         const long long units = (all / rows + sequences) * a.c.kv_heads;     // at most
-        p.many_grid = std::max<long long>(units, p.slots);
-        // no unit is cut where units, at least all / rows of them, fill the chip, or none can have 12 tiles
-        if (all / rows * a.c.kv_heads <= p.slots / 2 && reach > 11 * tetra_dev::kManyTile)
-            p.many_join_grid = std::min<long long>(units, p.slots / 2) * p.waves;
+        p.many_grid = std::max<long long>(units, slots);
+        // the device may cut units if it would at the fewest units and the most keys
+        const int least = static_cast<int>(std::min<long long>(std::max<long long>(all / rows, 1) * a.c.kv_heads, kMaxGrid));
+        const int longest = static_cast<int>((reach + tetra_dev::kManyTile - 1) / tetra_dev::kManyTile);
+        const int splits = p.waves == 8 ? tetra_dev::many_splits<D, 8>(least, longest, slots)
+                                        : tetra_dev::many_splits<D, 4>(least, longest, slots);
+        if (splits > 1) {
+            p.slots = slots;
+            p.many_join_grid = std::min<long long>(units, slots / 2) * (rows / tetra_dev::kJoinRows<D>);
+        }
         // every sequence has the most rows: none is left for the other kernel
         if (static_cast<long long>(a.c.seqs) * a.max_new == a.rows) return p;
     }
@@ -125,7 +138,9 @@ void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hip
 }
 
 template <int D>
-int attend_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
+    const AttendPlan p = attend_plan<D>(a, cus);
+    if (p.few_grid > kMaxGrid || p.join_grid > kMaxGrid || p.many_grid > kMaxGrid) return TETRA_EINVAL;
     if (p.many_grid) {
         if (p.waves == 8) attend_many_launch<D, 8>(a, p, stream);
         else attend_many_launch<D, 4>(a, p, stream);
@@ -251,10 +266,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     a.q_heads = q_heads;
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
-    const AttendPlan p = attend_plan(a, cus);
-    if (p.few_grid > kMaxGrid || p.join_grid > kMaxGrid || p.many_grid > kMaxGrid || p.many_join_grid > kMaxGrid)
-        return TETRA_EINVAL;
-    return cache->head_dim == 64 ? attend_launch<64>(a, p, stream) : attend_launch<128>(a, p, stream);
+    return cache->head_dim == 64 ? attend_launch<64>(a, cus, stream) : attend_launch<128>(a, cus, stream);
 }
 
 size_t tetra_sample_workspace_bytes(int rows, int vocab) { return rows < 1 || vocab < 1 || vocab > kMaxVocab ? 0 : 256; }
