@@ -269,7 +269,10 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     return cache->head_dim == 64 ? attend_launch<64>(a, cus, stream) : attend_launch<128>(a, cus, stream);
 }
 
-size_t tetra_sample_workspace_bytes(int rows, int vocab) { return rows < 1 || vocab < 1 || vocab > kMaxVocab ? 0 : 256; }
+size_t tetra_sample_workspace_bytes(int rows, int vocab) {
+    if (rows < 1 || vocab < 1 || vocab > kMaxVocab) return 0;
+    return static_cast<size_t>(rows) * tetra_dev::sample_row_space(vocab);
+}
 
 int tetra_sample(const float* logits, long long stride, int rows, int vocab, const float* temperature,
                  const int* top_k, const float* top_p, const float* min_p, const float* u, int* tokens,
@@ -280,9 +283,31 @@ int tetra_sample(const float* logits, long long stride, int rows, int vocab, con
     if (!aligned(logits, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) ||
         !aligned(min_p, 4) || !aligned(u, 4) || !aligned(tokens, 4) || !aligned(workspace, 256))
         return TETRA_EALIGN;
-    const tetra_dev::SampleArgs a{logits, stride, temperature, top_p, min_p, u, top_k, tokens, vocab};
-    hipLaunchKernelGGL(tetra_dev::sample_kernel, dim3(static_cast<unsigned>(rows)), dim3(tetra_dev::kSampleThreads), 0,
-                       stream, a);
+    tetra_dev::SampleArgs a;
+    a.logits = logits;
+    a.stride = stride;
+    a.temperature = temperature;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.u = u;
+    a.top_k = top_k;
+    a.tokens = tokens;
+    a.space = static_cast<uint8_t*>(workspace);
+    a.row_space = tetra_dev::sample_row_space(vocab);
+    a.vocab = vocab;
+    a.tiles = (vocab + tetra_dev::kSampleTile - 1) / tetra_dev::kSampleTile;
+    a.groups = (vocab + tetra_dev::kSampleGroup - 1) / tetra_dev::kSampleGroup;
+    // a tile a wave, up to four workgroups a CU over all rows
+    int cus = 0;
+    if (int st = device_cus(&cus)) return st;
+    a.parts = std::max(1, std::min((a.tiles + 3) / 4, 4 * cus / rows));
+    if (static_cast<long long>(rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
+    const dim3 g(static_cast<unsigned>(rows * a.parts)), b(256);
+    hipLaunchKernelGGL(tetra_dev::sample_max_kernel, g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::sample_cut_kernel, g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::sample_sum_kernel, g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::sample_token_kernel, dim3(static_cast<unsigned>(rows)), dim3(tetra_dev::kTokenThreads),
+                       8 * static_cast<size_t>(a.tiles), stream, a);
     return launch_status();
 }
 
