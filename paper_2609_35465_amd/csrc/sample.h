@@ -27,7 +27,8 @@ namespace tetra_dev {
 
 constexpr uint32_t kLowestKey = 0x007FFFFFu;   // of -inf
 constexpr int kSampleTile = 512;               // logits of a wave's step: 8 a lane, 64 apart
-constexpr int kSampleGroup = 128;              // logits with a maximum of their own
+constexpr int kMostGroups = 2048;              // maxima of lanes' logits that the first kernel leaves of a row
+constexpr int kMostParts = 128;                // workgroups of a row
 constexpr int kSampleBins = 2048;              // of the weights' logarithms, 0 down to -41
 constexpr float kBinsPerUnit = kSampleBins / 41.f;
 constexpr int kSampleList = 16384;             // candidates that a row's list holds
@@ -43,7 +44,8 @@ struct SampleArgs {
     int* tokens;
     uint8_t* space;        // SampleSpace of every row, row_space bytes each
     size_t row_space;
-    int vocab, tiles, groups, parts;
+    int vocab, tiles, parts;
+    int groups, wave_groups;      // of a row, and of each of its 4 parts waves: 16 (of four lanes) or 4 (of sixteen)
 };
 
 // What a row's kernels leave for each other, followed by the tiles' sums
@@ -51,8 +53,10 @@ struct SampleArgs {
 struct SampleSpace {
     unsigned long long mass[kSampleBins];
     unsigned count[kSampleBins];
+    unsigned top_key;                // key of the largest logit
+    int first;                       // index of the first of the largest logits (greedy rows)
     unsigned listed;                 // candidates found; the list holds the first kSampleList
-    unsigned low_key;                // candidates by key: this and above
+    int group_bin;                   // candidates by groups: of this bin of kGroupBins and those above
     int bin_low, bin_high, bin_k;    // candidates by bin: bin_low .. bin_high, and bin_k
     unsigned count_k;                // tokens above bin_k
     unsigned long long mass_low, mass_k, mass_all;   // weight above bin_low, above bin_k, of all
@@ -72,14 +76,15 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     return __builtin_bit_cast(float, key >> 31 ? key ^ 0x80000000u : ~key);
 }
 
-// t, a weight's logarithm
+// t, a weight's logarithm; -48 and below, and of NaN, is -48 (the weight is 0)
 __device__ __forceinline__ float log_of(float x, float top, float inverse) {
 #pragma clang fp contract(off)
-    return fmaxf(x == top ? 0.f : (x - top) * inverse, -64.f);
+    return fmaxf(x == top ? 0.f : (x - top) * inverse, -48.f);
 }
 
 // floor(2^40 2^t): the series of 2^f to f^7 with |f| <= 1/2 (its remainder is
-// 5e-9), every operation rounded by itself
+// 5e-9), every operation rounded by itself; then its mantissa, 2^40 for 1.0,
+// shifted by the exponent
 __device__ __forceinline__ uint64_t weight_of(float t) {
 #pragma clang fp contract(off)
     const float whole = rintf(t), f = t - whole;
@@ -91,9 +96,9 @@ __device__ __forceinline__ uint64_t weight_of(float t) {
     p = p * f + 0x1.ebfbe0p-3f;
     p = p * f + 0x1.62e430p-1f;
     p = p * f + 1.f;
-    const float s = p * __builtin_bit_cast(float, (static_cast<int>(whole) + 167) << 23);
-    const uint32_t hi = static_cast<uint32_t>(s * 0x1p-20f);
-    return (static_cast<uint64_t>(hi) << 20) + static_cast<uint32_t>(s - static_cast<float>(hi) * 0x1p20f);
+    const uint32_t q = __builtin_bit_cast(uint32_t, p) + (static_cast<uint32_t>(static_cast<int>(whole)) << 23);
+    const uint32_t mantissa = (q & 0x7FFFFFu) | 0x800000u;
+    return (static_cast<uint64_t>(mantissa) << 17) >> (127 - (q >> 23));
 }
 
 constexpr float kNoWeight = -41.f;     // weights of this logarithm and below are 0
@@ -101,64 +106,92 @@ constexpr float kNoWeight = -41.f;     // weights of this logarithm and below ar
 // falls with t
 __device__ __forceinline__ int bin_of(float t) { return min(kSampleBins - 1, static_cast<int>(t * -kBinsPerUnit)); }
 
+// the same in 256 bins, for the groups' maxima
+constexpr int kGroupBins = 256;
+__device__ __forceinline__ int group_bin_of(float t) {
+    return min(kGroupBins - 1, static_cast<int>(t * -(kGroupBins / 41.f)));
+}
+
 // the order of the tokens in one number: by key, then by index from the first on
 __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) {
     return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(~index);
 }
 
-template <class T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-template <class T>
-__device__ __forceinline__ T wave_max(T v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = max(v, static_cast<T>(__shfl_xor(v, o, 64)));
-    return v;
-}
-
-// sum of the lanes up to and with this one
-template <class T>
-__device__ __forceinline__ T wave_upto(T v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T u = __shfl_up(v, o, 64);
-        if ((threadIdx.x & 63) >= static_cast<unsigned>(o)) v += u;
+// v of the lane that the DPP control names, 0 where there is none or the row of
+// lanes is masked
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T dpp(T v) {
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t u = v;
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, ROWS, 0xF, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, ROWS, 0xF, false);
+        return static_cast<T>(static_cast<uint64_t>(hi) << 32 | lo);
+    } else {
+        return static_cast<T>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xF, false));
     }
-    return v;
 }
 
-// the sum over WAVES waves, in every thread
+template <class T>
+__device__ __forceinline__ T lane_of(T v, int lane) {
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t u = v;
+        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(u), lane);
+        const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane);
+        return static_cast<T>(static_cast<uint64_t>(hi) << 32 | lo);
+    } else {
+        return static_cast<T>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+    }
+}
+
+// over the lanes up to and with this one: the sum, or for unsigned numbers the maximum
+struct Sum {
+    template <class T>
+    __device__ T operator()(T a, T b) const { return a + b; }
+};
+struct Max {
+    template <class T>
+    __device__ T operator()(T a, T b) const { return a > b ? a : b; }
+};
+
+template <class F, class T>
+__device__ __forceinline__ T row_upto(F f, T v) {      // rows of 16 lanes
+    v = f(v, dpp<0x111, 0xF>(v));
+    v = f(v, dpp<0x112, 0xF>(v));
+    v = f(v, dpp<0x114, 0xF>(v));
+    return f(v, dpp<0x118, 0xF>(v));
+}
+
+template <class F, class T>
+__device__ __forceinline__ T wave_upto(F f, T v) {
+    v = row_upto(f, v);
+    v = f(v, dpp<0x142, 0xA>(v));
+    return f(v, dpp<0x143, 0xC>(v));
+}
+
+template <class F, class T>
+__device__ __forceinline__ T wave_all(F f, T v) { return lane_of(wave_upto(f, v), 63); }
+
+// the sum over WAVES (at most 16) waves, in every thread
 template <int WAVES, class T>
 __device__ T group_sum(T v, T* lds) {
-    v = wave_sum(v);
+    v = wave_all(Sum(), v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    T s = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) s += lds[w];
-    return s;
+    return lane_of(row_upto(Sum(), lds[threadIdx.x % WAVES]), WAVES - 1);
 }
 
 // the sum over the threads up to and with this one, and over all
 template <int WAVES, class T>
 __device__ T group_upto(T v, T* lds, T* all) {
-    v = wave_upto(v);
+    v = wave_upto(Sum(), v);
     __syncthreads();
     if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    T s = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w == static_cast<int>(threadIdx.x >> 6)) v += s;
-        s += lds[w];
-    }
-    *all = s;
-    return v;
+    const T waves = row_upto(Sum(), lds[threadIdx.x % WAVES]);
+    *all = lane_of(waves, WAVES - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return wave ? v + lane_of(waves, wave - 1) : v;
 }
 
 enum SampleKind { kFixed, kByGroups, kByBins, kUnfiltered };
@@ -169,39 +202,33 @@ struct SampleRow {
     SampleSpace* space;
     float top, inverse, top_p;
     uint32_t top_key;
-    double min_weight;
+    uint64_t min_weight;
     int k;               // of top-k, 0: off
     SampleKind kind;     // kFixed: the token needs no weights (greedy, or nothing but -inf)
 };
 
-// by every thread of a workgroup of WAVES waves, with a place in LDS each
-template <int WAVES>
-__device__ SampleRow sample_row(const SampleArgs& a, int row, uint32_t* lds) {
+// before the largest logit is known: kFixed only by the temperature
+__device__ __forceinline__ SampleRow sample_settings(const SampleArgs& a, int row) {
     SampleRow r;
     r.x = a.logits + row * a.stride;
     r.space = reinterpret_cast<SampleSpace*>(a.space + row * a.row_space);
-    const unsigned* largest = r.space->largest(a.tiles);
     const float temperature = a.temperature[row];
-    r.top_p = a.top_p[row];
-    r.min_weight = fmin(fmax(static_cast<double>(a.min_p[row]), 0.0), 1.0) * 0x1p40;
-    r.k = a.top_k[row];
-    uint32_t best = 0;
-    for (int i = threadIdx.x; i < a.groups; i += 64 * WAVES) best = max(best, largest[i]);
-    best = wave_max(best);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = best;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) best = max(best, lds[w]);
-    __syncthreads();
-    r.top_key = best;
-    r.top = logit_of(best);
     r.inverse = 0x1.715476p+0f / temperature;
+    r.top_p = a.top_p[row];
+    r.min_weight = static_cast<uint64_t>(ceil(fmin(fmax(static_cast<double>(a.min_p[row]), 0.0), 1.0) * 0x1p40));
+    r.k = a.top_k[row];
     if (r.k < 0 || r.k >= a.vocab) r.k = 0;
-    if (best == kLowestKey || !(temperature > 0.f)) r.kind = kFixed;
+    if (!(temperature > 0.f)) r.kind = kFixed;
     else if (r.k > 0 && r.k <= kMostByGroups && 2 * r.k <= a.groups) r.kind = kByGroups;
     else if (r.k > 0 || r.top_p < 1.f) r.kind = kByBins;
     else r.kind = kUnfiltered;
     return r;
+}
+
+__device__ __forceinline__ void sample_top(SampleRow& r, uint32_t top_key) {
+    r.top_key = top_key;
+    r.top = logit_of(top_key);
+    if (r.top_key == kLowestKey) r.kind = kFixed;
 }
 
 // ceil(p mass), one at least
@@ -210,241 +237,325 @@ __device__ __forceinline__ uint64_t share_of(float p, uint64_t mass) {
     return s >= 1.0 ? static_cast<uint64_t>(s) : 1;
 }
 
-// appends the flagged lanes' indices to the row's list
-__device__ __forceinline__ void append(SampleSpace* space, bool has, int index) {
-    const unsigned long long b = __ballot(has);
-    if (!b) return;
-    const int lane = threadIdx.x & 63, leader = __builtin_ctzll(b);
-    unsigned at = 0;
-    if (lane == leader) at = atomicAdd(&space->listed, static_cast<unsigned>(__popcll(b)));
-    at = __shfl(at, leader, 64) + __popcll(b & ((1ull << lane) - 1));
-    if (has && at < kSampleList) space->list[at] = index;
+// A workgroup's candidates, gathered in LDS so that the row's list takes one
+// atomic for all of them (each costs a way to memory and back).
+struct Candidates {
+    static constexpr int kHeld = 1024;
+    unsigned count, at;
+    int index[kHeld];
+
+    __device__ __forceinline__ void clear() {
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+    }
+    __device__ __forceinline__ void add(bool has, int i, SampleSpace* space) {
+        const unsigned long long b = __ballot(has);
+        if (!b) return;
+        const int lane = threadIdx.x & 63, leader = __builtin_ctzll(b);
+        unsigned n = 0;
+        if (lane == leader) n = atomicAdd(&count, static_cast<unsigned>(__popcll(b)));
+        n = lane_of(n, leader) + __popcll(b & ((1ull << lane) - 1));
+        if (has && n < kHeld) index[n] = i;
+        if (has && n >= kHeld) {       // no room: straight to the list
+            const unsigned to = atomicAdd(&space->listed, 1u);
+            if (to < kSampleList) space->list[to] = i;
+        }
+    }
+    __device__ __forceinline__ void to_list(SampleSpace* space) {
+        __syncthreads();
+        const unsigned n = count < kHeld ? count : kHeld;
+        if (n == 0) return;
+        if (threadIdx.x == 0) at = atomicAdd(&space->listed, n);
+        __syncthreads();
+        for (unsigned i = threadIdx.x; i < n; i += blockDim.x)
+            if (at + i < kSampleList) space->list[at + i] = index[i];
+    }
+};
+
+// A wave's tiles, each lane's eight logits of one in x (-inf past the row's end):
+// f(tile, x).  The next tile is on its way meanwhile.
+template <class F>
+__device__ __forceinline__ void each_tile(const SampleArgs& a, const float* row, int first, F f) {
+    const int lane = threadIdx.x & 63, step = a.parts * 4;
+    auto load = [&](float (&x)[8], int t) {
+        const int i0 = t * kSampleTile + lane;
+        if ((t + 1) * kSampleTile <= a.vocab) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = row[i0 + 64 * j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = i0 + 64 * j < a.vocab ? row[i0 + 64 * j] : -INFINITY;
+        }
+    };
+    float x[8], next[8];
+    if (first < a.tiles) load(x, first);
+    for (int t = first; t < a.tiles; t += step) {
+        if (t + step < a.tiles) load(next, t + step);
+        f(t, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = next[j];
+    }
 }
 
-// First: the largest key of every 128 logits; and the row's space is cleared.
+// First: the largest logits, a maximum for every four or sixteen lanes of a wave;
+// and the row's space is cleared.
 __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float* x = a.logits + row * a.stride;
+    const int lane = threadIdx.x & 63, wave = part * 4 + (threadIdx.x >> 6);
     SampleSpace* space = reinterpret_cast<SampleSpace*>(a.space + row * a.row_space);
     for (int i = part * 256 + threadIdx.x; i < kSampleBins; i += a.parts * 256) {
         space->mass[i] = 0;
         space->count[i] = 0;
     }
-    if (part == 0 && threadIdx.x == 0) space->listed = 0;
-    unsigned* largest = space->largest(a.tiles);
-    for (int t = part * 4 + wave; t < a.tiles; t += a.parts * 4) {
-        uint32_t key[4] = {0, 0, 0, 0};
+    if (part == 0 && threadIdx.x == 0) {
+        space->listed = 0;
+        space->first = a.vocab;
+    }
+    float top = -INFINITY;
+    each_tile(a, a.logits + row * a.stride, wave, [&](int, const float (&x)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = t * kSampleTile + 64 * j + lane;
-            if (i < a.vocab) key[j / 2] = max(key[j / 2], key_of(x[i]));
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            key[g] = wave_max(key[g]);
-            if (lane == g && 4 * t + g < a.groups) largest[4 * t + g] = key[g];
-        }
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);      // of NaN and a number, the number
+    });
+    uint32_t key = key_of(top);
+    key = Max()(key, dpp<0xB1, 0xF>(key));
+    key = Max()(key, dpp<0x4E, 0xF>(key));
+    unsigned* largest = space->largest(a.tiles) + wave * a.wave_groups;
+    if (a.wave_groups == 16) {
+        if (lane % 4 == 0) largest[lane / 4] = key;
+    } else {
+        key = Max()(key, dpp<0x141, 0xF>(key));
+        key = Max()(key, dpp<0x140, 0xF>(key));
+        if (lane % 16 == 0) largest[lane / 16] = key;
     }
 }
 
-// Then what a filtered row's cut is found from.  A top-k of at most 512 goes by
-// the groups: their k-th largest maximum is at most the k-th largest logit, so
-// the logits from there on (some 1.4 k of them, if the large ones lie anywhere)
-// hold the k.  Other filtered rows count and weigh their tokens in 2,048 bins of
-// the weight's logarithm.
+// Then the sums of rows without a cut, and what the others' cut is found from.
+// A top-k of at most 512 goes by the groups: their k-th largest maximum is at
+// most the k-th largest logit, so the logits from its bin on (some 1.4 k of
+// them, if the large ones lie anywhere) hold the k.  Other filtered rows count and
+// weigh their tokens in 2,048 bins of the weight's logarithm.  Greedy rows look
+// for the first of the largest logits.
 __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
     __shared__ unsigned long long mass[kSampleBins];
     __shared__ unsigned count[kSampleBins];
+    __shared__ Candidates found;
     __shared__ uint32_t lds[4];
+    __shared__ int last;
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const SampleRow r = sample_row<4>(a, row, lds);
-    if (r.kind == kByGroups) {
-        // the key's upper 16 bits, rounded down: a bound just as well
-        const unsigned* largest = r.space->largest(a.tiles);
-        constexpr int kHeld = 8;
-        uint32_t held[kHeld];
+    const int tid = threadIdx.x, lane = tid & 63, wave = part * 4 + (tid >> 6);
+    SampleRow r = sample_settings(a, row);
+    constexpr int kHeld = kMostGroups / 256;
+    uint32_t held[kHeld], best = 0;
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) held[i] = tid + 256 * i < a.groups ? largest[tid + 256 * i] : 0;
-        uint32_t low = 0;
-        for (int bit = 31; bit >= 16; --bit) {
-            const uint32_t t = low | 1u << bit;
-            uint32_t c = 0;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) c += held[i] >= t;
-            for (int i = tid + 256 * kHeld; i < a.groups; i += 256) c += largest[i] >= t;
-            if (group_sum<4>(c, lds) >= static_cast<uint32_t>(r.k)) low = t;
-        }
-        if (part == 0 && tid == 0) r.space->low_key = low;
-        for (int t = part * 4 + wave; t < a.tiles; t += a.parts * 4) {
-            float x[8];
+    for (int i = 0; i < kHeld; ++i) {
+        held[i] = tid + 256 * i < a.groups ? r.space->largest(a.tiles)[tid + 256 * i] : 0;
+        best = Max()(best, held[i]);
+    }
+    best = wave_all(Max(), best);
+    if (lane == 0) lds[tid >> 6] = best;
+    count[tid] = 0;
+    __syncthreads();
+    sample_top(r, Max()(Max()(lds[0], lds[1]), Max()(lds[2], lds[3])));
+    if (part == 0 && tid == 0) r.space->top_key = r.top_key;
+    if (r.kind == kUnfiltered) {
+        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+            uint64_t sum = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = t * kSampleTile + 64 * j + lane;
-                x[j] = i < a.vocab ? r.x[i] : -INFINITY;
+                const uint64_t w = weight_of(log_of(x[j], r.top, r.inverse));
+                sum += w >= r.min_weight ? w : 0;
             }
+            sum = wave_all(Sum(), sum);
+            if (lane == 0) r.space->sums()[t] = sum;
+        });
+    } else if (r.kind == kByGroups) {
+        // the bin of the k-th largest maximum (the last if fewer have a weight)
+        static_assert(kGroupBins == 256, "a bin a thread");
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const float l = log_of(logit_of(held[i]), r.top, r.inverse);
+            if (held[i] && l > kNoWeight) atomicAdd(&count[group_bin_of(l)], 1u);
+        }
+        if (tid == 0) last = kGroupBins - 1;
+        found.clear();
+        const uint32_t mine = count[tid];
+        uint32_t all;
+        const uint32_t upto = group_upto<4>(mine, lds, &all);
+        if (upto >= static_cast<uint32_t>(r.k) && upto - mine < static_cast<uint32_t>(r.k)) last = tid;
+        __syncthreads();
+        const int bin = last;
+        if (part == 0 && tid == 0) r.space->group_bin = bin;
+        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t key = key_of(x[j]);
-                if (__any(key >= low))
-                    append(r.space, key >= low && log_of(logit_of(key), r.top, r.inverse) > kNoWeight,
-                           t * kSampleTile + 64 * j + lane);
+                const float l = log_of(x[j], r.top, r.inverse);
+                const bool has = l > kNoWeight && group_bin_of(l) <= bin;
+                if (__any(has)) found.add(has, t * kSampleTile + 64 * j + lane, r.space);
             }
-        }
+        });
+        found.to_list(r.space);
     } else if (r.kind == kByBins) {
         for (int i = tid; i < kSampleBins; i += 256) {
             mass[i] = 0;
             count[i] = 0;
         }
         __syncthreads();
-        for (int t = part * 4 + wave; t < a.tiles; t += a.parts * 4) {
-            float x[8];
+        each_tile(a, r.x, wave, [&](int, const float (&x)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = t * kSampleTile + 64 * j + lane;
-                x[j] = i < a.vocab ? r.x[i] : -INFINITY;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float l = log_of(logit_of(key_of(x[j])), r.top, r.inverse);
+                const float l = log_of(x[j], r.top, r.inverse);
                 if (l > kNoWeight) {
                     atomicAdd(&mass[bin_of(l)], static_cast<unsigned long long>(weight_of(l)));
                     atomicAdd(&count[bin_of(l)], 1u);
                 }
             }
-        }
+        });
         __syncthreads();
         for (int i = tid; i < kSampleBins; i += 256)
             if (count[i]) {
                 atomicAdd(&r.space->mass[i], mass[i]);
                 atomicAdd(&r.space->count[i], count[i]);
             }
+    } else if (r.top_key != kLowestKey) {
+        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = t * kSampleTile + 64 * j + lane;
+                if (i < a.vocab && key_of(x[j]) == r.top_key) atomicMin(&r.space->first, i);
+            }
+        });
     }
 }
 
-// Then the sums: of every tile's weights that are left for certain.  A row in
-// bins first finds the bins that its cuts can lie in (top-p's share is one of
-// top-k's weight, which bin_k leaves open a little), and lists the tokens there.
-__global__ __launch_bounds__(256) void sample_sum_kernel(SampleArgs a) {
+// Then rows in bins: the bins that their cuts can lie in (top-p's share is one
+// of top-k's weight, which bin_k leaves open a little), the tokens there, and
+// of every tile the sum of the weights above them.
+__global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a) {
     __shared__ uint32_t lds[4];
-    __shared__ unsigned long long lds64[4], found_mass[4];
+    __shared__ uint64_t lds64[4];
+    __shared__ unsigned long long found_mass[3];
     __shared__ unsigned found_count;
-    __shared__ int found_bin[4];
+    __shared__ int found_bin[3];
+    __shared__ Candidates found;
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const SampleRow r = sample_row<4>(a, row, lds);
-    if (r.kind != kByBins && r.kind != kUnfiltered) return;
-    int low = kSampleBins, high = -1, bin_k = -1;
-    if (r.kind == kByBins) {
-        constexpr int kPer = kSampleBins / 256;
-        unsigned long long m[kPer], mine_mass = 0, all_mass;
-        uint32_t c[kPer], mine_count = 0, all_count;
+    const int tid = threadIdx.x, lane = tid & 63, wave = part * 4 + (tid >> 6);
+    SampleRow r = sample_settings(a, row);
+    if (r.kind != kByBins) return;
+    sample_top(r, r.space->top_key);
+    if (r.kind != kByBins) return;
+    constexpr int kPer = kSampleBins / 256;
+    uint64_t m[kPer], mine_mass = 0, all_mass;
+    uint32_t c[kPer], mine_count = 0, all_count;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        m[i] = r.space->mass[tid * kPer + i];
+        c[i] = r.space->count[tid * kPer + i];
+        mine_mass += m[i];
+        mine_count += c[i];
+    }
+    if (tid < 3) found_bin[tid] = -1;
+    found.clear();
+    const uint64_t mass0 = group_upto<4>(mine_mass, lds64, &all_mass) - mine_mass;
+    const uint32_t count0 = group_upto<4>(mine_count, lds, &all_count) - mine_count;
+    // the bin in which the count reaches k
+    const bool by_k = r.k > 0 && static_cast<uint32_t>(r.k) < all_count;
+    if (by_k) {
+        uint64_t mb = mass0;
+        uint32_t cb = count0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            m[i] = r.space->mass[tid * kPer + i];
-            c[i] = r.space->count[tid * kPer + i];
-            mine_mass += m[i];
-            mine_count += c[i];
-        }
-        const unsigned long long mass0 = group_upto<4>(mine_mass, lds64, &all_mass) - mine_mass;
-        const uint32_t count0 = group_upto<4>(mine_count, lds, &all_count) - mine_count;
-        if (tid < 4) found_bin[tid] = -1;
-        __syncthreads();
-        // the bin in which the count reaches k
-        const bool by_k = r.k > 0 && static_cast<uint32_t>(r.k) < all_count;
-        {
-            unsigned long long mb = mass0;
-            uint32_t cb = count0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (by_k && cb < static_cast<uint32_t>(r.k) && cb + c[i] >= static_cast<uint32_t>(r.k)) {
-                    found_bin[0] = tid * kPer + i;
-                    found_count = cb;
-                    found_mass[0] = mb;
-                    found_mass[1] = mb + m[i];
-                }
-                mb += m[i];
-                cb += c[i];
+            if (cb < static_cast<uint32_t>(r.k) && cb + c[i] >= static_cast<uint32_t>(r.k)) {
+                found_bin[0] = tid * kPer + i;
+                found_count = cb;
+                found_mass[0] = mb;
+                found_mass[1] = mb + m[i];
             }
-        }
-        __syncthreads();
-        bin_k = found_bin[0];
-        const unsigned long long least = by_k ? found_mass[0] : all_mass, most = by_k ? found_mass[1] : all_mass;
-        if (r.top_p < 1.f) {
-            const unsigned long long from = share_of(r.top_p, least), to = share_of(r.top_p, most);
-            unsigned long long mb = mass0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (mb < from && mb + m[i] >= from) {
-                    found_bin[1] = tid * kPer + i;
-                    found_mass[2] = mb;
-                }
-                if (mb < to && mb + m[i] >= to) found_bin[2] = tid * kPer + i;
-                mb += m[i];
-            }
-            __syncthreads();
-            low = found_bin[1];
-            high = by_k ? min(found_bin[2], bin_k) : found_bin[2];
-        } else {
-            low = high = bin_k;
-            if (tid == 0) found_mass[2] = found_mass[0];
-            __syncthreads();
-        }
-        if (low < 0) low = high = kSampleBins;      // top-k leaves every token that has a weight
-        if (part == 0 && tid == 0) {
-            r.space->bin_low = low;
-            r.space->bin_high = high;
-            r.space->bin_k = bin_k;
-            r.space->count_k = by_k ? found_count : 0;
-            r.space->mass_k = by_k ? found_mass[0] : 0;
-            r.space->mass_low = low < kSampleBins ? found_mass[2] : all_mass;
-            r.space->mass_all = all_mass;
+            mb += m[i];
+            cb += c[i];
         }
     }
-    for (int t = part * 4 + wave; t < a.tiles; t += a.parts * 4) {
-        float x[8];
+    __syncthreads();
+    const int bin_k = found_bin[0];
+    int low = bin_k, high = bin_k;
+    uint64_t mass_low = by_k ? found_mass[0] : all_mass;
+    if (r.top_p < 1.f) {
+        const uint64_t from = share_of(r.top_p, by_k ? found_mass[0] : all_mass);
+        const uint64_t to = share_of(r.top_p, by_k ? found_mass[1] : all_mass);
+        uint64_t mb = mass0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = t * kSampleTile + 64 * j + lane;
-            x[j] = i < a.vocab ? r.x[i] : -INFINITY;
+        for (int i = 0; i < kPer; ++i) {
+            if (mb < from && mb + m[i] >= from) {
+                found_bin[1] = tid * kPer + i;
+                found_mass[2] = mb;
+            }
+            if (mb < to && mb + m[i] >= to) found_bin[2] = tid * kPer + i;
+            mb += m[i];
         }
-        unsigned long long sum = 0;
+        __syncthreads();
+        low = found_bin[1];
+        high = by_k && bin_k < found_bin[2] ? bin_k : found_bin[2];
+        mass_low = found_mass[2];
+    } else if (!by_k) {
+        low = high = kSampleBins;      // top-k leaves every token that has a weight
+    }
+    if (part == 0 && tid == 0) {
+        r.space->bin_low = low;
+        r.space->bin_high = high;
+        r.space->bin_k = bin_k;
+        r.space->count_k = by_k ? found_count : 0;
+        r.space->mass_k = by_k ? found_mass[0] : 0;
+        r.space->mass_low = mass_low;
+        r.space->mass_all = all_mass;
+    }
+    each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+        uint64_t sum = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float l = log_of(logit_of(key_of(x[j])), r.top, r.inverse);
+            const float l = log_of(x[j], r.top, r.inverse);
+            const int b = bin_of(l);
             const uint64_t w = weight_of(l);
-            if (r.kind == kByBins) {
-                const int b = bin_of(l);
-                if (b < low && static_cast<double>(w) >= r.min_weight) sum += w;
-                append(r.space, l > kNoWeight && ((b >= low && b <= high) || b == bin_k), t * kSampleTile + 64 * j + lane);
-            } else if (static_cast<double>(w) >= r.min_weight) {
-                sum += w;
-            }
+            sum += b < low && w >= r.min_weight ? w : 0;
+            found.add(l > kNoWeight && ((b >= low && b <= high) || b == bin_k), t * kSampleTile + 64 * j + lane, r.space);
         }
-        sum = wave_sum(sum);
+        sum = wave_all(Sum(), sum);
         if (lane == 0) r.space->sums()[t] = sum;
-    }
+    });
+    found.to_list(r.space);
+}
+
+// v of lane ^ STEP
+template <int STEP>
+__device__ __forceinline__ uint64_t across(uint64_t v) {
+    if constexpr (STEP == 1) return dpp<0xB1, 0xF>(v);
+    else if constexpr (STEP == 2) return dpp<0x4E, 0xF>(v);
+    else if constexpr (STEP == 4) return dpp<0x1B, 0xF>(dpp<0x141, 0xF>(v));
+    else if constexpr (STEP == 8) return dpp<0x128, 0xF>(v);
+    else return __shfl_xor(v, STEP, 64);
 }
 
 // sorts one number a thread, the first m (a power of two, at least 64) of the
 // workgroup, falling
 __device__ __forceinline__ uint64_t sorted(uint64_t v, int m, uint64_t* lds) {
     const int tid = threadIdx.x;
-    for (int size = 2; size <= m; size <<= 1)
-        for (int step = size >> 1; step >= 1; step >>= 1) {
-            uint64_t other;
-            if (step >= 64) {
-                __syncthreads();
-                lds[tid] = v;
-                __syncthreads();
-                other = lds[tid ^ step];
-            } else {
-                other = __shfl_xor(v, step, 64);
-            }
-            const bool larger_first = ((tid & size) == 0) == ((tid & step) == 0);
-            v = larger_first ? max(v, other) : min(v, other);
+    for (int size = 2; size <= m; size <<= 1) {
+        const bool falling = (tid & size) == 0;
+        auto place = [&](uint64_t other, int step) {
+            const bool larger = falling == ((tid & step) == 0);
+            v = (v > other) == larger ? v : other;
+        };
+        for (int step = size >> 1; step >= 64; step >>= 1) {
+            __syncthreads();
+            lds[tid] = v;
+            __syncthreads();
+            place(lds[tid ^ step], step);
         }
+        if (size > 32) place(across<32>(v), 32);
+        if (size > 16) place(across<16>(v), 16);
+        if (size > 8) place(across<8>(v), 8);
+        if (size > 4) place(across<4>(v), 4);
+        if (size > 2) place(across<2>(v), 2);
+        place(across<1>(v), 1);
+    }
     return v;
 }
 
@@ -455,26 +566,11 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
     __shared__ uint32_t lds[kTokenWaves];
     __shared__ int one;
     const int row = blockIdx.x, tid = threadIdx.x;
-    const SampleRow r = sample_row<kTokenWaves>(a, row, lds);
+    SampleRow r = sample_settings(a, row);
+    sample_top(r, r.space->top_key);
     SampleSpace* space = r.space;
     if (r.kind == kFixed) {
-        // the first of the largest
-        const unsigned* largest = space->largest(a.tiles);
-        if (tid == 0) one = a.groups;
-        __syncthreads();
-        for (int i = tid; i < a.groups; i += kTokenThreads)
-            if (largest[i] == r.top_key) {
-                atomicMin(&one, i);
-                break;
-            }
-        __syncthreads();
-        const int g = one, i = g * kSampleGroup + tid;
-        __syncthreads();
-        if (tid == 0) one = a.vocab;
-        __syncthreads();
-        if (tid < kSampleGroup && i < a.vocab && key_of(r.x[i]) == r.top_key) atomicMin(&one, i);
-        __syncthreads();
-        if (tid == 0) a.tokens[row] = r.top_key == kLowestKey ? -1 : one;
+        if (tid == 0) a.tokens[row] = r.top_key == kLowestKey ? -1 : space->first;
         return;
     }
     const bool by_groups = r.kind == kByGroups, by_bins = r.kind == kByBins;
@@ -516,19 +612,19 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
             if (mine) lds64[tid] = place;
             const int n = static_cast<int>(group_sum<kTokenWaves>(static_cast<uint32_t>(mine), lds));
             cut = lds64[max(n, 1) - 1];
-            if (mine && static_cast<double>(w) >= r.min_weight)
+            if (mine && w >= r.min_weight)
                 atomicAdd(&sums[static_cast<uint32_t>(~place) / kSampleTile], static_cast<unsigned long long>(w));
         } else {
             // many candidates (logits next to each other): bit by bit, from the list or from the row
             const bool from_list = listed <= kSampleList;
             const int n = from_list ? listed : a.vocab;
-            const uint32_t low_key = by_groups ? space->low_key : 0;
+            const int group_bin = by_groups ? space->group_bin : 0;
             auto each = [&](auto f) {
                 for (int i = tid; i < n; i += kTokenThreads) {
                     const uint32_t index = from_list ? space->list[i] : i, key = key_of(r.x[index]);
                     const float l = log_of(logit_of(key), r.top, r.inverse);
                     const int b = bin_of(l);
-                    if (from_list || (l > kNoWeight && (by_groups ? key >= low_key : (b >= low && b <= high) || b == bin_k)))
+                    if (from_list || (l > kNoWeight && (by_groups ? group_bin_of(l) <= group_bin : (b >= low && b <= high) || b == bin_k)))
                         f(place_of(key, index), b, l);
                 }
             };
@@ -558,7 +654,7 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
             }
             each([&](uint64_t place, int b, float l) {
                 const uint64_t w = weight_of(l);
-                if (place >= cut && b >= low && b <= high && static_cast<double>(w) >= r.min_weight)
+                if (place >= cut && b >= low && b <= high && w >= r.min_weight)
                     atomicAdd(&sums[static_cast<uint32_t>(~place) / kSampleTile], static_cast<unsigned long long>(w));
             });
         }
@@ -587,7 +683,7 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
     if (tid < kSampleTile && i < a.vocab) {
         const uint32_t key = key_of(r.x[i]);
         if (place_of(key, i) >= cut) w = weigh(key);
-        if (static_cast<double>(w) < r.min_weight) w = 0;
+        if (w < r.min_weight) w = 0;
     }
     const uint64_t upto = one64[0] + group_upto<kTokenWaves>(w, waves64, &all);
     if (point < upto && point >= upto - w) a.tokens[row] = i;
@@ -595,8 +691,8 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
 
 // bytes of a row's space
 inline size_t sample_row_space(int vocab) {
-    const size_t tiles = (vocab + kSampleTile - 1) / kSampleTile, groups = (vocab + kSampleGroup - 1) / kSampleGroup;
-    return (sizeof(SampleSpace) + 8 * tiles + 4 * groups + 255) / 256 * 256;
+    const size_t tiles = (vocab + kSampleTile - 1) / kSampleTile;
+    return (sizeof(SampleSpace) + 8 * tiles + 4 * kMostGroups + 255) / 256 * 256;
 }
 
 }  // namespace tetra_dev

@@ -296,16 +296,17 @@ int tetra_sample(const float* logits, long long stride, int rows, int vocab, con
     a.row_space = tetra_dev::sample_row_space(vocab);
     a.vocab = vocab;
     a.tiles = (vocab + tetra_dev::kSampleTile - 1) / tetra_dev::kSampleTile;
-    a.groups = (vocab + tetra_dev::kSampleGroup - 1) / tetra_dev::kSampleGroup;
     // a tile a wave, up to four workgroups a CU over all rows
     int cus = 0;
     if (int st = device_cus(&cus)) return st;
-    a.parts = std::max(1, std::min((a.tiles + 3) / 4, 4 * cus / rows));
+    a.parts = std::max(1, std::min({(a.tiles + 3) / 4, 4 * cus / rows, tetra_dev::kMostParts}));
+    a.wave_groups = a.parts * 4 * 16 <= tetra_dev::kMostGroups ? 16 : 4;
+    a.groups = a.parts * 4 * a.wave_groups;
     if (static_cast<long long>(rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
     const dim3 g(static_cast<unsigned>(rows * a.parts)), b(256);
     hipLaunchKernelGGL(tetra_dev::sample_max_kernel, g, b, 0, stream, a);
     hipLaunchKernelGGL(tetra_dev::sample_cut_kernel, g, b, 0, stream, a);
-    hipLaunchKernelGGL(tetra_dev::sample_sum_kernel, g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::sample_bins_kernel, g, b, 0, stream, a);
     hipLaunchKernelGGL(tetra_dev::sample_token_kernel, dim3(static_cast<unsigned>(rows)), dim3(tetra_dev::kTokenThreads),
                        8 * static_cast<size_t>(a.tiles), stream, a);
     return launch_status();
