@@ -44,7 +44,7 @@ struct SampleArgs {
     int* tokens;
     uint8_t* space;        // SampleSpace of every row, row_space bytes each
     size_t row_space;
-    int vocab, tiles, parts;
+    int rows, vocab, tiles, parts;
     int groups, wave_groups;      // of a row, and of each of its 4 parts waves: 16 (of four lanes) or 4 (of sixteen)
 };
 
@@ -272,35 +272,54 @@ struct Candidates {
     }
 };
 
-// A wave's tiles, each lane's eight logits of one in x (-inf past the row's end):
-// f(tile, x).  The next tile is on its way meanwhile.
-template <class F>
-__device__ __forceinline__ void each_tile(const SampleArgs& a, const float* row, int first, F f) {
-    const int lane = threadIdx.x & 63, step = a.parts * 4;
-    auto load = [&](float (&x)[8], int t) {
-        const int i0 = t * kSampleTile + lane;
-        if ((t + 1) * kSampleTile <= a.vocab) {
+// Neighbouring workgroups take different rows, one row further in every round:
+// workgroups go to the XCDs and CUs in turn, and so the parts of the rows with
+// most to do come to all of them (64 rows with a period of 8 settings: 49 us with
+// a row's parts side by side, which put them on a quarter of the CUs, 41 so).
+__device__ __forceinline__ void row_and_part(int rows, int& row, int& part) {
+    part = blockIdx.x / rows;
+    row = (blockIdx.x - part * rows + part) % rows;
+}
+
+// A wave's tiles of a row, `first` and every `step` further: a lane's eight logits
+// of one (-inf past the row's end).  The first is on its way from the start, the
+// next one during f(tile, x).
+struct Tiles {
+    const float* row;
+    int vocab, tiles, first, step;
+    float x[8];
+
+    __device__ __forceinline__ Tiles(const SampleArgs& a, int r, int wave, int waves)
+        : row(a.logits + r * a.stride), vocab(a.vocab), tiles(a.tiles), first(wave), step(waves) {
+        if (first < tiles) load(x, first);
+    }
+    __device__ __forceinline__ void load(float (&to)[8], int t) const {
+        const int i0 = t * kSampleTile + (threadIdx.x & 63);
+        if ((t + 1) * kSampleTile <= vocab) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = row[i0 + 64 * j];
+            for (int j = 0; j < 8; ++j) to[j] = row[i0 + 64 * j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = i0 + 64 * j < a.vocab ? row[i0 + 64 * j] : -INFINITY;
+            for (int j = 0; j < 8; ++j) to[j] = i0 + 64 * j < vocab ? row[i0 + 64 * j] : -INFINITY;
         }
-    };
-    float x[8], next[8];
-    if (first < a.tiles) load(x, first);
-    for (int t = first; t < a.tiles; t += step) {
-        if (t + step < a.tiles) load(next, t + step);
-        f(t, x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = next[j];
     }
-}
+    template <class F>
+    __device__ __forceinline__ void each(F f) {
+        float next[8];
+        for (int t = first; t < tiles; t += step) {
+            if (t + step < tiles) load(next, t + step);
+            f(t, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = next[j];
+        }
+    }
+};
 
 // First: the largest logits, a maximum for every four or sixteen lanes of a wave;
 // and the row's space is cleared.
 __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    int row, part;
+    row_and_part(a.rows, row, part);
     const int lane = threadIdx.x & 63, wave = part * 4 + (threadIdx.x >> 6);
     SampleSpace* space = reinterpret_cast<SampleSpace*>(a.space + row * a.row_space);
     for (int i = part * 256 + threadIdx.x; i < kSampleBins; i += a.parts * 256) {
@@ -312,7 +331,7 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
         space->first = a.vocab;
     }
     float top = -INFINITY;
-    each_tile(a, a.logits + row * a.stride, wave, [&](int, const float (&x)[8]) {
+    Tiles(a, row, wave, 4 * a.parts).each([&](int, const float (&x)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);      // of NaN and a number, the number
     });
@@ -332,8 +351,8 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
 // Then the sums of rows without a cut, and what the others' cut is found from.
 // A top-k of at most 512 goes by the groups: their k-th largest maximum is at
 // most the k-th largest logit, so the logits from its bin on (some 1.4 k of
-// them, if the large ones lie anywhere) hold the k.  Other filtered rows count and
-// weigh their tokens in 2,048 bins of the weight's logarithm.  Greedy rows look
+// them, if the large ones lie anywhere) hold the k.  Other filtered rows weigh (and
+// with a top-k count) their tokens in 2,048 bins of the weight's logarithm.  Greedy rows look
 // for the first of the largest logits.
 __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
     __shared__ unsigned long long mass[kSampleBins];
@@ -341,8 +360,10 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
     __shared__ Candidates found;
     __shared__ uint32_t lds[4];
     __shared__ int last;
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    int row, part;
+    row_and_part(a.rows, row, part);
     const int tid = threadIdx.x, lane = tid & 63, wave = part * 4 + (tid >> 6);
+    Tiles tiles(a, row, wave, 4 * a.parts);
     SampleRow r = sample_settings(a, row);
     constexpr int kHeld = kMostGroups / 256;
     uint32_t held[kHeld], best = 0;
@@ -358,7 +379,7 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
     sample_top(r, Max()(Max()(lds[0], lds[1]), Max()(lds[2], lds[3])));
     if (part == 0 && tid == 0) r.space->top_key = r.top_key;
     if (r.kind == kUnfiltered) {
-        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+        tiles.each([&](int t, const float (&x)[8]) {
             uint64_t sum = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -385,7 +406,7 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
         __syncthreads();
         const int bin = last;
         if (part == 0 && tid == 0) r.space->group_bin = bin;
-        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+        tiles.each([&](int t, const float (&x)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float l = log_of(x[j], r.top, r.inverse);
@@ -400,24 +421,23 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
             count[i] = 0;
         }
         __syncthreads();
-        each_tile(a, r.x, wave, [&](int, const float (&x)[8]) {
+        tiles.each([&](int, const float (&x)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float l = log_of(x[j], r.top, r.inverse);
                 if (l > kNoWeight) {
                     atomicAdd(&mass[bin_of(l)], static_cast<unsigned long long>(weight_of(l)));
-                    atomicAdd(&count[bin_of(l)], 1u);
+                    if (r.k) atomicAdd(&count[bin_of(l)], 1u);
                 }
             }
         });
         __syncthreads();
-        for (int i = tid; i < kSampleBins; i += 256)
-            if (count[i]) {
-                atomicAdd(&r.space->mass[i], mass[i]);
-                atomicAdd(&r.space->count[i], count[i]);
-            }
+        for (int i = tid; i < kSampleBins; i += 256) {
+            if (mass[i]) atomicAdd(&r.space->mass[i], mass[i]);
+            if (count[i]) atomicAdd(&r.space->count[i], count[i]);
+        }
     } else if (r.top_key != kLowestKey) {
-        each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+        tiles.each([&](int t, const float (&x)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int i = t * kSampleTile + 64 * j + lane;
@@ -430,17 +450,19 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
 // Then rows in bins: the bins that their cuts can lie in (top-p's share is one
 // of top-k's weight, which bin_k leaves open a little), the tokens there, and
 // of every tile the sum of the weights above them.
-__global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a) {
+__global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a, int parts) {
     __shared__ uint32_t lds[4];
     __shared__ uint64_t lds64[4];
     __shared__ unsigned long long found_mass[3];
     __shared__ unsigned found_count;
     __shared__ int found_bin[3];
     __shared__ Candidates found;
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    int row, part;
+    row_and_part(a.rows, row, part);
     const int tid = threadIdx.x, lane = tid & 63, wave = part * 4 + (tid >> 6);
     SampleRow r = sample_settings(a, row);
     if (r.kind != kByBins) return;
+    Tiles tiles(a, row, wave, 4 * parts);
     sample_top(r, r.space->top_key);
     if (r.kind != kByBins) return;
     constexpr int kPer = kSampleBins / 256;
@@ -507,7 +529,7 @@ __global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a) {
         r.space->mass_low = mass_low;
         r.space->mass_all = all_mass;
     }
-    each_tile(a, r.x, wave, [&](int t, const float (&x)[8]) {
+    tiles.each([&](int t, const float (&x)[8]) {
         uint64_t sum = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

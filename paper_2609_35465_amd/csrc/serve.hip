@@ -294,19 +294,25 @@ int tetra_sample(const float* logits, long long stride, int rows, int vocab, con
     a.tokens = tokens;
     a.space = static_cast<uint8_t*>(workspace);
     a.row_space = tetra_dev::sample_row_space(vocab);
+    a.rows = rows;
     a.vocab = vocab;
     a.tiles = (vocab + tetra_dev::kSampleTile - 1) / tetra_dev::kSampleTile;
-    // a tile a wave, up to four workgroups a CU over all rows
+    // A tile a wave where the chip has the room: two workgroups a CU over all rows, or up to 16 a row and four a CU.
+    // More of them take longer over the bins, which each adds to the row's (top-p 0.9 of 151,936: 16 rows 33 us in 32
+    // parts each, 40 in 64; 32 rows 44 in 16, 49 in 32; without a filter one row 12 us in 75, 16 in 16).
     int cus = 0;
     if (int st = device_cus(&cus)) return st;
-    a.parts = std::max(1, std::min({(a.tiles + 3) / 4, 4 * cus / rows, tetra_dev::kMostParts}));
+    a.parts = std::max(1, std::min({(a.tiles + 3) / 4, std::max(2 * cus / rows, std::min(16, 4 * cus / rows)),
+                                    tetra_dev::kMostParts}));
     a.wave_groups = a.parts * 4 * 16 <= tetra_dev::kMostGroups ? 16 : 4;
     a.groups = a.parts * 4 * a.wave_groups;
     if (static_cast<long long>(rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
     const dim3 g(static_cast<unsigned>(rows * a.parts)), b(256);
     hipLaunchKernelGGL(tetra_dev::sample_max_kernel, g, b, 0, stream, a);
     hipLaunchKernelGGL(tetra_dev::sample_cut_kernel, g, b, 0, stream, a);
-    hipLaunchKernelGGL(tetra_dev::sample_bins_kernel, g, b, 0, stream, a);
+    // few rows go by bins, and each of their parts has the more to do
+    const int bins_parts = std::min((a.tiles + 3) / 4, 2 * a.parts);
+    hipLaunchKernelGGL(tetra_dev::sample_bins_kernel, dim3(static_cast<unsigned>(rows * bins_parts)), b, 0, stream, a, bins_parts);
     hipLaunchKernelGGL(tetra_dev::sample_token_kernel, dim3(static_cast<unsigned>(rows)), dim3(tetra_dev::kTokenThreads),
                        8 * static_cast<size_t>(a.tiles), stream, a);
     return launch_status();
