@@ -322,7 +322,7 @@ def _expect(ok, what):
 
 
 class KVCache(ctypes.Structure):
-    """tetra_kv_cache; keeps the tensors it was made of in `tensors`."""
+    """tetra_kv_cache, from make_kv_cache(), which keeps the tensors it is made of with it."""
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int),
@@ -351,7 +351,7 @@ def make_kv_cache(k, v, scales, pages, lens) -> KVCache:
             and pages.dim() == 2 and tuple(lens.shape) == (pages.shape[0],)
             and all(t.is_contiguous() for t in (k, v, scales, pages, lens)), "make_kv_cache")
     cache = KVCache(_ptr(k), _ptr(v), _ptr(scales), _ptr(pages), _ptr(lens), n, page, heads, dim, *pages.shape)
-    cache.tensors = (k, v, scales, pages, lens)
+    cache.tensors, cache.sizes = (k, v, scales, pages, lens), (heads, dim, pages.shape[0])
     return cache
 
 
@@ -363,14 +363,27 @@ def rope_table(positions: int, head_dim: int, base: float = 1e6):
     return torch.from_numpy(np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32)).cuda()
 
 
-def _rows_of(t, heads, dim, what):
+_kinds = None                      # torch's float32, float16 and int32, once torch is in
+
+
+def _kinds_of_torch():
+    global _kinds
+    import torch
+    _kinds = torch.float32, torch.float16, torch.int32
+    return _kinds
+
+
+def _row_stride(t, rows, heads, dim, what):
     """Elements from a row to the next of t [rows, heads, dim] or [rows, heads * dim] (heads side by side)."""
+    if t.is_contiguous() and t.numel() == rows * heads * dim:
+        return heads * dim
     shape, stride = t.shape, t.stride()
+    _expect(shape[0] == rows and stride[-1] == 1, what)
     if len(shape) == 3:
-        _expect(shape[1:] == (heads, dim) and stride[2] == 1 and (heads == 1 or stride[1] == dim), what)
+        _expect(shape[1:] == (heads, dim) and (heads == 1 or stride[1] == dim), what)
     else:
-        _expect(len(shape) == 2 and shape[1] == heads * dim and stride[1] == 1, what)
-    return stride[0] if shape[0] > 1 else heads * dim
+        _expect(len(shape) == 2 and shape[1] == heads * dim, what)
+    return stride[0] if rows > 1 else heads * dim
 
 
 def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm=None, k_norm=None,
@@ -379,34 +392,37 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
     are sequence s's last tokens) to the cache, keys normed (k_norm fp32 [head_dim], optional) and rotated
     (rope from rope_table(), or None); q [rows, q_heads, head_dim] goes the same way into q_out (fp16,
     contiguous).  q and q_out may be None.  max_new: at least the largest count of rows of a sequence."""
-    import torch
-    heads, dim, kind = cache.kv_heads, cache.head_dim, k.dtype
-    _expect(kind in (torch.float32, torch.float16) and v.dtype == kind and starts.dtype == torch.int32
-            and starts.shape[0] == cache.seqs + 1 and v.shape[0] == k.shape[0], "tetra_kv_append")
-    a = KVInput(k=_ptr(k), v=_ptr(v), k_stride=_rows_of(k, heads, dim, "tetra_kv_append"),
-                v_stride=_rows_of(v, heads, dim, "tetra_kv_append"), half=int(kind == torch.float16), eps=eps,
-                q_norm=_ptr(q_norm), k_norm=_ptr(k_norm), rope=_ptr(rope), q_out=_ptr(q_out))
+    what = "tetra_kv_append"
+    f32, f16, i32 = _kinds or _kinds_of_torch()
+    heads, dim, seqs = cache.sizes
+    rows, kind, q_heads, q_stride, rope_rows = k.shape[0], k.dtype, 0, 0, 0
+    ok = (kind is f16 or kind is f32) and v.dtype is kind and starts.dtype is i32 and starts.numel() == seqs + 1
     for w in (q_norm, k_norm):
-        _expect(w is None or (w.dtype == torch.float32 and w.shape == (dim,) and w.is_contiguous()), "tetra_kv_append")
+        ok = ok and (w is None or (w.dtype is f32 and w.numel() == dim and w.is_contiguous()))
     if rope is not None:
-        _expect(rope.dtype == torch.float32 and rope.shape[1:] == (dim,) and rope.is_contiguous(), "tetra_kv_append")
-        a.rope_rows = rope.shape[0]
+        rope_rows = rope.numel() // dim
+        ok = ok and rope.dtype is f32 and rope.shape[-1] == dim and rope.is_contiguous()
     if q is not None:
-        _expect(q.dtype == kind and q_out is not None and q_out.dtype == torch.float16 and q_out.is_contiguous()
-                and q.shape[0] == k.shape[0] and q_out.numel() == q.numel(), "tetra_kv_append")
-        a.q, a.q_heads = _ptr(q), q.numel() // (q.shape[0] * dim) if q.shape[0] else 0
-        a.q_stride = _rows_of(q, a.q_heads, dim, "tetra_kv_append")
-    _check(_call("tetra_kv_append", ctypes.addressof(cache), ctypes.addressof(a), _ptr(starts), k.shape[0], max_new,
-                 _stream(stream)), "tetra_kv_append")
+        size = q_out.numel() if q_out is not None else 0
+        q_heads = size // (rows * dim) if rows else 0
+        ok = ok and q.dtype is kind and size == q_heads * rows * dim and q_out.dtype is f16 and q_out.is_contiguous()
+    _expect(ok, what)
+    if q is not None:
+        q_stride = _row_stride(q, rows, q_heads, dim, what)
+    a = KVInput(_ptr(q), k.data_ptr(), v.data_ptr(), q_stride, _row_stride(k, rows, heads, dim, what),
+                _row_stride(v, rows, heads, dim, what), kind is f16, _ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), rope_rows,
+                q_heads, _ptr(q_out))
+    _check(_call("tetra_kv_append", ctypes.addressof(cache), ctypes.addressof(a), starts.data_ptr(), rows, max_new,
+                 _stream(stream)), what)
 
 
 def kv_read(cache: KVCache, count: int, k_out, v_out, stream=None):
     """k_out, v_out fp16 [seqs, count, kv_heads, head_dim]: the last count tokens of every sequence."""
-    import torch
-    shape = (cache.seqs, count, cache.kv_heads, cache.head_dim)
+    f16 = (_kinds or _kinds_of_torch())[1]
+    heads, dim, seqs = cache.sizes
     for t in (k_out, v_out):
-        _expect(tuple(t.shape) == shape and t.dtype == torch.float16 and t.is_contiguous(), "tetra_kv_read")
-    _check(_call("tetra_kv_read", ctypes.addressof(cache), count, _ptr(k_out), _ptr(v_out), _stream(stream)),
+        _expect(t.dtype is f16 and t.numel() == seqs * count * heads * dim and t.is_contiguous(), "tetra_kv_read")
+    _check(_call("tetra_kv_read", ctypes.addressof(cache), count, k_out.data_ptr(), v_out.data_ptr(), _stream(stream)),
            "tetra_kv_read")
 
 
@@ -424,15 +440,15 @@ def kv_attend(cache: KVCache, q, starts, max_new: int, out, workspace, scale: fl
     """out (fp16, as q) = attention of q fp16 [rows, q_heads, head_dim] over the cache, which holds the rows'
     own tokens already (rows as in kv_append); scale: 1 / sqrt(head_dim) if None; window: how many tokens a
     row sees at most, its own among them (0: all); workspace from kv_attend_workspace(), one per stream."""
-    import torch
-    dim = cache.head_dim
-    _expect(q.dtype == out.dtype == torch.float16 and q.shape == out.shape and q.shape[0] > 0
-            and starts.dtype == torch.int32 and starts.shape[0] == cache.seqs + 1, "tetra_kv_attend")
-    heads = q.numel() // (q.shape[0] * dim)
-    _check(_call("tetra_kv_attend", ctypes.addressof(cache), _ptr(q), _rows_of(q, heads, dim, "tetra_kv_attend"),
-                 _ptr(starts), q.shape[0], max_new, heads, dim ** -0.5 if scale is None else scale, window, _ptr(out),
-                 _rows_of(out, heads, dim, "tetra_kv_attend"), _ptr(workspace), workspace.numel(), _stream(stream)),
-           "tetra_kv_attend")
+    what = "tetra_kv_attend"
+    _, f16, i32 = _kinds or _kinds_of_torch()
+    dim, seqs = cache.sizes[1:]
+    rows = q.shape[0]
+    heads = q.numel() // (rows * dim) if rows else 0
+    _expect(q.dtype is f16 and out.dtype is f16 and heads and starts.dtype is i32 and starts.numel() == seqs + 1, what)
+    _check(_call("tetra_kv_attend", ctypes.addressof(cache), q.data_ptr(), _row_stride(q, rows, heads, dim, what),
+                 starts.data_ptr(), rows, max_new, heads, dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                 _row_stride(out, rows, heads, dim, what), workspace.data_ptr(), workspace.numel(), _stream(stream)), what)
 
 
 def sample_workspace(rows: int, vocab: int):
@@ -447,13 +463,12 @@ def sample_workspace(rows: int, vocab: int):
 def sample(logits, temperature, top_k, top_p, min_p, u, tokens, workspace, stream=None):
     """tokens int32 [rows] drawn from logits fp32 [rows, vocab] with the rows' temperature, top_p, min_p and
     random numbers u (fp32 [rows]) and top_k (int32 [rows]); workspace from sample_workspace()."""
-    import torch
+    f32, _, i32 = _kinds or _kinds_of_torch()
     rows, vocab = logits.shape
-    f32 = (temperature, top_p, min_p, u)
-    _expect(logits.dtype == torch.float32 and logits.stride(1) == 1
-            and all(t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous() for t in f32)
-            and all(t.dtype == torch.int32 and t.shape == (rows,) and t.is_contiguous() for t in (top_k, tokens)),
-            "tetra_sample")
-    _check(_call("tetra_sample", _ptr(logits), logits.stride(0) if rows > 1 else vocab, rows, vocab, _ptr(temperature),
-                 _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(tokens), _ptr(workspace), workspace.numel(),
-                 _stream(stream)), "tetra_sample")
+    ok = logits.dtype is f32 and logits.stride(1) == 1
+    for t, kind in ((temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32), (u, f32), (tokens, i32)):
+        ok = ok and t.dtype is kind and t.numel() == rows and t.is_contiguous()
+    _expect(ok, "tetra_sample")
+    _check(_call("tetra_sample", logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                 temperature.data_ptr(), top_k.data_ptr(), top_p.data_ptr(), min_p.data_ptr(), u.data_ptr(),
+                 tokens.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)), "tetra_sample")

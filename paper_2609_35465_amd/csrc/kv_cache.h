@@ -77,18 +77,40 @@ __device__ __forceinline__ Span span_of(const int* starts, const int* lens, int 
     return s;
 }
 
-// the number of i < n with f(i) <= x, for f that does not fall; x and the
-// result are uniform in the wave
+// The sequence that holds place x, and its span: the first one with base(start of
+// the next, its number) above x.  Each lane loads a sequence, all at once; x and
+// the result are uniform in the wave.
+struct Place {
+    int seq, start;    // seq -1: none; starts[seq]
+    Span s;
+};
+
 template <class F>
-__device__ __forceinline__ int count_upto(int n, int x, F f) {
+__device__ __forceinline__ Place locate(const int* starts, const int* lens, int rows, int max_new, int seqs, int x, F base) {
     const int lane = threadIdx.x & 63;
-    int c = 0;
-    for (int i = 0; i < n; i += 64) {
-        const unsigned long long b = __ballot(i + lane < n && f(i + lane) <= x);
-        c += __popcll(b);
-        if (~b) break;
+    Place p;
+    p.seq = -1;
+    for (int i0 = 0; i0 < seqs; i0 += 64) {
+        const int i = i0 + lane;
+        int a = 0, b = 0, len = 0;
+        if (i < seqs) {
+            a = starts[i];
+            b = starts[i + 1];
+            len = lens[i];
+        }
+        a = min(max(a, 0), rows);
+        b = min(max(b, 0), rows);
+        const unsigned long long has = __ballot(i < seqs && base(b, i + 1) > x);
+        if (!has) continue;
+        const int l = __builtin_ctzll(has);
+        p.seq = i0 + l;
+        p.start = p.s.row0 = __builtin_amdgcn_readlane(a, l);
+        p.s.n = min(max(__builtin_amdgcn_readlane(b, l) - p.start, 0), max_new);
+        p.s.len = max(__builtin_amdgcn_readlane(len, l), 0);
+        p.s.first = p.s.len - p.s.n;
+        break;
     }
-    return c;
+    return p;
 }
 
 // Page items of the sequences before `seq`.  New tokens n >= 1 touch at most
@@ -198,8 +220,10 @@ __device__ __forceinline__ float grown_scale(float amax, float before, float* ld
     return fmaxf(before, s < kSmallestScale ? 0.f : s);
 }
 
+// `entry`: where the table names the page; it is on its way with the values
 template <int D, bool HALF>
-__device__ void append_keys(const AppendArgs& a, const Span& s, int number, int page, int head, float* lds) {
+__device__ void append_keys(const AppendArgs& a, const Span& s, int number, const int* entry, int head, float* lds) {
+    const int page = *entry;
     constexpr int kLanes = D / 8, kPerPass = 64 / kLanes, kPasses = kGroupTokens / kPerPass;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int sub = lane % kLanes, slot = lane / kLanes;
@@ -216,6 +240,7 @@ __device__ void append_keys(const AppendArgs& a, const Span& s, int number, int 
         else
             for (float& e : x[p]) e = 0.f;
     }
+    if (page < 0 || page >= a.c.num_pages) return;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
         norm_and_rotate<D>(x[p], a.k_norm, a.eps, a.rope, a.rope_rows, token0 + p * kPerPass, sub);
@@ -256,7 +281,8 @@ __device__ void append_keys(const AppendArgs& a, const Span& s, int number, int 
 }
 
 template <int D, bool HALF>
-__device__ void append_values(const AppendArgs& a, const Span& s, int number, int page, int head, float* lds) {
+__device__ void append_values(const AppendArgs& a, const Span& s, int number, const int* entry, int head, float* lds) {
+    const int page = *entry;
     constexpr int kPairs = D / 2, kTokens = kGroupTokens * kPairs / 64;   // a lane: two dimensions of kTokens tokens
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int pair = lane % kPairs, part = lane / kPairs;
@@ -272,6 +298,7 @@ __device__ void append_values(const AppendArgs& a, const Span& s, int number, in
         if (t >= from && t < s.len)
             x[j] = load2<HALF>(a.v, (s.row0 + t - s.first) * a.v_stride + head * D + 2 * pair);
     }
+    if (page < 0 || page >= a.c.num_pages) return;
 #pragma unroll
     for (int j = 0; j < kTokens; ++j) amax = larger(larger(amax, x[j][0]), x[j][1]);
     float* held = a.c.scales + (static_cast<size_t>(page) * a.c.kv_heads + head) * 2 + 1;
@@ -309,15 +336,14 @@ __device__ void append_queries(const AppendArgs& a, int unit) {
     const int chunks = (a.q_heads + a.q_chunk - 1) / a.q_chunk;
     const int row = unit / chunks;
     if (row >= a.rows) return;
-    const int head0 = (unit - row * chunks) * a.q_chunk;
-    const int seq = count_upto(a.c.seqs, row, [&](int i) { return a.starts[i + 1]; });
-    if (seq >= a.c.seqs) return;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    if (row < s.row0 || row >= s.row0 + s.n) return;
-    const int position = s.first + row - s.row0;
-    for (int h = head0 + lane / kLanes; h < min(head0 + a.q_chunk, a.q_heads); h += kTeams) {
-        float x[8];
-        load_head<D, HALF>(x, a.q, row * a.q_stride + h * D, sub);
+    const int head0 = (unit - row * chunks) * a.q_chunk, end = min(head0 + a.q_chunk, a.q_heads);
+    const int first = head0 + lane / kLanes;
+    float x0[8] = {};
+    if (first < end) load_head<D, HALF>(x0, a.q, row * a.q_stride + first * D, sub);
+    const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, row, [](int start, int) { return start; });
+    if (at.seq < 0 || row < at.s.row0 || row >= at.s.row0 + at.s.n) return;
+    const int position = at.s.first + row - at.s.row0;
+    auto finish = [&](float (&x)[8], int h) {
         norm_and_rotate<D>(x, a.q_norm, a.eps, a.rope, a.rope_rows, position, sub);
         f16x4 lo, hi;
 #pragma unroll
@@ -328,6 +354,12 @@ __device__ void append_queries(const AppendArgs& a, int unit) {
         uint16_t* out = a.q_out + (static_cast<size_t>(row) * a.q_heads + h) * D + 4 * sub;
         *reinterpret_cast<f16x4*>(out) = lo;
         *reinterpret_cast<f16x4*>(out + D / 2) = hi;
+    };
+    if (first < end) finish(x0, first);
+    for (int h = first + kTeams; h < end; h += kTeams) {
+        float x[8];
+        load_head<D, HALF>(x, a.q, row * a.q_stride + h * D, sub);
+        finish(x, h);
     }
 }
 
@@ -343,53 +375,67 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a) {
         return;
     }
     const int item = b / (a.c.kv_heads * 2), rest = b - item * a.c.kv_heads * 2;
-    const int seq = count_upto(a.c.seqs, item, [&](int i) {
-        return item_base(min(max(a.starts[i + 1], 0), a.rows), i + 1, a.c.page_shift, a.max_new);
-    });
-    if (seq >= a.c.seqs) return;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int base = item_base(min(max(a.starts[seq], 0), a.rows), seq, a.c.page_shift, a.max_new);
-    if (item < base) return;
+    const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, item,
+                              [&](int start, int i) { return item_base(start, i, a.c.page_shift, a.max_new); });
+    if (at.seq < 0) return;
+    const Span s = at.s;
+    const int base = item_base(at.start, at.seq, a.c.page_shift, a.max_new);
     const int number = (max(s.first, 0) >> a.c.page_shift) + item - base;
-    if (s.n == 0 || number >= a.c.max_pages || (static_cast<long long>(number) << a.c.page_shift) >= s.len) return;
-    const int page = a.c.pages[static_cast<size_t>(seq) * a.c.max_pages + number];
-    if (page < 0 || page >= a.c.num_pages) return;
-    if (rest & 1) append_values<D, HALF>(a, s, number, page, rest >> 1, lds);
-    else append_keys<D, HALF>(a, s, number, page, rest >> 1, lds);
+    if (item < base || s.n == 0 || number >= a.c.max_pages || (static_cast<long long>(number) << a.c.page_shift) >= s.len)
+        return;
+    const int* entry = a.c.pages + static_cast<size_t>(at.seq) * a.c.max_pages + number;
+    if (rest & 1) append_values<D, HALF>(a, s, number, entry, rest >> 1, lds);
+    else append_keys<D, HALF>(a, s, number, entry, rest >> 1, lds);
 }
 
 // The last `count` tokens of every sequence as fp16, [seqs][count][kv_heads][D]
-// each for keys and values; zeros before a sequence's start.  A thread takes
-// eight dimensions of a token.
+// each for keys and values; zeros before a sequence's start.  A workgroup of 2 D
+// threads takes 16 tokens of a head, the first D threads its keys, the others its
+// values, which LDS turns.
 template <int D>
-__global__ __launch_bounds__(256) void kv_read_kernel(KvCache c, int count, uint16_t* k_out, uint16_t* v_out) {
-    const size_t i = blockIdx.x * static_cast<size_t>(256) + threadIdx.x;
-    const int part = static_cast<int>(i % (D / 8));
-    const size_t r = i / (D / 8);
-    const int head = static_cast<int>(r % c.kv_heads);
-    const size_t st = r / c.kv_heads;
-    const int seq = static_cast<int>(st / count);
-    if (seq >= c.seqs) return;
-    const int token = c.lens[seq] - count + static_cast<int>(st % count);
-    const int number = token >> c.page_shift;
-    f16x8 k = {}, v = {};
-    if (token >= 0 && number < c.max_pages) {
-        const int page = c.pages[static_cast<size_t>(seq) * c.max_pages + number];
-        if (page >= 0 && page < c.num_pages) {
-            const size_t ph = static_cast<size_t>(page) * c.kv_heads + head;
-            const float ks = c.scales[ph * 2], vs = c.scales[ph * 2 + 1];
-            const int at = token & (c.page_tokens - 1);
-            const int8_t* kp = c.k + (ph * c.page_tokens + at) * D + 8 * part;
-            const int8_t* vp = c.v + (ph * c.page_tokens + (at & ~15)) * D + 8 * part * 16 + (at & 15);
-#pragma unroll
-            for (int d = 0; d < 8; ++d) {
-                k[d] = static_cast<_Float16>(static_cast<float>(kp[d]) * ks);
-                v[d] = static_cast<_Float16>(static_cast<float>(vp[16 * d]) * vs);
-            }
-        }
+__global__ __launch_bounds__(2 * D) void kv_read_kernel(KvCache c, int count, int groups, uint16_t* k_out, uint16_t* v_out) {
+    __shared__ __align__(16) _Float16 turned[kGroupTokens][D + 8];
+    const int tid = threadIdx.x;
+    const int head = blockIdx.x % c.kv_heads, rest = blockIdx.x / c.kv_heads;
+    const int seq = rest / groups, group = rest - seq * groups;
+    const int len = max(c.lens[seq], 0), first = len - count;
+    const int t0 = (first & ~(kGroupTokens - 1)) + group * kGroupTokens;   // a multiple of 16, below zero perhaps
+    const int number = t0 >> c.page_shift;
+    int page = -1;
+    if (t0 >= 0 && t0 < len && number < c.max_pages) page = c.pages[static_cast<size_t>(seq) * c.max_pages + number];
+    const bool there = page >= 0 && page < c.num_pages;
+    const size_t ph = static_cast<size_t>(there ? page : 0) * c.kv_heads + head;
+    const bool values = tid >= D;
+    const int i = values ? tid - D : tid;
+    u32x4 q = {0, 0, 0, 0};
+    float scale = 0.f;
+    if (there) {
+        const int8_t* at = (values ? c.v : c.k) + (ph * c.page_tokens + (t0 & (c.page_tokens - 1))) * D + 16 * i;
+        q = *reinterpret_cast<const u32x4*>(at);
+        scale = c.scales[2 * ph + (values ? 1 : 0)];
     }
-    *reinterpret_cast<f16x8*>(k_out + i * 8) = k;
-    *reinterpret_cast<f16x8*>(v_out + i * 8) = v;
+    // 16 keys' dimensions of a token, or a dimension's 16 tokens
+    _Float16 x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = static_cast<_Float16>(static_cast<float>(static_cast<int8_t>(q[e / 4] >> (8 * (e % 4)))) * scale);
+    if (values)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) turned[e][i] = x[e];
+    __syncthreads();
+    const int token = i / (D / 16), part = i % (D / 16) * 16, t = t0 + token;
+    if (t < first || t >= len) return;
+    uint16_t* out = (values ? v_out : k_out) + ((static_cast<size_t>(seq) * count + (t - first)) * c.kv_heads + head) * D + part;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        f16x8 y;
+        if (values) {
+            y = *reinterpret_cast<const f16x8*>(&turned[token][part + 8 * v]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = x[8 * v + e];
+        }
+        *reinterpret_cast<f16x8*>(out + 8 * v) = y;
+    }
 }
 
 }  // namespace tetra_dev

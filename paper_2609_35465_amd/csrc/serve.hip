@@ -219,15 +219,15 @@ int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint1
     if (int st = cache_of(cache, &c)) return st;
     if (count < 1 || !k_out || !v_out) return TETRA_EINVAL;
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return TETRA_EALIGN;
-    const long long rows = static_cast<long long>(c.seqs) * count;
-    if (rows > (1ll << 40) / (static_cast<long long>(c.kv_heads) * cache->head_dim)) return TETRA_EINVAL;
-    const long long grid = (rows * c.kv_heads * (cache->head_dim / 8) + 255) / 256;
-    if (grid > kMaxGrid) return TETRA_EINVAL;
-    const dim3 g(static_cast<unsigned>(grid)), b(256);
+    // groups of 16 tokens that `count` tokens can touch
+    const int groups = count / tetra_dev::kGroupTokens + 2;
+    const long long grid = static_cast<long long>(groups) * c.seqs;
+    if (grid > kMaxGrid / c.kv_heads) return TETRA_EINVAL;
+    const dim3 g(static_cast<unsigned>(grid * c.kv_heads));
     if (cache->head_dim == 64)
-        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<64>), g, b, 0, stream, c, count, k_out, v_out);
+        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<64>), g, dim3(128), 0, stream, c, count, groups, k_out, v_out);
     else
-        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<128>), g, b, 0, stream, c, count, k_out, v_out);
+        hipLaunchKernelGGL((tetra_dev::kv_read_kernel<128>), g, dim3(256), 0, stream, c, count, groups, k_out, v_out);
     return launch_status();
 }
 
