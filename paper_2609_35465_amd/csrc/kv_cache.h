@@ -24,6 +24,8 @@
 
 #include <cstdint>
 
+#include "lanes.h"
+
 namespace tetra_dev {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -154,13 +156,6 @@ __device__ __forceinline__ void load_head(float (&x)[8], const void* p, long lon
     }
 }
 
-template <int LANES>
-__device__ __forceinline__ float sum_over(float v) {
-#pragma unroll
-    for (int o = LANES / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
 // norm (if weight) and rotation (if a table) of a head of a token at `position`
 template <int D>
 __device__ __forceinline__ void norm_and_rotate(float (&x)[8], const float* weight, float eps, const float* rope,
@@ -169,7 +164,7 @@ __device__ __forceinline__ void norm_and_rotate(float (&x)[8], const float* weig
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += x[i] * x[i];
-        s = 1.f / sqrtf(sum_over<D / 8>(s) * (1.f / D) + eps);
+        s = __builtin_amdgcn_rsqf(team_all<D / 8>(Sum(), s) * (1.f / D) + eps);
         const f32x4 a = *reinterpret_cast<const f32x4*>(weight + 4 * sub);
         const f32x4 b = *reinterpret_cast<const f32x4*>(weight + D / 2 + 4 * sub);
 #pragma unroll
@@ -209,8 +204,7 @@ __device__ __forceinline__ int requantized(int q, float ratio) { return static_c
 // `before` is the old tokens' scale, 0 without any.  Every wave of the
 // workgroup takes part.
 __device__ __forceinline__ float grown_scale(float amax, float before, float* lds, int waves) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+    amax = wave_all(Max(), amax);
     if (waves > 1) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = amax;
         __syncthreads();

@@ -23,6 +23,8 @@
 
 #include <cstdint>
 
+#include "lanes.h"
+
 namespace tetra_dev {
 
 constexpr uint32_t kLowestKey = 0x007FFFFFu;   // of -inf
@@ -116,60 +118,6 @@ __device__ __forceinline__ int group_bin_of(float t) {
 __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) {
     return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(~index);
 }
-
-// v of the lane that the DPP control names, 0 where there is none or the row of
-// lanes is masked
-template <int CTRL, int ROWS, class T>
-__device__ __forceinline__ T dpp(T v) {
-    if constexpr (sizeof(T) == 8) {
-        const uint64_t u = v;
-        const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, ROWS, 0xF, false);
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, ROWS, 0xF, false);
-        return static_cast<T>(static_cast<uint64_t>(hi) << 32 | lo);
-    } else {
-        return static_cast<T>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xF, false));
-    }
-}
-
-template <class T>
-__device__ __forceinline__ T lane_of(T v, int lane) {
-    if constexpr (sizeof(T) == 8) {
-        const uint64_t u = v;
-        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(u), lane);
-        const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane);
-        return static_cast<T>(static_cast<uint64_t>(hi) << 32 | lo);
-    } else {
-        return static_cast<T>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
-    }
-}
-
-// over the lanes up to and with this one: the sum, or for unsigned numbers the maximum
-struct Sum {
-    template <class T>
-    __device__ T operator()(T a, T b) const { return a + b; }
-};
-struct Max {
-    template <class T>
-    __device__ T operator()(T a, T b) const { return a > b ? a : b; }
-};
-
-template <class F, class T>
-__device__ __forceinline__ T row_upto(F f, T v) {      // rows of 16 lanes
-    v = f(v, dpp<0x111, 0xF>(v));
-    v = f(v, dpp<0x112, 0xF>(v));
-    v = f(v, dpp<0x114, 0xF>(v));
-    return f(v, dpp<0x118, 0xF>(v));
-}
-
-template <class F, class T>
-__device__ __forceinline__ T wave_upto(F f, T v) {
-    v = row_upto(f, v);
-    v = f(v, dpp<0x142, 0xA>(v));
-    return f(v, dpp<0x143, 0xC>(v));
-}
-
-template <class F, class T>
-__device__ __forceinline__ T wave_all(F f, T v) { return lane_of(wave_upto(f, v), 63); }
 
 // the sum over WAVES (at most 16) waves, in every thread
 template <int WAVES, class T>
