@@ -50,15 +50,13 @@ __device__ __forceinline__ f16x8 to_half8(uint32_t a, uint32_t b) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// maximum and sum over the four lanes of a row (lane % 16)
-__device__ __forceinline__ float max_over_groups(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float sum_over_groups(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
-}
+struct Larger {
+    __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// over the four lanes of a row (lane % 16)
+template <class F>
+__device__ __forceinline__ float over_groups(F f, float v) { return with_half(f, with_row(f, v)); }
 
 // ---------------------------------------------------------------- few rows
 //
@@ -108,15 +106,14 @@ __device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Span& s)
     return rows > a.few_most ? 0 : (rows + kFewRows - 1) / kFewRows;
 }
 
-__device__ __forceinline__ int few_work(const AttendArgs& a, int seq) {
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+__device__ __forceinline__ int few_work(const AttendArgs& a, const Span& s) {
     return few_row_tiles(a, s) * a.c.kv_heads * few_tiles(reach_of(a, s));
 }
 
 // sum over the workgroup's four waves, in every thread
-__device__ __forceinline__ int few_sum(int v, int* lds) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+template <class T>
+__device__ __forceinline__ T few_sum(T v, T* lds) {
+    v = wave_all(Sum(), v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -215,8 +212,8 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-        const float m = fmaxf(st.m, max_over_groups(top));
-        const float vref = fmaxf(st.vref, max_over_groups(b.vs));
+        const float m = fmaxf(st.m, over_groups(Larger(), top));
+        const float vref = fmaxf(st.vref, over_groups(Larger(), b.vs));
         const float alpha = fast_exp2(st.m - m), beta = alpha * (st.vref / vref);
         st.l *= alpha;
         if (__any(beta != 1.f)) {
@@ -253,17 +250,13 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
     __shared__ float sums[kFewWaves][kFewRows][D + 4];
     __shared__ float stat[kFewWaves][kFewRows][2];
     __shared__ int lds[4], found[2];
+    __shared__ Span found_span;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4, w = blockIdx.x;
     // The total, and the sequence that holds this workgroup's first tile with the
     // tiles before it.  Up to 256 sequences are one scan, more take two passes.
     auto scan = [&](int n, int& all) {
-        int upto = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += u;
-        }
+        int upto = wave_upto(Sum(), n);
         __syncthreads();
         if (lane == 63) lds[wave] = upto;
         __syncthreads();
@@ -274,11 +267,17 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
         }
         return upto;
     };
-    const int n0 = tid < a.c.seqs ? few_work(a, tid) : 0;
+    Span mine = {};
+    int n0 = 0;
+    if (tid < a.c.seqs) {
+        mine = span_of(a.starts, a.c.lens, a.rows, a.max_new, tid);
+        n0 = few_work(a, mine);
+    }
     int all, upto = scan(n0, all), total = all;
     if (a.c.seqs > 256) {
         int more = 0;
-        for (int i = tid + 256; i < a.c.seqs; i += 256) more += few_work(a, i);
+        for (int i = tid + 256; i < a.c.seqs; i += 256)
+            more += few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
         total += few_sum(more, lds);
     }
     const FewPlan plan(__builtin_amdgcn_readfirstlane(total), gridDim.x);
@@ -288,18 +287,28 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
         if (upto > from && upto - n <= from) {
             found[0] = s0 + tid;
             found[1] = upto - n;
+            found_span = mine;
         }
         before += all;
         s0 += 256;
         if (before > from || s0 >= a.c.seqs) break;
-        n = s0 + tid < a.c.seqs ? few_work(a, s0 + tid) : 0;
+        n = 0;
+        if (s0 + tid < a.c.seqs) {
+            mine = span_of(a.starts, a.c.lens, a.rows, a.max_new, s0 + tid);
+            n = few_work(a, mine);
+        }
         upto = scan(n, all) + before;
     }
     __syncthreads();
     int seq = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
+    Span s;
+    s.row0 = __builtin_amdgcn_readfirstlane(found_span.row0);
+    s.n = __builtin_amdgcn_readfirstlane(found_span.n);
+    s.first = __builtin_amdgcn_readfirstlane(found_span.first);
+    s.len = __builtin_amdgcn_readfirstlane(found_span.len);
     bool first = true;
     for (int x = from; x < to && seq < a.c.seqs; ++seq) {
-        const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+        if (!first) s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
         const Reach reach = reach_of(a, s);
         const int tiles = few_tiles(reach), rows = s.n * a.group;
         const int row_tiles = few_row_tiles(a, s), units = row_tiles * a.c.kv_heads;
@@ -329,7 +338,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
             for (f32x4& o : st.o) o = f32x4{0.f, 0.f, 0.f, 0.f};
             few_segment<D>(a, st, q, table, head, reach.begin + tile0 * kFewTile + wave * 64,
                            min(reach.end, reach.begin + tile1 * kFewTile), row_begin, row_end);
-            const float l = sum_over_groups(st.l);
+            const float l = over_groups(Sum(), st.l);
             __syncthreads();
             if (g == 0) {
                 stat[wave][r][0] = st.m;
@@ -375,67 +384,69 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
 }
 
 // Joins the parts of the units that span workgroups of attend_few_kernel
-// (`launched` of them): a workgroup per unit and row, D / 4 lanes for the
-// dimensions and as many teams of them as fit for the parts.
+// (`launched` of them): a workgroup per `span` (1, 2, 4 or 8) rows of a unit, D / 4
+// lanes for the dimensions and teams of them for the rows and the parts.
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int launched, int row_tiles_most, int rows_most) {
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int launched, int row_tiles_most, int spans, int span) {
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
-    __shared__ int lds[4];
-    __shared__ float sums[kTeams][D + 1];
+    __shared__ unsigned long long lds[4];
+    __shared__ float sums[kTeams][D + 4], stat[kTeams][2];
     const int tid = threadIdx.x;
-    const int r = blockIdx.x % rows_most, rest = blockIdx.x / rows_most;
-    const int per_seq = a.c.kv_heads * row_tiles_most;
+    const int rest = blockIdx.x / spans, per_seq = a.c.kv_heads * row_tiles_most;
     const int seq = rest / per_seq, unit = rest - seq * per_seq;
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
     const int rows = s.n * a.group, row_tiles = few_row_tiles(a, s);
     if (unit >= row_tiles * a.c.kv_heads) return;
     const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
+    const int r0 = (blockIdx.x - rest * spans) * span;
     const int tiles = few_tiles(reach_of(a, s));
-    if (tiles == 1 || row0 + r >= rows) return;
-    int all = 0, mine = 0;
+    if (tiles == 1 || row0 + r0 >= rows) return;
+    unsigned long long work = 0;        // of all sequences, and above that of those before this one
     for (int i = tid; i < a.c.seqs; i += 256) {
-        const int n = few_work(a, i);
-        all += n;
-        if (i < seq) mine += n;
+        const unsigned n = few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
+        work += n;
+        if (i < seq) work += static_cast<unsigned long long>(n) << 32;
     }
-    const FewPlan plan(few_sum(all, lds), launched);
-    const int u0 = few_sum(mine, lds) + unit * tiles, w0 = plan.owner(u0), w1 = plan.owner(u0 + tiles - 1);
+    work = few_sum(work, lds);
+    const FewPlan plan(static_cast<int>(work), launched);
+    const int u0 = static_cast<int>(work >> 32) + unit * tiles, w0 = plan.owner(u0), w1 = plan.owner(u0 + tiles - 1);
     if (w0 == w1) return;
     // the unit's first workgroup may have begun with another unit
     const float* part0 = a.partials + (2 * static_cast<size_t>(w0) + (plan.from(w0) == u0 ? 0 : 1)) * kFewSlot<D>;
     auto part = [&](int w) { return w == w0 ? part0 : a.partials + 2 * static_cast<size_t>(w) * kFewSlot<D>; };
-    const int team = tid / kLanes, d = tid % kLanes * 4;
+    // teams span t + i take row r0 + i
+    const int team = tid / kLanes, r = r0 + team % span, d = tid % kLanes * 4;
+    const bool there = r < kFewRows && row0 + r < rows;
     float m = kNoScore, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int w = w0 + team; w <= w1; w += kTeams) {
-        const float* p = part(w);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p + 2 * kFewRows + r * D + d);
-        const float pm = p[r], mnew = fmaxf(m, pm), fo = fast_exp2(m - mnew), fp = fast_exp2(pm - mnew);
-        l = l * fo + p[kFewRows + r] * fp;
-        o = o * fo + x * fp;
-        m = mnew;
-    }
-    // the teams': m and l, then the sums
-    __shared__ float stat[kTeams][2];
+    if (there)
+        for (int w = w0 + team / span; w <= w1; w += kTeams / span) {
+            const float* p = part(w);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(p + 2 * kFewRows + r * D + d);
+            const float pm = p[r], mnew = fmaxf(m, pm), fo = fast_exp2(m - mnew), fp = fast_exp2(pm - mnew);
+            l = l * fo + p[kFewRows + r] * fp;
+            o = o * fo + x * fp;
+            m = mnew;
+        }
+    // the first team of a row adds the others
     if (d == 0) {
         stat[team][0] = m;
         stat[team][1] = l;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sums[team][d + i] = o[i];
+    *reinterpret_cast<f32x4*>(&sums[team][d]) = o;
     __syncthreads();
-    if (tid < D) {
-        for (int i = 0; i < kTeams; ++i) m = fmaxf(m, stat[i][0]);
-        float sum = 0.f, x = 0.f;
-        for (int i = 0; i < kTeams; ++i) {
-            const float f = fast_exp2(stat[i][0] - m);
-            sum += f * stat[i][1];
-            x += f * sums[i][tid];
-        }
-        const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
-        reinterpret_cast<_Float16*>(a.out)[(s.row0 + t) * a.out_stride + h * D + tid] =
-            static_cast<_Float16>(sum > 0.f ? x / sum : 0.f);
+    if (!there || team >= span) return;
+    for (int i = team + span; i < kTeams; i += span) {
+        const float pm = stat[i][0], mnew = fmaxf(m, pm), fo = fast_exp2(m - mnew), fp = fast_exp2(pm - mnew);
+        l = l * fo + stat[i][1] * fp;
+        o = o * fo + *reinterpret_cast<const f32x4*>(&sums[i][d]) * fp;
+        m = mnew;
     }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
+    f16x4 v;
+    for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
+    *reinterpret_cast<f16x4*>(a.out + (s.row0 + t) * a.out_stride + h * D + d) = v;
 }
 
 // ---------------------------------------------------------------- many rows
@@ -501,14 +512,9 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
         row_tiles += t;
         if (t) most = max(most, (r.end - r.begin + kManyTile - 1) / kManyTile);
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        row_tiles += __shfl_xor(row_tiles, o, 64);
-        most = max(most, __shfl_xor(most, o, 64));
-    }
     ManyPlan p;
-    p.row_tiles = __builtin_amdgcn_readfirstlane(row_tiles);
-    most = __builtin_amdgcn_readfirstlane(most);
+    p.row_tiles = wave_all(Sum(), row_tiles);
+    most = wave_all(Max(), most);
     p.splits = many_splits<D, NW>(p.row_tiles * a.c.kv_heads, most, slots);
     return p;
 }
@@ -519,13 +525,7 @@ __device__ __forceinline__ void many_find(const AttendArgs& a, int rank, int& se
     const int lane = threadIdx.x & 63;
     for (int i = 0, before = 0; i < a.c.seqs; i += 64) {
         const int n = i + lane < a.c.seqs ? many_row_tiles<NW>(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i + lane)) : 0;
-        int upto = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += u;
-        }
-        upto += before;
+        const int upto = wave_upto(Sum(), n) + before;
         const unsigned long long has = __ballot(upto > rank);
         if (has) {
             const int l = __builtin_ctzll(has);
@@ -753,9 +753,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                 }
                 top = fmaxf(top, x - c);
             }
-            const uint32_t ut = __builtin_bit_cast(uint32_t, top);
-            const auto sw = __builtin_amdgcn_permlane32_swap(ut, ut, false, false);
-            top = fmaxf(__builtin_bit_cast(float, static_cast<uint32_t>(sw[0])), __builtin_bit_cast(float, static_cast<uint32_t>(sw[1])));
+            top = with_half(Larger(), top);
             if (__any(top > m + kSlack) || lnew != lref) {
                 const float mnew = fmaxf(m, top), alpha = fast_exp2(m - mnew), beta = alpha * fast_exp2(lref - lnew);
                 l *= alpha;
@@ -799,7 +797,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         tile(j, 0, sc, sc2);
         if (j + 1 < n) tile(j + 1, 1, sc2, sc);
     }
-    l += __shfl_xor(l, 32, 64);
+    l = with_half(Sum(), l);
     if (!there) return;
     if (splits > 1) {
         float* slot = a.partials + static_cast<size_t>(blockIdx.x) * kManySlot<D, NW>;

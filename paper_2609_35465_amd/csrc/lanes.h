@@ -78,4 +78,18 @@ __device__ __forceinline__ T team_all(F f, T v) {
     return v;
 }
 
+// f of the lane's v and that of lane ^ 32, or of lane ^ 16
+template <class F>
+__device__ __forceinline__ float with_half(F f, float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return f(__builtin_bit_cast(float, static_cast<uint32_t>(r[0])), __builtin_bit_cast(float, static_cast<uint32_t>(r[1])));
+}
+template <class F>
+__device__ __forceinline__ float with_row(F f, float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return f(__builtin_bit_cast(float, static_cast<uint32_t>(r[0])), __builtin_bit_cast(float, static_cast<uint32_t>(r[1])));
+}
+
 }  // namespace tetra_dev

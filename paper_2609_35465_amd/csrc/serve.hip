@@ -71,7 +71,7 @@ constexpr int kMaxVocab = 1 << 22;     // so that a row's sum of weights, 2^62 a
 // pieces, are the device's own matter.
 struct AttendPlan {
     long long few_grid = 0, join_grid = 0;            // attend_few_kernel, 0: none
-    int row_tiles = 0, rows_most = 0;                 // of a sequence in it: row tiles; rows of one
+    int row_tiles = 0, spans = 0, span = 1;           // of a sequence in it: row tiles; the join's rows a workgroup
     long long many_grid = 0, many_join_grid = 0;      // attend_many_kernel, 0: none
     int waves = 0, slots = 0;
 };
@@ -118,11 +118,16 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
         if (static_cast<long long>(a.c.seqs) * a.max_new == a.rows) return p;
     }
     p.row_tiles = (a.few_most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
-    p.rows_most = std::min(a.few_most, tetra_dev::kFewRows);
     p.few_grid = few_groups;
     const long long units = static_cast<long long>(p.row_tiles) * a.c.kv_heads * a.c.seqs;
     if (units > kMaxGrid / tiles) p.few_grid = kMaxGrid + 1;
-    if (tiles > 1) p.join_grid = units * p.rows_most;
+    if (tiles > 1) {
+        // a row a workgroup where that is few of them, and the parts may be many
+        const int rows_most = std::min(a.few_most, tetra_dev::kFewRows);
+        while (p.span < 8 && p.span < rows_most && units * rows_most > 2 * p.span * cus) p.span *= 2;
+        p.spans = (rows_most + p.span - 1) / p.span;
+        p.join_grid = units * p.spans;
+    }
     return p;
 }
 
@@ -150,7 +155,7 @@ int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
         hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), dim3(static_cast<unsigned>(p.few_grid)), dim3(256), 0, stream, a);
         if (p.join_grid)
             hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), dim3(static_cast<unsigned>(p.join_grid)), dim3(256), 0,
-                               stream, a, static_cast<int>(p.few_grid), p.row_tiles, p.rows_most);
+                               stream, a, static_cast<int>(p.few_grid), p.row_tiles, p.spans, p.span);
     }
     return launch_status();
 }
