@@ -19,7 +19,8 @@ struct AttendArgs {
     const uint16_t* q;
     const int* starts;
     uint16_t* out;
-    float* partials;
+    float* partials;  // of attend_few's workgroups
+    float* pieces;    // of the many-row units
     long long q_stride, out_stride;
     float scale;      // |scale| log2(e)
     uint32_t q_flip;  // 0x80008000 if the scale is negative: turns q instead
@@ -246,13 +247,23 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
-    __shared__ float sums[kFewWaves][kFewRows][D + 4];
-    __shared__ float stat[kFewWaves][kFewRows][2];
-    __shared__ int lds[4], found[2];
-    __shared__ Span found_span;
+struct FewLds {
+    float sums[kFewWaves][kFewRows][D + 4];
+    float stat[kFewWaves][kFewRows][2];
+    int lds[4], found[2];
+    Span span;
+};
+
+// workgroup w of `launched`
+template <int D>
+__device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launched, FewLds<D>& sh) {
+    auto& sums = sh.sums;
+    auto& stat = sh.stat;
+    auto& lds = sh.lds;
+    auto& found = sh.found;
+    Span& found_span = sh.span;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r = lane & 15, g = lane >> 4, w = blockIdx.x;
+    const int r = lane & 15, g = lane >> 4;
     // The total, and the sequence that holds this workgroup's first tile with the
     // tiles before it.  Up to 256 sequences are one scan, more take two passes.
     auto scan = [&](int n, int& all) {
@@ -280,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
             more += few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
         total += few_sum(more, lds);
     }
-    const FewPlan plan(__builtin_amdgcn_readfirstlane(total), gridDim.x);
+    const FewPlan plan(__builtin_amdgcn_readfirstlane(total), launched);
     if (w >= plan.workers) return;
     const int from = plan.from(w), to = plan.from(w + 1);
     for (int s0 = 0, n = n0, before = 0;;) {
@@ -383,22 +394,33 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
     }
 }
 
-// Joins the parts of the units that span workgroups of attend_few_kernel
-// (`launched` of them): a workgroup per `span` (1, 2, 4 or 8) rows of a unit, D / 4
-// lanes for the dimensions and teams of them for the rows and the parts.
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int launched, int row_tiles_most, int spans, int span) {
+__global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
+    __shared__ FewLds<D> sh;
+    attend_few<D>(a, blockIdx.x, gridDim.x, sh);
+}
+
+// Joins the parts of the units that span workgroups of attend_few (`launched` of
+// them): a workgroup per `span` (1, 2, 4 or 8) rows of a unit, D / 4 lanes for the
+// dimensions and teams of them for the rows and the parts.
+struct JoinShape {
+    int launched, row_tiles_most, spans, span;
+};
+
+template <int D>
+__device__ __forceinline__ void attend_join(const AttendArgs& a, int block, const JoinShape& shape) {
+    const int launched = shape.launched, row_tiles_most = shape.row_tiles_most, spans = shape.spans, span = shape.span;
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
     __shared__ unsigned long long lds[4];
     __shared__ float sums[kTeams][D + 4], stat[kTeams][2];
     const int tid = threadIdx.x;
-    const int rest = blockIdx.x / spans, per_seq = a.c.kv_heads * row_tiles_most;
+    const int rest = block / spans, per_seq = a.c.kv_heads * row_tiles_most;
     const int seq = rest / per_seq, unit = rest - seq * per_seq;
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
     const int rows = s.n * a.group, row_tiles = few_row_tiles(a, s);
     if (unit >= row_tiles * a.c.kv_heads) return;
     const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
-    const int r0 = (blockIdx.x - rest * spans) * span;
+    const int r0 = (block - rest * spans) * span;
     const int tiles = few_tiles(reach_of(a, s));
     if (tiles == 1 || row0 + r0 >= rows) return;
     unsigned long long work = 0;        // of all sequences, and above that of those before this one
@@ -447,6 +469,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, int laun
     f16x4 v;
     for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
     *reinterpret_cast<f16x4*>(a.out + (s.row0 + t) * a.out_stride + h * D + d) = v;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinShape shape) {
+    attend_join<D>(a, blockIdx.x, shape);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -547,14 +574,27 @@ __device__ __forceinline__ int split_from(int split, int tiles, int splits) {
 template <int D, int NW>
 constexpr int kManySlot = 32 * NW * (D + 2);
 
+template <int D>
+struct ManyLds {
+    _Float16 k[2][D / 8][kManyTile][8];   // [8 dimensions][token]
+    _Float16 v[2][4][2][D][8];            // [16 tokens][half][dimension][8 tokens]
+};
+
+// Workgroups from `blocks` on, `few` of them, run attend_few: in a batch of
+// prompts and single tokens both go side by side.
 template <int D, int NW, bool ONE>
-__global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, int slots) {
+__global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, int slots, int blocks, int few) {
     constexpr int kRows = 32 * NW, kThreads = 64 * NW;
     constexpr int kKeys = 4 * D, kPer = 8 * D / kThreads;       // 16-byte pieces of a tile's keys; a thread's pieces of both
     constexpr int kGroups = ONE ? 1 : 4, kWindow = 64 / kGroups;   // scales of a tile; tiles whose scales 64 lanes hold
     static_assert(8 * D % kThreads == 0, "whole pieces a thread");
-    __shared__ __align__(16) _Float16 kt[2][D / 8][kManyTile][8];   // [8 dimensions][token]
-    __shared__ __align__(16) _Float16 vt[2][4][2][D][8];            // [16 tokens][half][dimension][8 tokens]
+    constexpr size_t kLds = sizeof(ManyLds<D>) > sizeof(FewLds<D>) ? sizeof(ManyLds<D>) : sizeof(FewLds<D>);
+    __shared__ __align__(16) char lds[kLds];
+    if constexpr (NW == kFewWaves)
+        if (static_cast<int>(blockIdx.x) >= blocks)
+            return attend_few<D>(a, blockIdx.x - blocks, few, *reinterpret_cast<FewLds<D>*>(lds));
+    auto& kt = reinterpret_cast<ManyLds<D>*>(lds)->k;
+    auto& vt = reinterpret_cast<ManyLds<D>*>(lds)->v;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const ManyPlan plan = many_plan<D, NW>(a, slots);
     // the last row tiles first: those have the most keys
@@ -800,7 +840,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     l = with_half(Sum(), l);
     if (!there) return;
     if (splits > 1) {
-        float* slot = a.partials + static_cast<size_t>(blockIdx.x) * kManySlot<D, NW>;
+        float* slot = a.pieces + static_cast<size_t>(blockIdx.x) * kManySlot<D, NW>;
         const int r = 32 * wave + (lane & 31);
         if (half == 0) {
             slot[r] = m;
@@ -833,9 +873,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
 template <int D>
 constexpr int kJoinRows = 1024 / D;
 
+// Workgroups from `blocks` on run attend_join.
 template <int D, int NW>
-__global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots) {
+__global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots, int blocks, JoinShape shape) {
     constexpr int kRows = 32 * NW, kParts = kRows / kJoinRows<D>;
+    if (static_cast<int>(blockIdx.x) >= blocks) return attend_join<D>(a, blockIdx.x - blocks, shape);
     const ManyPlan plan = many_plan<D, NW>(a, slots);
     if (plan.splits == 1) return;
     const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts, head = rest % a.c.kv_heads;
@@ -847,7 +889,7 @@ __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int
     const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
     const int row0 = (rank - first) * kRows, r = part * kJoinRows<D> + static_cast<int>(threadIdx.x) / (D / 4);
     if (row0 + r >= s.n * a.group) return;
-    const float* unit = a.partials +
+    const float* unit = a.pieces +
                         (static_cast<size_t>(rest / a.c.kv_heads) * plan.splits * a.c.kv_heads + head) * kManySlot<D, NW>;
     const size_t step = static_cast<size_t>(a.c.kv_heads) * kManySlot<D, NW>;
     const int d = static_cast<int>(threadIdx.x) % (D / 4) * 4;

@@ -55,13 +55,11 @@ int device_cus(int* cus) {
 constexpr int kFewGroupsPerCU = 2;
 constexpr size_t kMinAttendWorkspace = 4096;
 
-// the parts of attend_few_kernel's workgroups, or the pieces of
-// attend_many_kernel's units (as many of 128 rows as of 256 in twice the room);
-// the kernels of a call run one after another
+// the parts of attend_few's workgroups, and behind them the pieces of the
+// many-row units (of 128 rows twice as many as of 256, in the same room)
+size_t few_parts(int cus) { return static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128>; }
 size_t attend_workspace(int cus) {
-    const size_t few = static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128>;
-    const size_t many = static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 8>;
-    return (std::max(few, many) * sizeof(float) + 255) / 256 * 256;
+    return ((few_parts(cus) + static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 8>) * sizeof(float) + 255) / 256 * 256;
 }
 
 constexpr long long kMaxGrid = 0x7FFFFFFFll;
@@ -131,32 +129,40 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     return p;
 }
 
+// the many-row kernel, with `few` workgroups of the other in the same launch
 template <int D, int NW>
-void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
-    const dim3 g(static_cast<unsigned>(p.many_grid)), b(64 * NW), j(static_cast<unsigned>(p.many_join_grid));
+void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, int few, hipStream_t stream) {
+    const dim3 g(static_cast<unsigned>(p.many_grid + few)), b(64 * NW);
+    const int blocks = static_cast<int>(p.many_grid);
     if (a.c.page_tokens >= tetra_dev::kManyTile)
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, true>), g, b, 0, stream, a, p.slots);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, true>), g, b, 0, stream, a, p.slots, blocks, few);
     else
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, false>), g, b, 0, stream, a, p.slots);
-    if (p.many_join_grid)
-        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, NW>), j, dim3(256), 0, stream, a, p.slots);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, false>), g, b, 0, stream, a, p.slots, blocks, few);
 }
 
 template <int D>
 int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
     const AttendPlan p = attend_plan<D>(a, cus);
-    if (p.few_grid > kMaxGrid || p.join_grid > kMaxGrid || p.many_grid > kMaxGrid) return TETRA_EINVAL;
+    if (p.few_grid > kMaxGrid || p.many_grid + p.few_grid > kMaxGrid || p.many_join_grid + p.join_grid > kMaxGrid)
+        return TETRA_EINVAL;
+    const tetra_dev::JoinShape shape{static_cast<int>(p.few_grid), p.row_tiles, p.spans, p.span};
+    const bool together = p.waves == tetra_dev::kFewWaves;      // workgroups of one size: both kinds in a launch
+    const int few = together ? static_cast<int>(p.few_grid) : 0;
     if (p.many_grid) {
-        if (p.waves == 8) attend_many_launch<D, 8>(a, p, stream);
-        else attend_many_launch<D, 4>(a, p, stream);
-        if (int st = launch_status()) return st;
+        if (p.waves == 8) attend_many_launch<D, 8>(a, p, 0, stream);
+        else attend_many_launch<D, 4>(a, p, few, stream);
     }
-    if (p.few_grid) {
+    if (p.few_grid && !few)
         hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), dim3(static_cast<unsigned>(p.few_grid)), dim3(256), 0, stream, a);
-        if (p.join_grid)
-            hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), dim3(static_cast<unsigned>(p.join_grid)), dim3(256), 0,
-                               stream, a, static_cast<int>(p.few_grid), p.row_tiles, p.spans, p.span);
-    }
+    if (int st = launch_status()) return st;
+    const int blocks = static_cast<int>(p.many_join_grid);
+    const dim3 g(static_cast<unsigned>(p.many_join_grid + p.join_grid));
+    if (blocks && p.waves == 8)
+        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 8>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
+    else if (blocks)
+        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
+    else if (p.join_grid)
+        hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), g, dim3(256), 0, stream, a, shape);
     return launch_status();
 }
 
@@ -262,6 +268,7 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     a.starts = starts;
     a.out = out;
     a.partials = static_cast<float*>(workspace);
+    a.pieces = a.partials + few_parts(cus);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.scale = std::fabs(scale) * 1.44269504f;

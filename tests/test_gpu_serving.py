@@ -382,6 +382,18 @@ def test_attend_windows(window, news):
     _check_attend(Cache(24, lens, 2, 32, 128), news, 10, window=window)
 
 
+@pytest.mark.parametrize("seqs", [257, 600])
+@pytest.mark.parametrize("prompts", [False, True])
+def test_attend_many_sequences(seqs, prompts):
+    """More sequences than a workgroup scans at once, idle ones and (in some) prompts among them."""
+    rng = np.random.default_rng(seqs)
+    news = rng.integers(0, 3, seqs)
+    if prompts:
+        news[rng.integers(0, seqs, 6)] = rng.integers(40, 150, 6)
+    lens = [int(n + rng.integers(0, 500) * (n > 0)) for n in news]
+    _check_attend(Cache(34, lens, 1, 16, 64), news, 2)
+
+
 @pytest.mark.parametrize("news", [(1,), (40,), (200,)])
 def test_attend_long_context(news):
     """Many pieces of one sequence, with the context's end inside a page."""
