@@ -25,6 +25,7 @@ struct AttendArgs {
     float scale;      // |scale| log2(e)
     uint32_t q_flip;  // 0x80008000 if the scale is negative: turns q instead
     int rows, max_new, q_heads, group, window;
+    int few_tile;     // tokens of a tile of attend_few: 64 for each wave of its workgroups
     int few_most;     // sequences of up to so many rows (token, q head of a group) go through attend_few_kernel
 };
 
@@ -76,8 +77,6 @@ __device__ __forceinline__ float over_groups(F f, float v) { return with_half(f,
 // + i, so a lane of group g = lane / 16 gets the scores of 16 consecutive
 // tokens, and its V operand is one 16-byte load of the transposed values.
 
-constexpr int kFewWaves = 4;
-constexpr int kFewTile = 64 * kFewWaves;
 constexpr int kFewRows = 16;
 
 // slots of a workgroup's parts: [2][kFewRows] m and l, [kFewRows][D] sums
@@ -99,7 +98,9 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs& a, const Span& s) {
 
 // tiles of a sequence's unit (one at least, so that rows without keys are
 // written) and its units
-__device__ __forceinline__ int few_tiles(const Reach& r) { return max(1, (r.end - r.begin + kFewTile - 1) / kFewTile); }
+__device__ __forceinline__ int few_tiles(const AttendArgs& a, const Reach& r) {
+    return max(1, (r.end - r.begin + a.few_tile - 1) / a.few_tile);
+}
 
 // row tiles of a sequence: none if it goes through attend_many_kernel
 __device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Span& s) {
@@ -108,17 +109,19 @@ __device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Span& s)
 }
 
 __device__ __forceinline__ int few_work(const AttendArgs& a, const Span& s) {
-    return few_row_tiles(a, s) * a.c.kv_heads * few_tiles(reach_of(a, s));
+    return few_row_tiles(a, s) * a.c.kv_heads * few_tiles(a, reach_of(a, s));
 }
 
-// sum over the workgroup's four waves, in every thread
-template <class T>
+// sum over the workgroup's WAVES waves, in every thread
+template <int WAVES, class T>
 __device__ __forceinline__ T few_sum(T v, T* lds) {
     v = wave_all(Sum(), v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+    v = lds[0];
+    for (int w = 1; w < WAVES; ++w) v += lds[w];
+    return v;
 }
 
 // The workgroups that take part, a tile each at least, the first tile of one and
@@ -144,8 +147,8 @@ struct FewState {
     f32x4 o[D / 16];
 };
 
-// A wave's blocks of a segment: tokens from `block0`, every kFewTile further, below `stop`.
-template <int D>
+// A wave's blocks of a segment: tokens from `block0`, every STEP further, below `stop`.
+template <int D, int STEP>
 __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st, const f16x8 (&q)[D / 32],
                                             const int* table, int head, int block0, int stop, int row_begin,
                                             int row_end) {
@@ -181,8 +184,8 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
     if (block0 >= stop) return;
     Block b;
     load(b, block0, page_at(block0 + 16 * (r >> 2)), page_at(block0 + 16 * g));
-    for (int t0 = block0; t0 < stop; t0 += kFewTile) {
-        const int next = t0 + kFewTile;
+    for (int t0 = block0; t0 < stop; t0 += STEP) {
+        const int next = t0 + STEP;
         const int pk = page_at(next + 16 * (r >> 2)), pv = page_at(next + 16 * g);
         f32x4 s[4];
 #pragma unroll
@@ -246,17 +249,18 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
     }
 }
 
-template <int D>
+template <int D, int WAVES>
 struct FewLds {
-    float sums[kFewWaves][kFewRows][D + 4];
-    float stat[kFewWaves][kFewRows][2];
-    int lds[4], found[2];
+    float sums[WAVES][kFewRows][D + 4];
+    float stat[WAVES][kFewRows][2];
+    int lds[WAVES], found[2];
     Span span;
 };
 
-// workgroup w of `launched`
-template <int D>
-__device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launched, FewLds<D>& sh) {
+// workgroup w of `launched`, WAVES waves each (a.few_tile is 64 WAVES)
+template <int D, int WAVES>
+__device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launched, FewLds<D, WAVES>& sh) {
+    constexpr int kTile = 64 * WAVES;      // tokens, and threads
     auto& sums = sh.sums;
     auto& stat = sh.stat;
     auto& lds = sh.lds;
@@ -265,14 +269,14 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     // The total, and the sequence that holds this workgroup's first tile with the
-    // tiles before it.  Up to 256 sequences are one scan, more take two passes.
+    // tiles before it.  As many sequences as threads are one scan, more take two passes.
     auto scan = [&](int n, int& all) {
         int upto = wave_upto(Sum(), n);
         __syncthreads();
         if (lane == 63) lds[wave] = upto;
         __syncthreads();
         all = 0;
-        for (int i = 0; i < kFewWaves; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             if (i < wave) upto += lds[i];
             all += lds[i];
         }
@@ -285,11 +289,11 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
         n0 = few_work(a, mine);
     }
     int all, upto = scan(n0, all), total = all;
-    if (a.c.seqs > 256) {
+    if (a.c.seqs > kTile) {
         int more = 0;
-        for (int i = tid + 256; i < a.c.seqs; i += 256)
+        for (int i = tid + kTile; i < a.c.seqs; i += kTile)
             more += few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
-        total += few_sum(more, lds);
+        total += few_sum<WAVES>(more, lds);
     }
     const FewPlan plan(__builtin_amdgcn_readfirstlane(total), launched);
     if (w >= plan.workers) return;
@@ -301,7 +305,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             found_span = mine;
         }
         before += all;
-        s0 += 256;
+        s0 += kTile;
         if (before > from || s0 >= a.c.seqs) break;
         n = 0;
         if (s0 + tid < a.c.seqs) {
@@ -321,7 +325,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
     for (int x = from; x < to && seq < a.c.seqs; ++seq) {
         if (!first) s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
         const Reach reach = reach_of(a, s);
-        const int tiles = few_tiles(reach), rows = s.n * a.group;
+        const int tiles = few_tiles(a, reach), rows = s.n * a.group;
         const int row_tiles = few_row_tiles(a, s), units = row_tiles * a.c.kv_heads;
         const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
         for (int unit = (x - base) / tiles; unit < units && x < to; ++unit) {
@@ -347,8 +351,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             st.l = 0.f;
             st.vref = 1e-37f;
             for (f32x4& o : st.o) o = f32x4{0.f, 0.f, 0.f, 0.f};
-            few_segment<D>(a, st, q, table, head, reach.begin + tile0 * kFewTile + wave * 64,
-                           min(reach.end, reach.begin + tile1 * kFewTile), row_begin, row_end);
+            few_segment<D, kTile>(a, st, q, table, head, reach.begin + tile0 * kTile + wave * 64,
+                                  min(reach.end, reach.begin + tile1 * kTile), row_begin, row_end);
             const float l = over_groups(Sum(), st.l);
             __syncthreads();
             if (g == 0) {
@@ -362,13 +366,13 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             // the waves' sums joined, 4 dimensions a thread
             const bool whole = tile0 == 0 && tile1 == tiles;
             float* slot = a.partials + (2 * static_cast<size_t>(w) + (first ? 0 : 1)) * kFewSlot<D>;
-            for (int e = tid; e < min(rows - row0, kFewRows) * (D / 4); e += 256) {
+            for (int e = tid; e < min(rows - row0, kFewRows) * (D / 4); e += kTile) {
                 const int er = e / (D / 4), ed = e % (D / 4) * 4;
                 float m = stat[0][er][0];
-                for (int i = 1; i < kFewWaves; ++i) m = fmaxf(m, stat[i][er][0]);
+                for (int i = 1; i < WAVES; ++i) m = fmaxf(m, stat[i][er][0]);
                 float sum = 0.f;
                 f32x4 o = {0.f, 0.f, 0.f, 0.f};
-                for (int i = 0; i < kFewWaves; ++i) {
+                for (int i = 0; i < WAVES; ++i) {
                     const float f = fast_exp2(stat[i][er][0] - m);
                     sum += f * stat[i][er][1];
                     o += f * *reinterpret_cast<const f32x4*>(&sums[i][er][ed]);
@@ -396,8 +400,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a) {
-    __shared__ FewLds<D> sh;
-    attend_few<D>(a, blockIdx.x, gridDim.x, sh);
+    __shared__ FewLds<D, 4> sh;
+    attend_few<D, 4>(a, blockIdx.x, gridDim.x, sh);
 }
 
 // Joins the parts of the units that span workgroups of attend_few (`launched` of
@@ -421,7 +425,7 @@ __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, cons
     if (unit >= row_tiles * a.c.kv_heads) return;
     const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
     const int r0 = (block - rest * spans) * span;
-    const int tiles = few_tiles(reach_of(a, s));
+    const int tiles = few_tiles(a, reach_of(a, s));
     if (tiles == 1 || row0 + r0 >= rows) return;
     unsigned long long work = 0;        // of all sequences, and above that of those before this one
     for (int i = tid; i < a.c.seqs; i += 256) {
@@ -429,7 +433,7 @@ __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, cons
         work += n;
         if (i < seq) work += static_cast<unsigned long long>(n) << 32;
     }
-    work = few_sum(work, lds);
+    work = few_sum<4>(work, lds);
     const FewPlan plan(static_cast<int>(work), launched);
     const int u0 = static_cast<int>(work >> 32) + unit * tiles, w0 = plan.owner(u0), w1 = plan.owner(u0 + tiles - 1);
     if (w0 == w1) return;
@@ -508,17 +512,17 @@ struct ManyPlan {
 };
 
 // Units that do not fill the chip (`slots` workgroups at once) are cut along
-// their keys where that pays: a tile takes a workgroup 1.4 us, a piece's sums on
-// their way through memory D / 4096 us (128 rows; all pieces' together), the
-// join's launch 6 us.  Measured, 128 rows a workgroup, 32 heads of 128, us: 203
-// tokens after 3,893 105 whole and 41 in 8 pieces, 100 after 900 34 and 23 in 4;
-// 1,024 from the start 35 whole and 42 in 2, 512 from the start 22 and 27.
-template <int D, int NW>
+// their keys where that pays: a step of KS tiles takes a workgroup 1.75 us, a
+// piece's sums on their way through memory D NW / 16384 us (all pieces' together),
+// the join's launch 6 us.  Measured (one team of 128 rows, 32 heads of 128, us):
+// 203 tokens after 3,893 105 whole and 41 in 8 pieces, 100 after 900 34 and 23 in
+// 4; but 1,024 from the start 35 whole and 42 in 2, 512 from the start 22 and 27.
+template <int D, int NW, int KS>
 __host__ __device__ __forceinline__ int many_splits(int units, int tiles, int slots) {
-    if (units < 1 || 2 * units > slots || tiles < 8) return 1;
-    const float work = 1.4f * tiles, part = units * (D * NW / 16384.f);
+    if (units < 1 || 2 * units > slots || tiles < 4 * KS) return 1;
+    const float work = 1.75f / KS * tiles, part = units * (D * NW / 16384.f);
     float s = sqrtf(work / part);
-    s = fminf(s, fminf(static_cast<float>(slots / units), static_cast<float>(tiles / 4)));
+    s = fminf(s, fminf(static_cast<float>(slots / units), static_cast<float>(tiles / (2 * KS))));
     return s >= 2.f && work * (1.f - 1.f / s) > 6.f + part * s ? static_cast<int>(s) : 1;
 }
 
@@ -529,7 +533,7 @@ __device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s
 }
 
 // slots 0: no unit is cut
-template <int D, int NW>
+template <int D, int NW, int KS>
 __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
     int row_tiles = 0, most = 0;
     for (int i = threadIdx.x & 63; i < a.c.seqs; i += 64) {
@@ -542,7 +546,7 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
     ManyPlan p;
     p.row_tiles = wave_all(Sum(), row_tiles);
     most = wave_all(Max(), most);
-    p.splits = many_splits<D, NW>(p.row_tiles * a.c.kv_heads, most, slots);
+    p.splits = many_splits<D, NW, KS>(p.row_tiles * a.c.kv_heads, most, slots);
     return p;
 }
 
@@ -580,23 +584,29 @@ struct ManyLds {
     _Float16 v[2][4][2][D][8];            // [16 tokens][half][dimension][8 tokens]
 };
 
-// Workgroups from `blocks` on, `few` of them, run attend_few: in a batch of
-// prompts and single tokens both go side by side.
-template <int D, int NW, bool ONE>
-__global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, int slots, int blocks, int few) {
+// NW waves for the rows, KS teams of them for the keys: each takes every KS-th tile
+// of its unit in buffers of its own, and the first adds the others' sums at the
+// end.  With one team, workgroups from `blocks` on, `few` of them, run attend_few:
+// in a batch of prompts and single tokens both go side by side.
+template <int D, int NW, int KS, bool ONE>
+__global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs a, int slots, int blocks, int few) {
     constexpr int kRows = 32 * NW, kThreads = 64 * NW;
+    constexpr int kStep = KS * kManyTile;                       // tokens from a team's tile to its next
     constexpr int kKeys = 4 * D, kPer = 8 * D / kThreads;       // 16-byte pieces of a tile's keys; a thread's pieces of both
     constexpr int kGroups = ONE ? 1 : 4, kWindow = 64 / kGroups;   // scales of a tile; tiles whose scales 64 lanes hold
     static_assert(8 * D % kThreads == 0, "whole pieces a thread");
-    constexpr size_t kLds = sizeof(ManyLds<D>) > sizeof(FewLds<D>) ? sizeof(ManyLds<D>) : sizeof(FewLds<D>);
-    __shared__ __align__(16) char lds[kLds];
-    if constexpr (NW == kFewWaves)
+    using Few = FewLds<D, NW>;
+    constexpr size_t kLds = sizeof(ManyLds<D>) * KS;
+    __shared__ __align__(16) char lds[KS == 1 && kLds < sizeof(Few) ? sizeof(Few) : kLds];
+    if constexpr (KS == 1)
         if (static_cast<int>(blockIdx.x) >= blocks)
-            return attend_few<D>(a, blockIdx.x - blocks, few, *reinterpret_cast<FewLds<D>*>(lds));
-    auto& kt = reinterpret_cast<ManyLds<D>*>(lds)->k;
-    auto& vt = reinterpret_cast<ManyLds<D>*>(lds)->v;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const ManyPlan plan = many_plan<D, NW>(a, slots);
+            return attend_few<D, NW>(a, blockIdx.x - blocks, few, *reinterpret_cast<Few*>(lds));
+    const int lane = threadIdx.x & 63;
+    const int team = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const int tid = threadIdx.x - team * kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto& kt = reinterpret_cast<ManyLds<D>*>(lds)[team].k;
+    auto& vt = reinterpret_cast<ManyLds<D>*>(lds)[team].v;
+    const ManyPlan plan = many_plan<D, NW, KS>(a, slots);
     // the last row tiles first: those have the most keys
     const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, splits = plan.splits;
     const int rank = plan.row_tiles - 1 - rest / splits, split = rest % splits;
@@ -611,7 +621,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     const int reach_end = min(token1 + 1, reach.end), reach_begin = a.window > 0 ? max(0, token0 - a.window + 1) & ~63 : 0;
     const int unit_tiles = max(0, reach_end - reach_begin + kManyTile - 1) / kManyTile;
     const int tile0 = split_from(split, unit_tiles, splits), n = split_from(split + 1, unit_tiles, splits) - tile0;
-    const int begin = reach_begin + tile0 * kManyTile, end = min(reach_end, begin + n * kManyTile);
+    const int piece = reach_begin + tile0 * kManyTile, end = min(reach_end, piece + n * kManyTile);
+    const int begin = piece + team * kManyTile, mine = (n - team + KS - 1) / KS;      // the team's first tile, and its tiles
     const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
     const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
 
@@ -640,7 +651,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         float sg, lv;
     } win, next;
     auto load_pages = [&](Window& w, int first) {
-        const int t = begin + (first * kGroups + lane) * (kManyTile / kGroups);
+        const int t = begin + (first + lane / kGroups) * kStep + lane % kGroups * 16;
         const int id = t < end ? table[t >> a.c.page_shift] : -1;
         w.page = id < a.c.num_pages ? id : -1;
     };
@@ -663,7 +674,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     auto load_piece = [&](int u, int jk, int jv) {
         const int p = tid + u * kThreads;
         if (is_key(u)) {
-            const int t = begin + jk * kManyTile + (ONE ? 0 : p & 48);
+            const int t = begin + jk * kStep + (ONE ? 0 : p & 48);
             int page;
             if constexpr (ONE) page = page_at(jk, 0);
             else page = __shfl(jk - window0 < kWindow ? win.page : next.page, (jk % kWindow) * 4 + ((p & 63) >> 4), 64);
@@ -672,7 +683,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             raw[u] = *reinterpret_cast<const u32x4*>(at + (ONE ? p & 63 : p & 15) * D + (p >> 6) * 16);
         } else {
             const int g = __builtin_amdgcn_readfirstlane((p - kKeys) / D);
-            const int t = begin + jv * kManyTile + 16 * g;
+            const int t = begin + jv * kStep + 16 * g;
             const int8_t* at = a.c.v + (static_cast<size_t>(max(page_at(jv, g), 0)) * a.c.kv_heads + head) * stride +
                                static_cast<size_t>(t & (a.c.page_tokens - 1)) * D;
             raw[u] = *reinterpret_cast<const u32x4*>(at + (p - kKeys) % D * 16);
@@ -693,7 +704,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     // keys of tile jk and values of tile jv, from memory and into LDS (tiles past the last: the last again)
     auto load_tiles = [&](int jk, int jv) {
 #pragma unroll
-        for (int u = 0; u < kPer; ++u) load_piece(u, min(jk, n - 1), min(jv, n - 1));
+        for (int u = 0; u < kPer; ++u) load_piece(u, min(jk, max(mine, 1) - 1), min(jv, max(mine, 1) - 1));
     };
     auto write_tiles = [&](int bk, int bv) {
 #pragma unroll
@@ -720,33 +731,30 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         load_scales(win);
         load_pages(next, kWindow);
         next.sg = next.lv = 0.f;
-        u32x4 first_raw[kPer];
+        // the first two tiles, and the third on its way
+        u32x4 tile0_raw[kPer], tile1_raw[kPer];
+        auto move = [](u32x4 (&to)[kPer], const u32x4 (&from)[kPer]) {
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) to[u] = from[u];
+        };
         load_tiles(0, 0);
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) first_raw[u] = raw[u];
+        move(tile0_raw, raw);
         load_tiles(1, 0);
-        u32x4 second_raw[kPer];
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) second_raw[u] = raw[u];
+        move(tile1_raw, raw);
         load_tiles(2, 1);
-        u32x4 third_raw[kPer];
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) {
-            third_raw[u] = raw[u];
-            raw[u] = first_raw[u];
-        }
+        u32x4 tile2_raw[kPer];
+        move(tile2_raw, raw);
+        move(raw, tile0_raw);
         write_tiles(0, 0);
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) raw[u] = second_raw[u];
+        move(raw, tile1_raw);
         write_tiles(1, 0);
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) raw[u] = third_raw[u];
+        move(raw, tile2_raw);
         __syncthreads();
         scores(sc, 0);
     }
     // tile j, whose scores are in `cur`; those of tile j + 1 go into `ahead`
     auto tile = [&](int j, int b, f32x16 (&cur)[2], f32x16 (&ahead)[2]) {
-        const int t0 = begin + j * kManyTile;
+        const int t0 = begin + j * kStep;
         if (j == window0 + kWindow) {
             win = next;
             window0 = j;
@@ -755,7 +763,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         if (j == window0 + kWindow / 2) load_scales(next);
         __syncthreads();
         // a wave also goes through the tile before its first, for that one's scores
-        if (t0 < any_end && t0 + 2 * kManyTile > any_begin) {
+        if (t0 < any_end && t0 + kStep + kManyTile > any_begin) {
             float sg[kGroups], rel[kGroups], lnew = lref;
             bool none[kGroups], holes = false;
 #pragma unroll
@@ -833,9 +841,38 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     f32x16 sc2[2];
     for (int t = 0; t < 2; ++t)
         for (int i = 0; i < 16; ++i) sc2[t][i] = 0.f;
-    for (int j = 0; j < n; j += 2) {
+    const int steps = (n + KS - 1) / KS;       // of every team, for the barriers
+    for (int j = 0; j < steps; j += 2) {
         tile(j, 0, sc, sc2);
-        if (j + 1 < n) tile(j + 1, 1, sc2, sc);
+        if (j + 1 < steps) tile(j + 1, 1, sc2, sc);
+    }
+    if constexpr (KS > 1) {
+        static_assert(KS == 2 && sizeof(ManyLds<D>) >= sizeof(float) * kThreads * (D / 2), "the second team's sums fit");
+        float* sums = reinterpret_cast<float*>(lds) + tid;
+        float* stat = reinterpret_cast<float*>(lds + sizeof(ManyLds<D>)) + tid;
+        __syncthreads();
+        if (team == 1) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[(16 * d + i) * kThreads] = o[d][i];
+            stat[0] = m;
+            stat[kThreads] = l;
+            stat[2 * kThreads] = lref;
+        }
+        __syncthreads();
+        if (team == 1) return;
+        const float m1 = stat[0], l1 = stat[kThreads], lref1 = stat[2 * kThreads];
+        const float mnew = fmaxf(m, m1), lnew = fmaxf(lref, lref1);
+        const float f0 = fast_exp2(m - mnew), f1 = fast_exp2(m1 - mnew);
+        const float g0 = f0 * fast_exp2(lref - lnew), g1 = f1 * fast_exp2(lref1 - lnew);
+        l = l * f0 + l1 * f1;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * g0 + sums[(16 * d + i) * kThreads] * g1;
+        m = mnew;
+        lref = lnew;
     }
     l = with_half(Sum(), l);
     if (!there) return;
@@ -874,11 +911,11 @@ template <int D>
 constexpr int kJoinRows = 1024 / D;
 
 // Workgroups from `blocks` on run attend_join.
-template <int D, int NW>
+template <int D, int NW, int KS>
 __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots, int blocks, JoinShape shape) {
     constexpr int kRows = 32 * NW, kParts = kRows / kJoinRows<D>;
     if (static_cast<int>(blockIdx.x) >= blocks) return attend_join<D>(a, blockIdx.x - blocks, shape);
-    const ManyPlan plan = many_plan<D, NW>(a, slots);
+    const ManyPlan plan = many_plan<D, NW, KS>(a, slots);
     if (plan.splits == 1) return;
     const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts, head = rest % a.c.kv_heads;
     const int rank = plan.row_tiles - 1 - rest / a.c.kv_heads;

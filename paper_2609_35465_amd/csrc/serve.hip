@@ -56,10 +56,10 @@ constexpr int kFewGroupsPerCU = 2;
 constexpr size_t kMinAttendWorkspace = 4096;
 
 // the parts of attend_few's workgroups, and behind them the pieces of the
-// many-row units (of 128 rows twice as many as of 256, in the same room)
+// many-row units
 size_t few_parts(int cus) { return static_cast<size_t>(cus) * kFewGroupsPerCU * 2 * tetra_dev::kFewSlot<128>; }
 size_t attend_workspace(int cus) {
-    return ((few_parts(cus) + static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 8>) * sizeof(float) + 255) / 256 * 256;
+    return ((few_parts(cus) + 2 * static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 4>) * sizeof(float) + 255) / 256 * 256;
 }
 
 constexpr long long kMaxGrid = 0x7FFFFFFFll;
@@ -71,15 +71,17 @@ struct AttendPlan {
     long long few_grid = 0, join_grid = 0;            // attend_few_kernel, 0: none
     int row_tiles = 0, spans = 0, span = 1;           // of a sequence in it: row tiles; the join's rows a workgroup
     long long many_grid = 0, many_join_grid = 0;      // attend_many_kernel, 0: none
-    int waves = 0, slots = 0;
+    int waves = 0, teams = 0;                         // of its workgroups
+    int slots = 0;                                    // workgroups at once, 0: units are not cut
 };
 
 template <int D>
 AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     AttendPlan p;
+    a.few_tile = 256;
     const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
     const long long reach = a.window > 0 ? std::min<long long>(kept, static_cast<long long>(a.window) + a.max_new + 64) : kept;
-    const long long tiles = (reach + tetra_dev::kFewTile - 1) / tetra_dev::kFewTile;
+    const long long tiles = (reach + a.few_tile - 1) / a.few_tile;
     const long long most = static_cast<long long>(a.max_new) * a.group;      // rows of a sequence
     const long long most_tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
     const long long few_groups = static_cast<long long>(cus) * kFewGroupsPerCU;
@@ -93,30 +95,39 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     if (!all_few) {
         // sequences of the most rows that the rows would make, and their units
         const long long full = (a.rows + a.max_new - 1) / a.max_new;
-        const long long units8 = full * ((most + 255) / 256) * a.c.kv_heads;
-        // 128 rows a workgroup, two of them a CU, while those are one round of the chip (32 heads, 1,024 tokens 35 us
-        // against 41, 2,048 69 and 71), else 256 rows, whose tiles are turned into fp16 for twice as many (4,096 tokens
-        // 174 against 154)
-        p.waves = units8 < cus ? 4 : 8;
-        const int slots = p.waves == 8 ? cus : 2 * cus;
+        const long long units4 = full * ((most + 127) / 128) * a.c.kv_heads;
+        // Where every sequence fills max_new rows there are no few-row sequences; should `starts` end before the last
+        // row after all, attend_many_kernel takes what there is.
+        const bool mixed = static_cast<long long>(a.c.seqs) * a.max_new != a.rows;
+        if (!mixed) a.few_most = 0;
+        // Three forms of the workgroup.  128 rows with two teams for the keys, so that a CU has eight waves for few rows,
+        // where they are one round of the chip, or two rounds of long prompts from the start, whose short units even out.
+        // 256 rows for more: a tile is turned into fp16 for twice as many.  Of batches that may have few-row sequences,
+        // 128 rows with one team up to two rounds, since those run beside it.  Measured (128 rows with one team, with two,
+        // 256 rows; heads of 128, us): 1,024 tokens of 32 heads 36, 32, 43; 2,048 73, 62, 74; 2,800 -, 107, 96; 8 x 203
+        // tokens of 40 heads after 1,797 84, 104, 86; 2 x 500 from the start 25, 30, 28.
+        p.waves = 8;
+        if (mixed ? units4 <= 2 * cus : units4 <= cus || (units4 <= 2 * cus && a.max_new >= 1024)) p.waves = 4;
+        p.teams = p.waves == 4 && !mixed ? 2 : 1;
+        const int at_once = p.waves * p.teams == 4 ? 2 * cus : cus;
         const long long rows = 32 * p.waves, all = static_cast<long long>(a.rows) * a.group;
-        const long long sequences = std::min<long long>(a.c.seqs, all / (few_rows + 1));
+        const long long sequences = std::min<long long>(a.c.seqs, all / (a.few_most + 1));
         const long long units = (all / rows + sequences) * a.c.kv_heads;     // at most
-        p.many_grid = std::max<long long>(units, slots);
-        // the device may cut units if it would at the fewest units and the most keys
+        p.many_grid = std::max<long long>(units, at_once);
+        // the device may cut units of 128 rows if it would at the fewest units and the most keys
         const int least = static_cast<int>(std::min<long long>(std::max<long long>(all / rows, 1) * a.c.kv_heads, kMaxGrid));
         const int longest = static_cast<int>((reach + tetra_dev::kManyTile - 1) / tetra_dev::kManyTile);
-        const int splits = p.waves == 8 ? tetra_dev::many_splits<D, 8>(least, longest, slots)
-                                        : tetra_dev::many_splits<D, 4>(least, longest, slots);
-        if (splits > 1) {
-            p.slots = slots;
-            p.many_join_grid = std::min<long long>(units, slots / 2) * (rows / tetra_dev::kJoinRows<D>);
+        if (p.waves == 4 && (p.teams == 2 ? tetra_dev::many_splits<D, 4, 2>(least, longest, at_once)
+                                          : tetra_dev::many_splits<D, 4, 1>(least, longest, at_once)) > 1) {
+            p.slots = at_once;
+            p.many_join_grid = std::min<long long>(units, at_once / 2) * (rows / tetra_dev::kJoinRows<D>);
         }
-        // every sequence has the most rows: none is left for the other kernel
-        if (static_cast<long long>(a.c.seqs) * a.max_new == a.rows) return p;
+        if (!mixed) return p;
     }
     p.row_tiles = (a.few_most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
-    p.few_grid = few_groups;
+    // in workgroups of the size of attend_many_kernel's, which they run beside
+    p.few_grid = p.waves == 8 ? cus : few_groups;
+    a.few_tile = p.waves == 8 ? 512 : 256;
     const long long units = static_cast<long long>(p.row_tiles) * a.c.kv_heads * a.c.seqs;
     if (units > kMaxGrid / tiles) p.few_grid = kMaxGrid + 1;
     if (tiles > 1) {
@@ -129,15 +140,14 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     return p;
 }
 
-// the many-row kernel, with `few` workgroups of the other in the same launch
-template <int D, int NW>
-void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, int few, hipStream_t stream) {
-    const dim3 g(static_cast<unsigned>(p.many_grid + few)), b(64 * NW);
-    const int blocks = static_cast<int>(p.many_grid);
+template <int D, int NW, int KS>
+void attend_many_launch(const tetra_dev::AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+    const dim3 g(static_cast<unsigned>(p.many_grid + p.few_grid)), b(64 * NW * KS);
+    const int blocks = static_cast<int>(p.many_grid), few = static_cast<int>(p.few_grid);
     if (a.c.page_tokens >= tetra_dev::kManyTile)
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, true>), g, b, 0, stream, a, p.slots, blocks, few);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, KS, true>), g, b, 0, stream, a, p.slots, blocks, few);
     else
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, false>), g, b, 0, stream, a, p.slots, blocks, few);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, NW, KS, false>), g, b, 0, stream, a, p.slots, blocks, few);
 }
 
 template <int D>
@@ -145,22 +155,18 @@ int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
     const AttendPlan p = attend_plan<D>(a, cus);
     if (p.few_grid > kMaxGrid || p.many_grid + p.few_grid > kMaxGrid || p.many_join_grid + p.join_grid > kMaxGrid)
         return TETRA_EINVAL;
-    const tetra_dev::JoinShape shape{static_cast<int>(p.few_grid), p.row_tiles, p.spans, p.span};
-    const bool together = p.waves == tetra_dev::kFewWaves;      // workgroups of one size: both kinds in a launch
-    const int few = together ? static_cast<int>(p.few_grid) : 0;
-    if (p.many_grid) {
-        if (p.waves == 8) attend_many_launch<D, 8>(a, p, 0, stream);
-        else attend_many_launch<D, 4>(a, p, few, stream);
-    }
-    if (p.few_grid && !few)
-        hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), dim3(static_cast<unsigned>(p.few_grid)), dim3(256), 0, stream, a);
+    if (p.waves == 8) attend_many_launch<D, 8, 1>(a, p, stream);
+    else if (p.teams == 2) attend_many_launch<D, 4, 2>(a, p, stream);
+    else if (p.teams == 1) attend_many_launch<D, 4, 1>(a, p, stream);
+    else hipLaunchKernelGGL((tetra_dev::attend_few_kernel<D>), dim3(static_cast<unsigned>(p.few_grid)), dim3(256), 0, stream, a);
     if (int st = launch_status()) return st;
+    const tetra_dev::JoinShape shape{static_cast<int>(p.few_grid), p.row_tiles, p.spans, p.span};
     const int blocks = static_cast<int>(p.many_join_grid);
     const dim3 g(static_cast<unsigned>(p.many_join_grid + p.join_grid));
-    if (blocks && p.waves == 8)
-        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 8>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
+    if (blocks && p.teams == 1)
+        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4, 1>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
     else if (blocks)
-        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
+        hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4, 2>), g, dim3(256), 0, stream, a, p.slots, blocks, shape);
     else if (p.join_grid)
         hipLaunchKernelGGL((tetra_dev::attend_join_kernel<D>), g, dim3(256), 0, stream, a, shape);
     return launch_status();

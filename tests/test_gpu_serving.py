@@ -394,6 +394,24 @@ def test_attend_many_sequences(seqs, prompts):
     _check_attend(Cache(34, lens, 1, 16, 64), news, 2)
 
 
+@pytest.mark.parametrize("news,rows", [((60, 2), 120), ((1, 0, 1), 3), ((300, 1, 0), 900), ((7, 3), 14)])
+def test_attend_rows_past_the_last_start(news, rows):
+    """Fewer rows in use than the buffers hold, as where a graph is captured for a full batch: the used ones come out
+    as ever, the others stay untouched."""
+    lens = [n + 40 * (n > 0) for n in news]
+    c = Cache(35, lens, 2, 16, 128)
+    want = _check_attend(c, news, 8)
+    used = sum(news)
+    q = np.zeros((rows, 8, 128), np.float16)
+    q[:used] = (np.random.default_rng(2).standard_normal((used, 8, 128)) * 2).astype(np.float16)
+    out = torch.full((rows, 8, 128), 7.0, dtype=torch.float16, device="cuda")
+    tt.kv_attend(c.upload(), _dev(q), _dev(_starts(news)), rows // len(news), out, _workspace())
+    got = out.cpu().numpy()
+    assert np.all(got[used:] == 7)
+    # the split of the keys may differ with the rows' count: two fp16 roundings and those of the weights
+    assert np.all(np.abs(got[:used].astype(np.float64) - want) <= 2.0 ** -9 * np.abs(want) + 2.0 ** -8)
+
+
 @pytest.mark.parametrize("news", [(1,), (40,), (200,)])
 def test_attend_long_context(news):
     """Many pieces of one sequence, with the context's end inside a page."""
