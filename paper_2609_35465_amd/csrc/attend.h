@@ -532,12 +532,24 @@ __device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s
     return rows > a.few_most ? (rows + 32 * NW - 1) / (32 * NW) : 0;
 }
 
-// slots 0: no unit is cut
-template <int D, int NW, int KS>
-__device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
+// What a workgroup of units finds for itself: its row tile's sequence and rows.
+struct ManyUnit {
+    Span s;
+    int seq, row0;      // seq -1: none
+};
+
+// Every wave looks for itself, the sequences a lane each: first the plan, then
+// row tile `rank_of(plan)` of all.  slots 0: no unit is cut.
+template <int D, int NW, int KS, class F>
+__device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots, F rank_of, ManyUnit& unit) {
+    const int lane = threadIdx.x & 63;
+    auto span_at = [&](int i) {
+        return i < a.c.seqs ? span_of(a.starts, a.c.lens, a.rows, a.max_new, i) : Span{0, 0, 0, 0};
+    };
+    Span mine = span_at(lane);                     // of the first 64 sequences
     int row_tiles = 0, most = 0;
-    for (int i = threadIdx.x & 63; i < a.c.seqs; i += 64) {
-        const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, i);
+    for (int i0 = 0; i0 < a.c.seqs; i0 += 64) {
+        const Span s = i0 ? span_at(i0 + lane) : mine;
         const int t = many_row_tiles<NW>(a, s);
         const Reach r = reach_of(a, s);
         row_tiles += t;
@@ -547,26 +559,24 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots) {
     p.row_tiles = wave_all(Sum(), row_tiles);
     most = wave_all(Max(), most);
     p.splits = many_splits<D, NW, KS>(p.row_tiles * a.c.kv_heads, most, slots);
-    return p;
-}
-
-// the sequence of row tile `rank` of all, and its first one
-template <int NW>
-__device__ __forceinline__ void many_find(const AttendArgs& a, int rank, int& seq, int& first) {
-    const int lane = threadIdx.x & 63;
-    for (int i = 0, before = 0; i < a.c.seqs; i += 64) {
-        const int n = i + lane < a.c.seqs ? many_row_tiles<NW>(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i + lane)) : 0;
+    const int rank = rank_of(p);
+    unit.seq = -1;
+    if (rank < 0) return p;
+    for (int i0 = 0, before = 0; i0 < a.c.seqs; i0 += 64) {
+        if (i0) mine = span_at(i0 + lane);
+        const int n = many_row_tiles<NW>(a, mine);
         const int upto = wave_upto(Sum(), n) + before;
         const unsigned long long has = __ballot(upto > rank);
         if (has) {
             const int l = __builtin_ctzll(has);
-            seq = i + l;
-            first = __builtin_amdgcn_readlane(upto - n, l);
-            return;
+            unit.seq = i0 + l;
+            unit.row0 = (rank - lane_of(upto - n, l)) * 32 * NW;
+            unit.s = {lane_of(mine.row0, l), lane_of(mine.n, l), lane_of(mine.first, l), lane_of(mine.len, l)};
+            return p;
         }
-        before = __builtin_amdgcn_readlane(upto, 63);
+        before = lane_of(upto, 63);
     }
-    seq = first = -1;
+    return p;
 }
 
 // the first of a unit's tiles that piece `split` of it takes
@@ -606,16 +616,15 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     const int tid = threadIdx.x - team * kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     auto& kt = reinterpret_cast<ManyLds<D>*>(lds)[team].k;
     auto& vt = reinterpret_cast<ManyLds<D>*>(lds)[team].v;
-    const ManyPlan plan = many_plan<D, NW, KS>(a, slots);
     // the last row tiles first: those have the most keys
-    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, splits = plan.splits;
-    const int rank = plan.row_tiles - 1 - rest / splits, split = rest % splits;
-    if (rank < 0) return;
-    int seq, first;
-    many_find<NW>(a, rank, seq, first);
-    if (seq < 0) return;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int rows = s.n * a.group, row0 = (rank - first) * kRows;
+    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads;
+    ManyUnit unit;
+    const ManyPlan plan =
+        many_plan<D, NW, KS>(a, slots, [&](const ManyPlan& p) { return p.row_tiles - 1 - rest / p.splits; }, unit);
+    if (unit.seq < 0) return;
+    const int splits = plan.splits, split = rest % splits, seq = unit.seq, row0 = unit.row0;
+    const Span s = unit.s;
+    const int rows = s.n * a.group;
     const Reach reach = reach_of(a, s);
     const int token0 = s.first + row0 / a.group, token1 = s.first + (min(row0 + kRows, rows) - 1) / a.group;
     const int reach_end = min(token1 + 1, reach.end), reach_begin = a.window > 0 ? max(0, token0 - a.window + 1) & ~63 : 0;
@@ -915,16 +924,13 @@ template <int D, int NW, int KS>
 __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots, int blocks, JoinShape shape) {
     constexpr int kRows = 32 * NW, kParts = kRows / kJoinRows<D>;
     if (static_cast<int>(blockIdx.x) >= blocks) return attend_join<D>(a, blockIdx.x - blocks, shape);
-    const ManyPlan plan = many_plan<D, NW, KS>(a, slots);
-    if (plan.splits == 1) return;
     const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts, head = rest % a.c.kv_heads;
-    const int rank = plan.row_tiles - 1 - rest / a.c.kv_heads;
-    if (rank < 0) return;
-    int seq, first;
-    many_find<NW>(a, rank, seq, first);
-    if (seq < 0) return;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int row0 = (rank - first) * kRows, r = part * kJoinRows<D> + static_cast<int>(threadIdx.x) / (D / 4);
+    ManyUnit found;
+    const ManyPlan plan = many_plan<D, NW, KS>(
+        a, slots, [&](const ManyPlan& p) { return p.splits == 1 ? -1 : p.row_tiles - 1 - rest / a.c.kv_heads; }, found);
+    if (found.seq < 0) return;
+    const Span s = found.s;
+    const int row0 = found.row0, r = part * kJoinRows<D> + static_cast<int>(threadIdx.x) / (D / 4);
     if (row0 + r >= s.n * a.group) return;
     const float* unit = a.pieces +
                         (static_cast<size_t>(rest / a.c.kv_heads) * plan.splits * a.c.kv_heads + head) * kManySlot<D, NW>;
