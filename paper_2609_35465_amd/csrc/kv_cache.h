@@ -17,7 +17,12 @@
 // append: page_tokens' tokens of one head share a scale, so a workgroup takes
 // one page and head (keys and values apart), a wave each 16 tokens of it.
 // With old tokens in the page the scale can only grow: s' = max(s, amax/127),
-// and if it grows they are rounded again, rint(q s / s').
+// and if it grows they are rounded again, rint(q s / s').  A batch of single
+// tokens is a chain of dependent loads (span, page, its old tokens and scale), so
+// everything that does not depend on the page is loaded before it: 64 sequences
+// of 8 heads by 128, 40 q heads: 6.6 us, one sequence of 32 q heads 5.5 us.  Prompts are
+// bound by HBM: 4,096 tokens of 8 heads and 32 q heads by 128 from fp32, 145 MB,
+// 32.5 us, 4,450 GB/s (a large copy: 5,030).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -385,7 +390,7 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a) {
 // The last `count` tokens of every sequence as fp16, [seqs][count][kv_heads][D]
 // each for keys and values; zeros before a sequence's start.  A workgroup of 2 D
 // threads takes 16 tokens of a head, the first D threads its keys, the others its
-// values, which LDS turns.
+// values, which LDS turns.  4,096 tokens of 8 heads by 128: 7.7 us, 3,270 GB/s.
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvCache c, int count, int groups, uint16_t* k_out, uint16_t* v_out) {
     __shared__ __align__(16) _Float16 turned[kGroupTokens][D + 8];

