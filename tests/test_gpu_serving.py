@@ -458,6 +458,29 @@ def test_attend_unused_places_do_not_matter(news):
     assert np.array_equal(_check_attend(c, news, 4), first)
 
 
+@pytest.mark.parametrize("news", [(1, 1, 1), (40, 3, 1), (100, 80, 33)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_attend_not_finite_queries_stay_alone(news, bad):
+    """A q that is not finite makes its own output NaN and no other: the rest stay as far from the output without it
+    as two outputs within _check_attend's bound can be, whose |weight| |value| sums are at most the largest value."""
+    c = Cache(29, (170, 500, 3000), 2, 64, 128)
+    starts, rows = _starts(news), sum(news)
+    q = c.rng.standard_normal((rows, 8, c.dim)).astype(np.float16)
+    spoilt = q.copy()
+    mine = np.zeros((rows, 8), bool)
+    for row, head in ((0, 3), (rows - 1, 0)):
+        spoilt[row, head, 5] = bad
+        mine[row, head] = True
+    cache, outs = c.upload(), []
+    for x in (q, spoilt):
+        out = torch.zeros((rows, 8, c.dim), dtype=torch.float16, device="cuda")
+        tt.kv_attend(cache, _dev(x), _dev(starts), max(news), out, _workspace())
+        outs.append(out.cpu().numpy().astype(np.float64))
+    largest = max(float(np.abs(c.sequence(i)[1]).max()) for i in range(3))
+    assert np.isnan(outs[1][mine]).all()
+    assert np.abs(outs[1][~mine] - outs[0][~mine]).max() <= 2 * (2.5 * 2.0 ** -11 * largest + 2.0 ** -24)
+
+
 @pytest.mark.parametrize("news", [(1,), (100,)])
 @pytest.mark.parametrize("kind", ["large", "apart", "zero", "small"])
 def test_attend_scales(news, kind):
