@@ -78,7 +78,7 @@ struct Span {
 __device__ __forceinline__ Span span_of(const int* starts, const int* lens, int rows, int max_new, int seq) {
     Span s;
     s.row0 = min(max(starts[seq], 0), rows);
-    s.n = min(max(min(starts[seq + 1], rows) - s.row0, 0), max_new);
+    s.n = min(max(min(max(starts[seq + 1], 0), rows) - s.row0, 0), max_new);
     s.len = max(lens[seq], 0);
     s.first = s.len - s.n;   // below zero if the length does not hold the new tokens
     return s;

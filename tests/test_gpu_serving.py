@@ -412,6 +412,26 @@ def test_attend_rows_past_the_last_start(news, rows):
     assert np.all(np.abs(got[:used].astype(np.float64) - want) <= 2.0 ** -9 * np.abs(want) + 2.0 ** -8)
 
 
+@pytest.mark.parametrize("rows", [10, 100])
+@pytest.mark.parametrize("after", [-(1 << 31), -(1 << 31) + 1, -7, 0, 3, 1 << 30, (1 << 31) - 1])
+def test_attend_bad_starts_stay_in_the_arrays(rows, after):
+    """Starts outside [0, rows]: q and out lie between guard rows, which come out as they were, and the rows that the
+    starts do name are those of a call without the bad ones."""
+    c = Cache(36, [rows - 4, 8], 2, 16, 64, max_pages=32)
+    cache, guard = c.upload(), 128
+    q = torch.full((rows + 2 * guard, 4, 64), float("nan"), dtype=torch.float16, device="cuda")
+    q[guard:guard + rows] = _dev(c.rng.standard_normal((rows, 4, 64)).astype(np.float16))
+    outs = []
+    print(f"[attend bad starts] rows={rows} after={after}", flush=True)
+    for starts in ([0, rows, rows], [0, (1 << 31) - 1, after], [-(1 << 31), rows, after]):
+        wide = torch.full_like(q, 7.0)
+        tt.kv_attend(cache, q[guard:guard + rows], _dev(np.array(starts, np.int32)), rows, wide[guard:guard + rows],
+                     _workspace())
+        assert torch.all(wide[:guard] == 7) and torch.all(wide[guard + rows:] == 7)
+        outs.append(wide[guard:guard + rows])
+    assert torch.isfinite(outs[0]).all() and torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
 @pytest.mark.parametrize("news", [(1,), (40,), (200,)])
 def test_attend_long_context(news):
     """Many pieces of one sequence, with the context's end inside a page."""
