@@ -94,11 +94,23 @@ struct Reach {
     int begin, end;
 };
 
+// the first token that a row at `position` may see; one below zero sees none, and
+// any window may be taken from the others
+__device__ __forceinline__ int window_begin(const AttendArgs& a, int position) {
+    return a.window > 0 ? max(position, 0) - a.window + 1 : 0;
+}
+
+// a multiple of 64 at or below that token, and below `end` rounded up to one: a
+// length may lie far past the table, whose tokens alone are counted from here
+__device__ __forceinline__ int reach_begin_of(const AttendArgs& a, int position, int end) {
+    return min(max(0, window_begin(a, position)), max(end, 0) + 63) & ~63;
+}
+
 __device__ __forceinline__ Reach reach_of(const AttendArgs& a, const Span& s) {
     Reach r;
     const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
     r.end = static_cast<int>(min(static_cast<long long>(s.len), kept));
-    r.begin = a.window > 0 ? max(0, s.first - a.window + 1) & ~63 : 0;
+    r.begin = reach_begin_of(a, s.first, r.end);
     return r;
 }
 
@@ -342,7 +354,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             const bool there = row < rows;
             const int position = s.first + token;
             const int row_end = there ? min(position + 1, reach.end) : 0;
-            const int row_begin = a.window > 0 ? position - a.window + 1 : 0;
+            const int row_begin = window_begin(a, position);
             f16x8 q[D / 32];
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -644,7 +656,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     const int rows = s.n * a.group;
     const Reach reach = reach_of(a, s);
     const int token0 = s.first + row0 / a.group, token1 = s.first + (min(row0 + kRows, rows) - 1) / a.group;
-    const int reach_end = min(token1 + 1, reach.end), reach_begin = a.window > 0 ? max(0, token0 - a.window + 1) & ~63 : 0;
+    const int reach_end = min(token1 + 1, reach.end), reach_begin = reach_begin_of(a, token0, reach_end);
     const int unit_tiles = max(0, reach_end - reach_begin + kManyTile - 1) / kManyTile;
     const int tile0 = split_from(split, unit_tiles, splits), n = split_from(split + 1, unit_tiles, splits) - tile0;
     const int piece = reach_begin + tile0 * kManyTile, end = min(reach_end, piece + n * kManyTile);
@@ -657,10 +669,10 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     const int rtoken = row / a.group, h = head * a.group + row - rtoken * a.group;
     const bool there = row < rows;
     const int position = s.first + rtoken;
-    const int row_end = there ? min(position + 1, end) : 0, row_begin = a.window > 0 ? position - a.window + 1 : 0;
+    const int row_end = there ? min(position + 1, end) : 0, row_begin = window_begin(a, position);
     const int wfirst = s.first + wrow / a.group, wlast = s.first + (min(wrow + 32, rows) - 1) / a.group;
-    const int all_end = min(wfirst + 1, end), all_begin = a.window > 0 ? wlast - a.window + 1 : 0;
-    const int any_end = wrow < rows ? min(wlast + 1, end) : 0, any_begin = a.window > 0 ? wfirst - a.window + 1 : 0;
+    const int all_end = min(wfirst + 1, end), all_begin = window_begin(a, wlast);
+    const int any_end = wrow < rows ? min(wlast + 1, end) : 0, any_begin = window_begin(a, wfirst);
 
     f16x8 q[D / 16];
 #pragma unroll

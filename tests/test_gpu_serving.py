@@ -412,6 +412,28 @@ def test_attend_rows_past_the_last_start(news, rows):
     assert np.all(np.abs(got[:used].astype(np.float64) - want) <= 2.0 ** -9 * np.abs(want) + 2.0 ** -8)
 
 
+@pytest.mark.parametrize("news", [(1, 3), (10, 5), (100, 64)])
+@pytest.mark.parametrize("window", [1, 200, (1 << 31) - 1])
+def test_attend_windows_and_lengths_up_to_the_type_s_end(news, window):
+    """The largest window is none, also for rows before a sequence's start; of a length far past the table the tokens
+    in the table are seen, as far as the window reaches back to them."""
+    c = Cache(37, [480, 480], 2, 16, 64)
+    c.lens[:] = [news[0] // 2, news[1] - 2]
+    got = _check_attend(c, news, 4, window=window)
+    assert np.all(got[:news[0] - news[0] // 2] == 0)
+    c.lens[:] = 480
+    rows = sum(news)
+    q = _dev(np.random.default_rng(4).standard_normal((rows, 4, 64)).astype(np.float16))
+    all_seen, far = (torch.full_like(q, float("nan")) for _ in range(2))
+    cache = c.upload()
+    c.d[4].fill_(480 + max(news))
+    tt.kv_attend(cache, q, _dev(_starts(news)), max(news), all_seen, _workspace())
+    c.d[4].fill_((1 << 31) - 1)
+    print(f"[attend far lengths] news={news} window={window}", flush=True)
+    tt.kv_attend(cache, q, _dev(_starts(news)), max(news), far, _workspace(), window=window)
+    assert torch.equal(far, all_seen if window > 1 << 30 else torch.zeros_like(q))
+
+
 @pytest.mark.parametrize("rows", [10, 100])
 @pytest.mark.parametrize("after", [-(1 << 31), -(1 << 31) + 1, -7, 0, 3, 1 << 30, (1 << 31) - 1])
 def test_attend_bad_starts_stay_in_the_arrays(rows, after):
