@@ -683,7 +683,8 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     }
 
     // Pages and scales of kWindow tiles, a lane each (of 16 tokens or of a tile): this window's and the next's.
-    // A negative page is none; sg is the factor of the scores, lv log2 of the values' scale.
+    // A negative page is none, and page 0's scales, read in its place, are not used; sg is the factor of the scores, lv
+    // log2 of the values' scale.
     struct Window {
         int page;
         float sg, lv;
@@ -695,8 +696,9 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     };
     auto load_scales = [&](Window& w) {
         const f32x2 x = *reinterpret_cast<const f32x2*>(a.c.scales + 2 * (static_cast<size_t>(max(w.page, 0)) * a.c.kv_heads + head));
-        w.sg = fmaxf(x[0] * a.scale, 1e-30f);
-        w.lv = x[1] > 0.f ? __builtin_amdgcn_logf(x[1]) : kNoLog;
+        const bool none = w.page < 0;
+        w.sg = none ? 1e-30f : fmaxf(x[0] * a.scale, 1e-30f);
+        w.lv = !none && x[1] > 0.f ? __builtin_amdgcn_logf(x[1]) : kNoLog;
     };
     auto of_lane = [&](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
     // page of the tokens 16 g .. of tile j, which lies in the present window or the next

@@ -500,6 +500,24 @@ def test_attend_unused_places_do_not_matter(news):
     assert np.array_equal(_check_attend(c, news, 4), first)
 
 
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("news", [(1, 1, 1), (70, 33, 1), (81, 130, 7)])
+@pytest.mark.parametrize("scale", [1e30, np.inf, np.nan, 0.0])
+def test_attend_scales_of_other_pages_do_not_matter(page, news, scale):
+    """Scales of pages that are no sequence's, page 0 of the pool among them, at prompts' ends inside a tile and at
+    holes of the table: the outputs keep every bit."""
+    c = Cache(38, [81, 333, 215], 2, page, 128)
+    c.table[1:, 2] = -1
+    if (c.table == 0).any():                   # page 0 is left to no one: its sequence takes a spare one
+        c.table[c.table == 0] = np.setdiff1d(np.arange(len(c.k)), c.table)[0]
+    unused = np.setdiff1d(np.arange(len(c.k)), c.table)
+    assert unused[0] == 0
+    first = _check_attend(c, news, 4)
+    c.scales[unused] = scale
+    c.k[unused], c.v[unused] = 127, 127
+    assert np.array_equal(_check_attend(c, news, 4), first)
+
+
 @pytest.mark.parametrize("news", [(1, 1, 1), (40, 3, 1), (100, 80, 33)])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 def test_attend_not_finite_queries_stay_alone(news, bad):
