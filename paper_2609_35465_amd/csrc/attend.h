@@ -30,9 +30,21 @@ struct AttendArgs {
 };
 
 constexpr float kNoScore = -3e38f;   // a maximum over no score
-// A weight is 2^(s - m + 15) before it becomes fp16: the largest is 2^15, so
-// weights down to 2^-29 of it keep their 11 bits.  l carries the same factor.
+// The scale of a key's values goes into its weight's exponent: the second product
+// takes w = 2^(s + v - m + 15) in fp16, v = log2 of the scale and m the running
+// maximum of s + v over the keys that the row sees, and l = sum 2^(-v) w.  So the
+// largest product with a value decides what is rounded away, whatever the pages'
+// scales are, and pages that a row does not see have no part in it.  fp16 keeps 11
+// bits of weights down to 2^-29 of the largest where it is 2^15; attend_many_kernel
+// lets m stay behind by up to kSlack, and there it is 2^-21.
 constexpr float kWeightShift = 15.f;
+
+// v: bounds that an fp16 output cannot tell from scales beyond them (127 times 2^-40
+// is a 512th of its smallest step), so that neither w, l nor their quotient leaves
+// fp32's range while the output is in fp16's
+__device__ __forceinline__ float log_scale(float scale) {
+    return fminf(fmaxf(__builtin_amdgcn_logf(scale), -40.f), 125.f);
+}
 
 // four whole numbers of -128..127 as fp16, exactly: 1024 + (q + 128) is the
 // byte q ^ 0x80 below the exponent byte 0x64
@@ -161,7 +173,7 @@ struct FewPlan {
 
 template <int D>
 struct FewState {
-    float m, l, vref;
+    float m, l;
     f32x4 o[D / 16];
 };
 
@@ -216,9 +228,12 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(to_half8(k[2], k[3]), q[2 * c + 1], s[t], 0, 0, 0);
             }
         }
-        const float sg = b.ks * a.scale;
+        // the lane's 16 tokens lie in one page
+        const float sg = b.ks * a.scale, lv = log_scale(b.vs);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) s[t] *= sg;
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(s[t][i], sg, lv);
         const int mine = t0 + 16 * g;       // the lane's 16 tokens
         if (__any(!b.there || mine < row_begin || mine + 16 > row_end)) {
 #pragma unroll
@@ -235,26 +250,24 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
         const float m = fmaxf(st.m, over_groups(Larger(), top));
-        const float vref = fmaxf(st.vref, over_groups(Larger(), b.vs));
-        const float alpha = fast_exp2(st.m - m), beta = alpha * (st.vref / vref);
+        const float alpha = fast_exp2(st.m - m);
         st.l *= alpha;
-        if (__any(beta != 1.f)) {
+        if (__any(alpha != 1.f)) {
 #pragma unroll
-            for (f32x4& o : st.o) o *= beta;
+            for (f32x4& o : st.o) o *= alpha;
         }
         st.m = m;
-        st.vref = vref;
-        // the page's scale of the values goes into the weights, relative to the largest so far
-        const float rel = b.vs / vref;
         f16x8 p[2];
+        float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float w = fast_exp2(s[t][i] - (m - kWeightShift));
-                st.l += w;
-                p[t / 2][4 * (t % 2) + i] = static_cast<_Float16>(w * rel);
+                sum += w;
+                p[t / 2][4 * (t % 2) + i] = static_cast<_Float16>(w);
             }
+        st.l += sum * fast_exp2(-lv);
         Block n;
         if (next < stop) load(n, next, pk, pv);
 #pragma unroll
@@ -367,7 +380,6 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             FewState<D> st;
             st.m = kNoScore;
             st.l = 0.f;
-            st.vref = 1e-37f;
             for (f32x4& o : st.o) o = f32x4{0.f, 0.f, 0.f, 0.f};
             few_segment<D, kTile>(a, st, q, table, head, reach.begin + tile0 * kTile + wave * 64,
                                   min(reach.end, reach.begin + tile1 * kTile), row_begin, row_end);
@@ -379,7 +391,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
             }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d)
-                *reinterpret_cast<f32x4*>(&sums[wave][r][16 * d + 4 * g]) = st.o[d] * st.vref;
+                *reinterpret_cast<f32x4*>(&sums[wave][r][16 * d + 4 * g]) = st.o[d];
             __syncthreads();
             // the waves' sums joined, 4 dimensions a thread
             const bool whole = tile0 == 0 && tile1 == tiles;
@@ -524,13 +536,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinShap
 // P^T, a product of 16 tokens in the order 0-3, 8-11 | 4-7, 12-15; the values
 // are written to LDS in that order.
 //
-// The scale of a page's values enters through the exponent, 2^(s - m + 15 +
-// log2(scale / largest so far)), and leaves the sum l again once for 16 tokens.
-// m follows the maximum only when a score passes it by 2^kSlack or more.
+// m follows the maximum only when it is passed by kSlack or more.
 
 constexpr int kManyTile = 64;
 constexpr float kSlack = 8.f;
-constexpr float kNoLog = -1e30f;        // log2 of a scale of zero
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -684,7 +693,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
 
     // Pages and scales of kWindow tiles, a lane each (of 16 tokens or of a tile): this window's and the next's.
     // A negative page is none, and page 0's scales, read in its place, are not used; sg is the factor of the scores, lv
-    // log2 of the values' scale.
+    // log_scale of the values.
     struct Window {
         int page;
         float sg, lv;
@@ -698,7 +707,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
         const f32x2 x = *reinterpret_cast<const f32x2*>(a.c.scales + 2 * (static_cast<size_t>(max(w.page, 0)) * a.c.kv_heads + head));
         const bool none = w.page < 0;
         w.sg = none ? 1e-30f : fmaxf(x[0] * a.scale, 1e-30f);
-        w.lv = !none && x[1] > 0.f ? __builtin_amdgcn_logf(x[1]) : kNoLog;
+        w.lv = none ? 0.f : log_scale(x[1]);
     };
     auto of_lane = [&](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
     // page of the tokens 16 g .. of tile j, which lies in the present window or the next
@@ -765,7 +774,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
                 x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                     *reinterpret_cast<const f16x8*>(kt[b][2 * c + half][32 * t + (lane & 31)]), q[c], x[t], 0, 0, 0);
     };
-    float m = kNoScore, l = 0.f, lref = kNoLog;
+    float m = kNoScore, l = 0.f;
     if (n > 0) {
         load_pages(win, 0);
         load_scales(win);
@@ -804,19 +813,16 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
         __syncthreads();
         // a wave also goes through the tile before its first, for that one's scores
         if (t0 < any_end && t0 + kStep + kManyTile > any_begin) {
-            float sg[kGroups], rel[kGroups], lnew = lref;
+            float sg[kGroups], lv[kGroups];
             bool none[kGroups], holes = false;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int at = (j - window0) * kGroups + g;
                 sg[g] = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, win.sg), at));
-                rel[g] = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, win.lv), at));
+                lv[g] = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, win.lv), at));
                 none[g] = of_lane(win.page, at) < 0;
-                lnew = fmaxf(lnew, rel[g]);
                 holes |= none[g];
             }
-#pragma unroll
-            for (float& x : rel) x = x > kNoLog ? fmaxf(x - lnew, -100.f) : 0.f;
             if (holes || t0 < all_begin || t0 + kManyTile > all_end) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -827,30 +833,27 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
                     }
             }
             // exponents with the maximum so far, and what they say of the new one
-            const float from = m > kNoScore ? m : 0.f;
-            float top = kNoScore;
+            const float from = m > kNoScore ? m : 0.f, c0 = kWeightShift - kSlack - from;
+            float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float c = kWeightShift - kSlack + rel[ONE ? 0 : g] - from;
-                float x = -INFINITY;
+                const float c = c0 + lv[ONE ? 0 : g];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float e = __builtin_fmaf(cur[g / 2][8 * (g % 2) + i], sg[ONE ? 0 : g], c);
                     cur[g / 2][8 * (g % 2) + i] = e;
-                    x = fmaxf(x, e);
+                    top = fmaxf(top, e);
                 }
-                top = fmaxf(top, x - c);
             }
-            top = with_half(Larger(), top);
-            if (__any(top > m + kSlack) || lnew != lref) {
-                const float mnew = fmaxf(m, top), alpha = fast_exp2(m - mnew), beta = alpha * fast_exp2(lref - lnew);
+            top = with_half(Larger(), top) - c0;
+            if (__any(top > m + kSlack)) {
+                const float mnew = fmaxf(m, top), alpha = fast_exp2(m - mnew);
                 l *= alpha;
 #pragma unroll
-                for (f32x16& x : o) x *= beta;
+                for (f32x16& x : o) x *= alpha;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) cur[t] += from - mnew;
                 m = mnew;
-                lref = lnew;
             }
             __builtin_amdgcn_s_setprio(1);
             scores(ahead, b ^ 1);
@@ -864,7 +867,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
                     sum += w;
                     p[g][i] = static_cast<_Float16>(w);
                 }
-                l += sum * fast_exp2(-rel[ONE ? 0 : g]);
+                l += sum * fast_exp2(-lv[ONE ? 0 : g]);
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g)
@@ -898,21 +901,17 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
                 for (int i = 0; i < 16; ++i) sums[(16 * d + i) * kThreads] = o[d][i];
             stat[0] = m;
             stat[kThreads] = l;
-            stat[2 * kThreads] = lref;
         }
         __syncthreads();
         if (team == 1) return;
-        const float m1 = stat[0], l1 = stat[kThreads], lref1 = stat[2 * kThreads];
-        const float mnew = fmaxf(m, m1), lnew = fmaxf(lref, lref1);
+        const float m1 = stat[0], l1 = stat[kThreads], mnew = fmaxf(m, m1);
         const float f0 = fast_exp2(m - mnew), f1 = fast_exp2(m1 - mnew);
-        const float g0 = f0 * fast_exp2(lref - lnew), g1 = f1 * fast_exp2(lref1 - lnew);
         l = l * f0 + l1 * f1;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * g0 + sums[(16 * d + i) * kThreads] * g1;
+            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f0 + sums[(16 * d + i) * kThreads] * f1;
         m = mnew;
-        lref = lnew;
     }
     l = with_half(Sum(), l);
     if (!there) return;
@@ -923,17 +922,16 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
             slot[r] = m;
             slot[kRows + r] = l;
         }
-        const float unit = fast_exp2(fmaxf(lref, -120.f));
         float* out = slot + 2 * kRows + r * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *reinterpret_cast<f32x4*>(out + 32 * d + 2 * i) =
-                    f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * unit;
+                    f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         return;
     }
-    const float inv = l > 0.f ? fast_exp2(fmaxf(lref, -120.f)) / l : 0.f;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
     uint16_t* out = a.out + (s.row0 + rtoken) * a.out_stride + h * D + 4 * half;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)

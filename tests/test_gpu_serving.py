@@ -434,6 +434,65 @@ def test_attend_windows_and_lengths_up_to_the_type_s_end(news, window):
     assert torch.equal(far, all_seen if window > 1 << 30 else torch.zeros_like(q))
 
 
+def _attend_rows(c, q, news, window=0):
+    """out of rows q [rows, heads, dim] (fp16) over c, and the oracle's (out, size), one array each."""
+    out = torch.full(q.shape, float("nan"), dtype=torch.float16, device="cuda")
+    tt.kv_attend(c.upload(), _dev(q), _dev(_starts(news)), int(max(news)), out, _workspace(), window=window)
+    starts, want, size = _starts(news), [], []
+    for i, n in enumerate(news):
+        w, s = ref.attend(q[starts[i]:starts[i + 1]], *c.sequence(i), int(c.lens[i]) - int(n), c.dim ** -0.5, window)
+        want.append(w)
+        size.append(s)
+    return out.cpu().numpy().astype(np.float64), np.concatenate(want), np.concatenate(size)
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 16), (128, 32)])
+@pytest.mark.parametrize("news,lens", [((6, 1), (35, 30)), ((100, 64), (100, 64)), ((100, 1), (100, 31))])
+@pytest.mark.parametrize("window", [0, 9])
+@pytest.mark.parametrize("power", [26, 60])
+def test_attend_large_page_that_a_row_does_not_see(dim, page, news, lens, window, power):
+    """Values 2^26 and 2^60 times as large from token 32 on, in the tile that holds the earlier tokens too: a row
+    before them, or (with the window) past them, keeps its precision."""
+    c = Cache(39, lens, 2, page, dim)
+    for i in range(2):
+        if lens[i] > 32:
+            c.scales[c.table[i, 32 // page], :, 1] *= np.float32(2.0 ** power)
+    q = (c.rng.standard_normal((sum(news), 8, dim)) * 2).astype(np.float16)
+    got, want, size = _attend_rows(c, q, news, window)
+    position = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, news)])
+    apart = (position < 32) | ((position >= 32 + page + window) if window else False)
+    assert apart.any()
+    bound = 2.0 ** -11 * np.abs(want) + 1.5 * 2.0 ** -11 * size + 2.0 ** -24
+    worst = float((np.abs(got - want) / bound)[apart].max())
+    print(f"[attend large page] dim={dim} page={page} news={news} window={window} 2^{power} worst {worst:.3f}", flush=True)
+    assert worst <= 1.0
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("news,lens", [((1, 3), (100, 300)), ((100, 70), (100, 300))])
+@pytest.mark.parametrize("power", [26, 40])
+def test_attend_large_page_without_weight(dim, page, news, lens, power):
+    """A page of values 2^26 and 2^40 times as large whose keys lie against every q, so that its weights are below
+    2^-80 of the others' sum: the output is the others' mean to its last bits."""
+    c = Cache(40, lens, 2, page, dim)
+    for i in range(2):
+        p = c.table[i, 0]
+        c.scales[p, :, 1] *= np.float32(2.0 ** power)
+        c.k[p] = -127
+        c.scales[p, :, 0] = 8.0 * (128 / dim) ** 0.5 / 127
+    rng = c.rng
+    q = np.maximum(np.abs(rng.standard_normal((sum(news), 8, dim)) * 2), 0.5).astype(np.float16)
+    got, want, size = _attend_rows(c, q, news)
+    position = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, news)])
+    others = position >= page                 # the rows that see another page too
+    scores = -8.0 * (128 / dim) ** 0.5 * q.astype(np.float64).sum(-1) * dim ** -0.5 / np.log(2)
+    assert scores.max() < -130                 # the others' best are above -40: at most 2^-90 of them, times 2^40
+    bound = 2.0 ** -11 * np.abs(want) + 1.5 * 2.0 ** -11 * size + 2.0 ** -24
+    worst = float((np.abs(got - want) / bound)[others].max())
+    print(f"[attend page without weight] dim={dim} page={page} news={news} 2^{power} worst {worst:.3f}", flush=True)
+    assert worst <= 1.0
+
+
 @pytest.mark.parametrize("rows", [10, 100])
 @pytest.mark.parametrize("after", [-(1 << 31), -(1 << 31) + 1, -7, 0, 3, 1 << 30, (1 << 31) - 1])
 def test_attend_bad_starts_stay_in_the_arrays(rows, after):
