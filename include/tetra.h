@@ -506,7 +506,8 @@ int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint1
  * zeros where a row sees none.  Head h reads the cache's head
  * h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.  Scores, maxima
  * and sums are fp32, a weight is rounded to fp16 before it meets the values.
- * A q with a NaN or an infinity makes that row and head's output NaN, no other.
+ * A q with a NaN or an infinity makes that row and head's output NaN, no other
+ * (zeros where the row sees no token).
  *   q:   device fp16, q_stride elements from a row to the next, 16-byte aligned
  *   out: device fp16, out_stride elements apart, 16-byte aligned; rows of no
  *        sequence are not written

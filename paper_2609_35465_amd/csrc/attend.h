@@ -62,6 +62,13 @@ __device__ __forceinline__ f16x8 to_half8(uint32_t a, uint32_t b) {
     return f16x8{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
 }
 
+// eight of a row's q, turned if the scale is negative.  An infinity becomes NaN, or
+// it would leave weights of zero and no trace where all its scores are -inf.
+__device__ __forceinline__ f16x8 query8(u32x4 v, uint32_t flip) {
+    const f16x8 q = __builtin_bit_cast(f16x8, v ^ flip);
+    return q + q * static_cast<_Float16>(0.f);
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 struct Larger {
@@ -375,7 +382,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
                 if (there)
                     v = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + 64 * (c / 2) +
                                                         16 * g + 8 * (c % 2));
-                q[c] = __builtin_bit_cast(f16x8, v ^ a.q_flip);
+                q[c] = query8(v, a.q_flip);
             }
             FewState<D> st;
             st.m = kNoScore;
@@ -688,7 +695,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     for (int c = 0; c < D / 16; ++c) {
         u32x4 v = {0, 0, 0, 0};
         if (there) v = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + rtoken) * a.q_stride + h * D + 16 * c + 8 * half);
-        q[c] = __builtin_bit_cast(f16x8, v ^ a.q_flip);
+        q[c] = query8(v, a.q_flip);
     }
 
     // Pages and scales of kWindow tiles, a lane each (of 16 tokens or of a tile): this window's and the next's.

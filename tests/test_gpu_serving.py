@@ -493,6 +493,31 @@ def test_attend_large_page_without_weight(dim, page, news, lens, power):
     assert worst <= 1.0
 
 
+@pytest.mark.parametrize("news", [(5, 1), (100, 90)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("sign", [-1, 0, 1])
+def test_attend_not_finite_queries_over_keys_of_one_sign(news, bad, sign):
+    """Keys that all have one sign (or nothing) where q is not finite, so that every score may be -inf, from the row
+    that sees one key on: NaN all the same, and zeros where a row sees no key."""
+    c = Cache(41, news, 2, 16, 64)
+    c.k[..., 7] = sign * 90
+    starts, rows = _starts(news), sum(news)
+    q = c.rng.standard_normal((rows, 8, 64)).astype(np.float16)
+    spoilt = np.array([0, 2, news[0] - 1, news[0]])
+    q[spoilt, 5, 7] = bad
+    out = torch.zeros((rows, 8, 64), dtype=torch.float16, device="cuda")
+    cache = c.upload()
+    tt.kv_attend(cache, _dev(q), _dev(starts), max(news), out, _workspace())
+    got = out.cpu().numpy()
+    mine = np.zeros((rows, 8), bool)
+    mine[spoilt, 5] = True
+    assert np.isnan(got[mine]).all() and np.isfinite(got[~mine]).all()
+    c.d[4].copy_(torch.tensor([news[0] - 1, 0], dtype=torch.int32))      # the first rows see nothing now
+    tt.kv_attend(cache, _dev(q), _dev(starts), max(news), out, _workspace())
+    got = out.cpu().numpy()
+    assert np.all(got[0] == 0) and np.all(got[news[0]:] == 0) and np.isnan(got[2, 5]).all()
+
+
 @pytest.mark.parametrize("rows", [10, 100])
 @pytest.mark.parametrize("after", [-(1 << 31), -(1 << 31) + 1, -7, 0, 3, 1 << 30, (1 << 31) - 1])
 def test_attend_bad_starts_stay_in_the_arrays(rows, after):
