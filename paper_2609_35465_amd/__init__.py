@@ -396,7 +396,8 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
     f32, f16, i32 = _kinds or _kinds_of_torch()
     heads, dim, seqs = cache.sizes
     rows, kind, q_heads, q_stride, rope_rows = k.shape[0], k.dtype, 0, 0, 0
-    ok = (kind is f16 or kind is f32) and v.dtype is kind and starts.dtype is i32 and starts.numel() == seqs + 1
+    ok = ((kind is f16 or kind is f32) and v.dtype is kind and starts.dtype is i32 and starts.numel() == seqs + 1
+          and starts.is_contiguous())
     for w in (q_norm, k_norm):
         ok = ok and (w is None or (w.dtype is f32 and w.numel() == dim and w.is_contiguous()))
     if rope is not None:
@@ -445,7 +446,8 @@ def kv_attend(cache: KVCache, q, starts, max_new: int, out, workspace, scale: fl
     dim, seqs = cache.sizes[1:]
     rows = q.shape[0]
     heads = q.numel() // (rows * dim) if rows else 0
-    _expect(q.dtype is f16 and out.dtype is f16 and heads and starts.dtype is i32 and starts.numel() == seqs + 1, what)
+    _expect(q.dtype is f16 and out.dtype is f16 and heads and starts.dtype is i32 and starts.numel() == seqs + 1
+            and starts.is_contiguous(), what)
     _check(_call("tetra_kv_attend", ctypes.addressof(cache), q.data_ptr(), _row_stride(q, rows, heads, dim, what),
                  starts.data_ptr(), rows, max_new, heads, dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
                  _row_stride(out, rows, heads, dim, what), workspace.data_ptr(), workspace.numel(), _stream(stream)), what)

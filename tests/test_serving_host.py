@@ -154,6 +154,24 @@ def test_binding_refuses_other_shapes_and_types():
     refused(tt.sample, x.T, f, i, f, f, f, i, f)
 
 
+def _small_cache():
+    return tt.make_kv_cache(torch.zeros((4, 2, 32, 64), dtype=torch.int8), torch.zeros((4, 2, 2, 64, 16), dtype=torch.int8),
+                            torch.zeros((4, 2, 2)), torch.zeros((3, 5), dtype=torch.int32),
+                            torch.zeros(3, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("starts", [torch.zeros((4, 2), dtype=torch.int32)[:, 1], torch.zeros(1, dtype=torch.int32).expand(4)])
+def test_binding_refuses_starts_with_gaps(starts):
+    """A column of a wider tensor, or one number spread over all places: the kernels read `seqs + 1` numbers in line."""
+    cache, k = _small_cache(), torch.zeros((3, 2, 64))
+    out = torch.zeros((3, 4, 64)).half()
+    for call in (lambda: tt.kv_append(cache, None, k, k, starts, 1, None, None),
+                 lambda: tt.kv_attend(cache, out, starts, 1, out, torch.zeros(64, dtype=torch.uint8))):
+        with pytest.raises(tt.TetraError) as e:
+            call()
+        assert e.value.status == tt.EINVAL
+
+
 def test_oracle_sampling_is_the_plain_draw():
     """The whole weights leave the distribution as it is: against a float64 draw with the same random number, the
     tokens agree (a cumulative sum would have to lie within 1e-7 of u to differ)."""
