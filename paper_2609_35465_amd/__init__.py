@@ -403,8 +403,9 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
     if rope is not None:
         rope_rows = rope.numel() // dim
         ok = ok and rope.dtype is f32 and rope.shape[-1] == dim and rope.is_contiguous()
-    if q is not None:
-        size = q_out.numel() if q_out is not None else 0
+    ok = ok and (q is None) == (q_out is None)
+    if ok and q is not None:
+        size = q_out.numel()
         q_heads = size // (rows * dim) if rows else 0
         ok = ok and q.dtype is kind and size == q_heads * rows * dim and q_out.dtype is f16 and q_out.is_contiguous()
     _expect(ok, what)

@@ -172,6 +172,15 @@ def test_binding_refuses_starts_with_gaps(starts):
         assert e.value.status == tt.EINVAL
 
 
+def test_binding_refuses_q_and_q_out_apart():
+    """kv_append takes both or neither; one without the other is refused with its status."""
+    cache, k, starts = _small_cache(), torch.zeros((3, 2, 64)), torch.zeros(4, dtype=torch.int32)
+    for q, out in ((torch.zeros((3, 4, 64)), None), (None, torch.zeros((3, 4, 64)).half())):
+        with pytest.raises(tt.TetraError) as e:
+            tt.kv_append(cache, q, k, k, starts, 1, None, out)
+        assert e.value.status == tt.EINVAL
+
+
 def test_oracle_sampling_is_the_plain_draw():
     """The whole weights leave the distribution as it is: against a float64 draw with the same random number, the
     tokens agree (a cumulative sum would have to lie within 1e-7 of u to differ)."""
