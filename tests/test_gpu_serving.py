@@ -841,6 +841,33 @@ def test_sample_masks():
         assert got[2] == got[4] == -1 and got[1] == n - 1
 
 
+@pytest.mark.parametrize("vocab", [524289, (1 << 22) - 77, 1 << 22])
+def test_sample_up_to_the_largest_vocabulary(vocab):
+    """More tiles than the last kernel has threads, and the most LDS that it asks for; the row's end inside a tile."""
+    rng = np.random.default_rng(vocab)
+    x = (rng.standard_normal((6, vocab)) * 2.5).astype(np.float32)
+    x[5, -1] = 30
+    print(f"[sample large] vocab={vocab}", flush=True)
+    got = _check_sample(x, [1.0, 0.7, 1.0, 0.8, 0.0, 1.0], [0, 50, 0, 3000, 0, 0], [1.0, 0.9, 0.9, 0.99, 1.0, 0.5],
+                        [0.0, 0.01, 0.0, 0.0, 0.0, 0.0], np.array([0.999, 0.3, 0.7, 0.5, 0.0, 0.9], np.float32))
+    assert got[5] == vocab - 1
+
+
+@pytest.mark.parametrize("equal", [1000, 1500, 16384, 16385, 40000])
+def test_sample_many_equal_logits_at_the_cut(equal):
+    """As many candidates as are sorted at once, as the row's list holds and more, for a top-k that goes by groups, one
+    that goes by bins, and a top-p alone."""
+    rng = np.random.default_rng(equal)
+    n = 60000
+    x = (rng.standard_normal((8, n)) * 0.5 - 8).astype(np.float32)
+    for r in range(8):
+        x[r, rng.choice(n, equal, replace=False)] = 2.5
+        x[r, rng.choice(n, 5, replace=False)] = 3.0
+    print(f"[sample equal] {equal}", flush=True)
+    _check_sample(x, 1.0, [50, 50, 512, 600, 600, 0, 0, 30000], [1.0, 0.5, 0.99, 1.0, 0.3, 0.5, 0.01, 0.9],
+                  [0.0, 0.0, 0.1, 0.0, 0.7, 0.0, 0.0, 0.0], rng.random(8))
+
+
 def test_sample_ends_of_u():
     rng = np.random.default_rng(17)
     x = rng.standard_normal((4, 2000)).astype(np.float32)
