@@ -481,7 +481,7 @@ typedef struct {
  *   starts:  device int32 [seqs + 1], rising from 0 to `rows` at most (what
  *            lies outside is ignored)
  *   max_new: at least the largest count of new rows of a sequence (rows past it
- *            are ignored), 1..rows
+ *            are ignored, those before it keep their positions), 1..rows
  * Two sequences of a call must not append to the same page.  No workspace.
  * Asynchronous; TETRA_EINVAL / TETRA_EALIGN / TETRA_EUNSUPPORTED before any
  * launch, TETRA_EDEVICE at launch.

@@ -75,20 +75,27 @@ struct Span {
     int first, len;  // their tokens first .. len - 1
 };
 
-__device__ __forceinline__ Span span_of(const int* starts, const int* lens, int rows, int max_new, int seq) {
+// from the starts of the sequence and of the next, and its length.  The rows past
+// max_new are the last ones, so the others' tokens end before the length there.
+__device__ __forceinline__ Span span_between(int start, int next, int len, int rows, int max_new) {
     Span s;
-    s.row0 = min(max(starts[seq], 0), rows);
-    s.n = min(max(min(max(starts[seq + 1], 0), rows) - s.row0, 0), max_new);
-    s.len = max(lens[seq], 0);
-    s.first = s.len - s.n;   // below zero if the length does not hold the new tokens
+    s.row0 = min(max(start, 0), rows);
+    const int all = max(min(max(next, 0), rows) - s.row0, 0);
+    s.n = min(all, max_new);
+    s.first = max(len, 0) - all;   // below zero if the length does not hold the new tokens
+    s.len = max(s.first + s.n, 0);
     return s;
+}
+
+__device__ __forceinline__ Span span_of(const int* starts, const int* lens, int rows, int max_new, int seq) {
+    return span_between(starts[seq], starts[seq + 1], lens[seq], rows, max_new);
 }
 
 // The sequence that holds place x, and its span: the first one with base(start of
 // the next, its number) above x.  Each lane loads a sequence, all at once; x and
 // the result are uniform in the wave.
 struct Place {
-    int seq, start;    // seq -1: none; starts[seq]
+    int seq, start;    // seq -1: none; starts[seq], clamped
     Span s;
 };
 
@@ -111,10 +118,8 @@ __device__ __forceinline__ Place locate(const int* starts, const int* lens, int 
         if (!has) continue;
         const int l = __builtin_ctzll(has);
         p.seq = i0 + l;
-        p.start = p.s.row0 = __builtin_amdgcn_readlane(a, l);
-        p.s.n = min(max(__builtin_amdgcn_readlane(b, l) - p.start, 0), max_new);
-        p.s.len = max(__builtin_amdgcn_readlane(len, l), 0);
-        p.s.first = p.s.len - p.s.n;
+        p.start = __builtin_amdgcn_readlane(a, l);
+        p.s = span_between(p.start, __builtin_amdgcn_readlane(b, l), __builtin_amdgcn_readlane(len, l), rows, max_new);
         break;
     }
     return p;

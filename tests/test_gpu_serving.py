@@ -518,6 +518,44 @@ def test_attend_not_finite_queries_over_keys_of_one_sign(news, bad, sign):
     assert np.all(got[0] == 0) and np.all(got[news[0]:] == 0) and np.isnan(got[2, 5]).all()
 
 
+@pytest.mark.parametrize("news,most", [((3, 1), 1), ((5, 9), 4), ((100, 30, 2), 40), ((90, 120), 100)])
+def test_rows_past_max_new_are_ignored(news, most):
+    """Sequences of more rows than max_new: the rows before it are appended and attend at the positions that `starts`
+    and the lengths give them, as in a call that takes all rows; the rows past it leave nothing."""
+    lens = [n + 37 * i + 5 for i, n in enumerate(news)]
+    c, rows = Cache(42, lens, 2, 16, 64), sum(news)
+    rope, starts = tt.rope_table(max(lens), 64), _dev(_starts(news))
+    q, k, v = (_dev(c.rng.standard_normal((rows, n, 64)).astype(np.float32)) for n in (4, 2, 2))
+    taken = np.concatenate([np.arange(n) < most for n in news])
+    print(f"[past max_new] news={news} max_new={most}", flush=True)
+    got = []
+    for m in (max(news), most):
+        cache = c.upload()
+        turned, out = (torch.full((rows, 4, 64), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+        tt.kv_append(cache, q, k, v, starts, m, rope, turned)
+        pool = c.download()
+        tt.kv_attend(c.upload(), turned, starts, m, out, _workspace())
+        got.append((turned.cpu().numpy(), out.cpu().numpy(), pool))
+    (turned, out, pool), (turned1, out1, pool1) = got
+    assert np.array_equal(turned1[taken], turned[taken]) and np.all(turned1[~taken] == 7) and np.all(out1[~taken] == 7)
+    # the split of the keys may differ with max_new: two fp16 roundings and those of the weights
+    assert np.all(np.abs(out1[taken].astype(np.float64) - out[taken]) <= 2.0 ** -9 * np.abs(out[taken]) + 2.0 ** -8)
+    for i, n in enumerate(news):
+        first, end = lens[i] - n, lens[i] - n + min(n, most)
+        for j in range(-(-lens[i] // 16)):
+            page, lo, hi = c.table[i, j], min(16, max(0, first - 16 * j)), min(16, max(0, end - 16 * j))
+            whole = 16 * j + 16 <= end                  # no ignored row lies in the page
+            assert np.array_equal(pool1[0][page, :, hi:], c.k[page, :, hi:])
+            if whole or hi <= lo:
+                want = pool if whole else (c.k, c.v, c.scales)
+                assert all(np.array_equal(a[page], b[page]) for a, b in zip(pool1, want))
+            else:                                       # its scale may be below that of the whole call
+                now = ref.page_tokens_of(*pool1, page, 0)[:, lo:hi]
+                all_rows = ref.page_tokens_of(*pool, page, 0)[:, lo:hi]
+                unit = pool[2][page, :, 0].astype(np.float64)[:, None, None]
+                assert np.all(np.abs(now - all_rows) <= 1.001 * unit)
+
+
 @pytest.mark.parametrize("rows", [10, 100])
 @pytest.mark.parametrize("after", [-(1 << 31), -(1 << 31) + 1, -7, 0, 3, 1 << 30, (1 << 31) - 1])
 def test_attend_bad_starts_stay_in_the_arrays(rows, after):
