@@ -505,7 +505,9 @@ int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint1
  *   out = sum_j exp(scale q . k_j) v_j / sum_j exp(scale q . k_j),
  * zeros where a row sees none.  Head h reads the cache's head
  * h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.  Scores, maxima
- * and sums are fp32, a weight is rounded to fp16 before it meets the values.
+ * and sums are fp32; a weight times its page's value scale is rounded to fp16
+ * before it meets the values (11 bits down to 2^-21 of the row's largest such
+ * product; pages that the row does not see have no part in it).
  * A q with a NaN or an infinity makes that row and head's output NaN, no other
  * (zeros where the row sees no token).
  *   q:   device fp16, q_stride elements from a row to the next, 16-byte aligned

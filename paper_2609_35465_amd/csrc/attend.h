@@ -37,6 +37,13 @@ constexpr float kNoScore = -3e38f;   // a maximum over no score
 // scales are, and pages that a row does not see have no part in it.  fp16 keeps 11
 // bits of weights down to 2^-29 of the largest where it is 2^15; attend_many_kernel
 // lets m stay behind by up to kSlack, and there it is 2^-21.
+//
+// The matrix cores take fp16 against the values, which are exact in it; a weight's
+// rounding, 2^-12 at most, takes the output's distance from 64 bits from 2.1e-4 of
+// its norm (that of fp16 outputs alone) to 2.2e-4 (few rows, whose largest weight is
+// exact) and 2.7e-4.  A second product with what the rounding leaves of the weights
+// gives 2.1e-4 and took 4,096 tokens from 165 to 221 us, 64 single tokens from 49.3
+// to 50.8.
 constexpr float kWeightShift = 15.f;
 
 // v: bounds that an fp16 output cannot tell from scales beyond them (127 times 2^-40
@@ -89,9 +96,9 @@ __device__ __forceinline__ float over_groups(F f, float v) { return with_half(f,
 // itself).  Of a unit that spans several workgroups each stores its part, and
 // a second kernel joins them.
 //
-// Measured: one sequence of 131,072 tokens, 8 heads of 128: 55 us, 4,850 GB/s of
+// Measured: one sequence of 131,072 tokens, 8 heads of 128: 55 us, 4,890 GB/s of
 // keys and values (a large copy reaches 5,030 here), and 6 to 7 us for the join;
-// 64 sequences of up to 4,096 tokens, 182 MB: 43 us, 4,190 GB/s, and 5 us.  One
+// 64 sequences of up to 4,096 tokens, 182 MB: 43 us, 4,230 GB/s, and 5 us.  One
 // of 203 tokens: 6 us, the way through memory four times over (the spans, the
 // page table, the keys, the weighted values) and no bandwidth to speak of.
 //
@@ -527,11 +534,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinShap
 // the next are under way, and keys two tiles and values one tile further go to
 // LDS, with those after them on their way from memory.
 //
-// Measured, 32 heads over 8 of 128: 4,096 tokens from the start 155 us, 885
+// Measured, 32 heads over 8 of 128: 4,096 tokens from the start 154 us, 890
 // TFLOP/s of the products that the mask leaves (a library product of 8,192^3 in
-// fp16 reaches 1,170); 16,384 tokens 994.  There the matrix cores are busy 42 % of
-// the cycles, the vector units 52 %, without a bank conflict in LDS.  Halving the
-// reads from LDS would gain 10 %, no conversion to fp16 12 %, no exponentials 2 %.
+// fp16 reaches 1,170); 16,384 tokens 2,154 us, 1,021.  Of 4,096 the matrix cores are
+// busy 42 % of the cycles, the vector units 51 %, without a bank conflict in LDS.
+// Heads of 64: 4,096 tokens 109 us, 630 TFLOP/s, vector units 62 %, matrix cores
+// 30 %: 86 % of the vector units' work for half the products.  Of heads of 128,
+// halving the reads from LDS would gain 10 %, no conversion to fp16 12 %, no
+// exponentials 2 %.
 // The two halves of a workgroup in opposite phases (products against weights, two
 // barriers a tile) took 167 us at any depth of reads ahead; l as a product of the
 // fp16 weights is wrong where pages' scales lie far apart, as it has the small
@@ -560,7 +570,7 @@ struct ManyPlan {
 // their keys where that pays: a step of KS tiles takes a workgroup 1.75 us, a
 // piece's sums on their way through memory D NW / 16384 us (all pieces' together),
 // the join's launch 6 us.  Measured (one team of 128 rows, 32 heads of 128, us):
-// 203 tokens after 3,893 105 whole and 41 in 8 pieces, 100 after 900 34 and 23 in
+// 203 tokens after 3,893 101 whole and 39 in 8 pieces, 100 after 900 32 and 23 in
 // 4; but 1,024 from the start 35 whole and 42 in 2, 512 from the start 22 and 27.
 template <int D, int NW, int KS>
 __host__ __device__ __forceinline__ int many_splits(int units, int tiles, int slots) {

@@ -592,7 +592,9 @@ __global__ __launch_bounds__(kTokenThreads) void sample_token_kernel(SampleArgs 
             if (mine && w >= r.min_weight)
                 atomicAdd(&sums[static_cast<uint32_t>(~place) / kSampleTile], static_cast<unsigned long long>(w));
         } else {
-            // many candidates (logits next to each other): bit by bit, from the list or from the row
+            // many candidates (logits next to each other): bit by bit, from the list or from the row.  Of 151,936
+            // logits, 2,000 equal ones and a top-k of 50: 107 us for one row, 130 for 64; all within 0.1: 64 passes over
+            // the row for each filter, 3.9 ms for one and 5.4 ms for 64 rows of top-p, 6.3 and 9.2 with a top-k too
             const bool from_list = listed <= kSampleList;
             const int n = from_list ? listed : a.vocab;
             const int group_bin = by_groups ? space->group_bin : 0;

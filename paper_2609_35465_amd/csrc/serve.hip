@@ -86,9 +86,12 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
     const long long most_tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
     const long long few_groups = static_cast<long long>(cus) * kFewGroupsPerCU;
     // attend_few_kernel reads the keys once for 16 rows.  Up to there it is ahead (64 sequences of 1,000 tokens, 8
-    // heads by 16 rows: 44 us against 64); with several row tiles only where few sequences leave the other kernel
-    // short of units (32 rows: 1 sequence of 4,096 14 us against 22, 8 of them 37 and 37, 32 of 1,000 43 and 36;
-    // 64 rows: 17 and 24, 58 and 43, 72 and 34).
+    // heads by 16 rows: 33 us against 59); with several row tiles only where few sequences leave the other kernel
+    // short of units (32 rows: 1 sequence of 4,096 13 us against 22, 8 of them 33 and 33, 32 of 1,000 31 and 27;
+    // 64 rows: 16 and 23, 51 and 35, 52 and 29).  Of contexts that one tile holds it also takes prompts whose row
+    // tiles are one round of the chip: one short loop and no join (203 tokens of 40 heads over 8 of 128 9.8 us against
+    // 15.7, 64 tokens 6.7 and 12.7, 8 times 20 after 183 11 and 15, 8 times 64 of 16 heads of 64 6.1 and 9.0).  What a
+    // context may be is told by the table's width, for the host does not know the lengths.
     const int few_rows = static_cast<int>(std::min<long long>(64, std::max<long long>(16, 2048 / (static_cast<long long>(a.c.seqs) * a.c.kv_heads))));
     const bool all_few = most <= few_rows || (tiles == 1 && most_tiles * a.c.kv_heads * a.c.seqs <= few_groups);
     a.few_most = static_cast<int>(all_few ? most : few_rows);
@@ -104,8 +107,8 @@ AttendPlan attend_plan(tetra_dev::AttendArgs& a, int cus) {
         // where they are one round of the chip, or two rounds of long prompts from the start, whose short units even out.
         // 256 rows for more: a tile is turned into fp16 for twice as many.  Of batches that may have few-row sequences,
         // 128 rows with one team up to two rounds, since those run beside it.  Measured (128 rows with one team, with two,
-        // 256 rows; heads of 128, us): 1,024 tokens of 32 heads 36, 32, 43; 2,048 73, 62, 74; 2,800 -, 107, 96; 8 x 203
-        // tokens of 40 heads after 1,797 84, 104, 86; 2 x 500 from the start 25, 30, 28.
+        // 256 rows; heads of 128, us): 1,024 tokens of 32 heads 34, 29, 41; 2,048 68, 61, 72; 2,800 93, 105, 95; 8 x 203
+        // tokens of 40 heads after 1,797 85, 92, 79; 2 x 500 of 32 from the start 22, 20, 25.
         p.waves = 8;
         if (mixed ? units4 <= 2 * cus : units4 <= cus || (units4 <= 2 * cus && a.max_new >= 1024)) p.waves = 4;
         p.teams = p.waves == 4 && !mixed ? 2 : 1;

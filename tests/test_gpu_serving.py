@@ -887,7 +887,7 @@ def test_sample_up_to_the_largest_vocabulary(vocab):
     x[5, -1] = 30
     print(f"[sample large] vocab={vocab}", flush=True)
     got = _check_sample(x, [1.0, 0.7, 1.0, 0.8, 0.0, 1.0], [0, 50, 0, 3000, 0, 0], [1.0, 0.9, 0.9, 0.99, 1.0, 0.5],
-                        [0.0, 0.01, 0.0, 0.0, 0.0, 0.0], np.array([0.999, 0.3, 0.7, 0.5, 0.0, 0.9], np.float32))
+                        [0.0, 0.01, 0.0, 0.0, 0.0, 0.0], [0.999, 0.3, 0.7, 0.5, 0.0, 0.9])
     assert got[5] == vocab - 1
 
 
