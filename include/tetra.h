@@ -560,6 +560,134 @@ int tetra_sample(const float* logits, long long stride, int rows, int vocab, con
  * rows < 1 or vocab is out of range). */
 size_t tetra_sample_workspace_bytes(int rows, int vocab);
 
+/*
+ * tetra_kv_append with the rotation's positions moved: the rows of sequence s
+ * are turned as tokens shifts[s] places further on (shifts: device int32
+ * [seqs], 0..2^30 - 1, what lies outside is clamped).  For sequences that
+ * tetra_kv_evict took `shifts` tokens from: their new tokens go on counting
+ * from where they were, while the cache's places close up.
+ */
+int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, const int* shifts,
+                       int rows, int max_new, hipStream_t stream);
+
+/*
+ * tetra_kv_attend for a batch in which groups of sequences begin with the same
+ * pages (a system prompt, a document, several answers to one prompt): the
+ * pages that a group shares are read once for all of its rows.
+ * Group g is the sequences groups[g] .. groups[g + 1] - 1; their first
+ * shared[g] tokens lie in the same pages, which all their tables name (of a
+ * page that shared[g] ends inside, nothing counts as shared).  Sequences of
+ * no group, those whose new rows begin before the shared tokens' end and those
+ * without rows are served as by tetra_kv_attend.  The result is that of
+ * tetra_kv_attend without a window, up to the order in which sums are rounded.
+ *   groups: device int32 [num_groups + 1], rising, 0..seqs
+ *   shared: device int32 [num_groups]
+ *   workspace: as for tetra_kv_attend, at least
+ *        tetra_kv_attend_shared_workspace_bytes()
+ * The result does not change from run to run.  Asynchronous; errors as for
+ * tetra_kv_attend, TETRA_EINVAL also for num_groups < 1 or > seqs.
+ */
+int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                           int max_new, int q_heads, float scale, const int* groups, const int* shared, int num_groups,
+                           uint16_t* out, long long out_stride, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* Workspace bytes of tetra_kv_attend_shared on the current device (host only;
+ * 0 when the device cannot be queried). */
+size_t tetra_kv_attend_shared_workspace_bytes(void);
+
+/*
+ * The attention weight that cached tokens get from the rows of a call (rows,
+ * q, scale and window as for tetra_kv_attend), added to what they had:
+ *   mass_out[s][h][j] = decay mass[s][h][j] + sum over the rows i of sequence s
+ *       that see token j, and the q heads of cache head h, of
+ *       exp(s_ij) / sum over the tokens t that row i sees of exp(s_it)
+ * for the tokens j < lens[s]; other places are not written.  Tokens of the
+ * rows themselves have no past: mass is not read there.  Sequences without
+ * rows keep what they have (mass_out = mass).  Rows are a sequence's last
+ * tokens, so a prompt can be weighed by its last few rows alone.  A q with a
+ * NaN or an infinity makes the weights that its row gives NaN.
+ *   mass:     device fp32 [seqs][kv_heads][mass_tokens], or NULL: all 0
+ *   mass_out: the same, may be mass itself; tokens from mass_tokens on have no
+ *             place in either
+ *   decay:    0..1
+ *   workspace: as for tetra_kv_attend, at least
+ *             tetra_kv_weigh_workspace_bytes(cache, rows, q_heads)
+ * Sums are fp32 of fp32 weights, in an order that the sizes fix: the result does not
+ * change from run to run.  Asynchronous; errors as for tetra_kv_attend.
+ */
+int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                   int max_new, int q_heads, float scale, int window, const float* mass, float* mass_out,
+                   int mass_tokens, float decay, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of tetra_kv_weigh (host only; only the cache's sizes are
+ * looked at; 0 if they are out of range or the device cannot be queried). */
+size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int q_heads);
+
+/*
+ * Thins out a cache: of every sequence and cache head the tokens of most
+ * weight, and the last ones, go in their order into the pages of another.
+ * With n = from->lens[s] tokens and b = min(to->lens[s], n) to keep, the last
+ * r = min(recent, b) stay, and of the n - r before them the b - r of the
+ * largest mass (equal ones: the first; NaN counts as -inf).  Heads choose for
+ * themselves, so place i of two heads need not be the same token.  A new page's
+ * scale is the largest of the pages' that its tokens come from; tokens of that
+ * scale stay as they are, others are rounded again, rint(q * scale / new).
+ *   from: the cache as it is.  to: pages for what is kept, of the same pool or
+ *         another: kv_heads, head_dim, page_tokens and seqs are the same, lens
+ *         holds the tokens to keep.  A page that `to` names for its first
+ *         lens[s] tokens must not be one of `from`'s tokens, nor named twice.
+ *   mass, mass_out: device fp32 [seqs][kv_heads][mass_tokens], and
+ *         [seqs][kv_heads][out_tokens]: what the kept tokens have, by their new
+ *         places (NULL: not wanted); places past b are not written.  Tokens
+ *         past mass_tokens count as 0, and kept ones past out_tokens have no
+ *         place.  mass_out is not mass.
+ *   recent: 0 or more
+ *   workspace: as for tetra_kv_attend, at least
+ *         tetra_kv_evict_workspace_bytes(from, to)
+ * Tokens without a page go in as zeros, and kept tokens that `to` has no page
+ * for are dropped.  Asynchronous; errors as for tetra_kv_append.
+ */
+int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const float* mass, int mass_tokens, int recent,
+                   float* mass_out, int out_tokens, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of tetra_kv_evict (host only; only the caches' sizes are
+ * looked at; 0 if they are out of range). */
+size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to);
+
+/*
+ * Log probabilities of given tokens under rows of logits, the rows' entropy
+ * and their likeliest tokens.  With T the row's temperature, m its largest
+ * logit, t_j = (x_j - m) / T and l = sum_j exp(t_j):
+ *   out[i][g]    = t_j - ln l for the token j = tokens[i][g] (-inf for a number
+ *                  outside 0..vocab - 1)
+ *   entropy[i]   = ln l - sum_j exp(t_j) t_j / l, in nats
+ *   top_tokens[i], top_out[i]: the `top` largest logits' tokens by falling
+ *                  logit (equal ones: the lowest index first) and their log
+ *                  probabilities; -1 and -inf where fewer are above -inf
+ * NaN counts as -inf; logits of +inf share all of the probability; a row of
+ * nothing but -inf gives -inf, an entropy of 0 and no tokens.
+ *   logits: device fp32 (half 0) or fp16 (half 1), `stride` elements from a row
+ *           to the next
+ *   temperature: device fp32 [rows], or NULL for 1; T <= 0 and NaN (rows that
+ *           are sampled greedily) count as 1
+ *   tokens: device int32 [rows][given], out: fp32 the same (given 0: NULL)
+ *   entropy: device fp32 [rows], or NULL
+ *   top_tokens, top_out: device int32 and fp32 [rows][top], top 0..64 (0: NULL)
+ *   workspace: as for tetra_kv_attend, at least
+ *           tetra_log_probs_workspace_bytes(rows, vocab, top)
+ * Sums are fp32; the result does not change from run to run.  vocab is at most
+ * 2^22.  Asynchronous; TETRA_EINVAL / TETRA_EALIGN / TETRA_EDEVICE as for
+ * tetra_sample.
+ */
+int tetra_log_probs(const void* logits, int half, long long stride, int rows, int vocab, const float* temperature,
+                    const int* tokens, int given, float* out, float* entropy, int top, int* top_tokens, float* top_out,
+                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of tetra_log_probs for these sizes (host only; 0 if they are
+ * out of range or the device cannot be queried). */
+size_t tetra_log_probs_workspace_bytes(int rows, int vocab, int top);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ TABLE_BLOB_BYTES = 18824
 MAX_BATCH = 8
 MAX_GROUP = 32
 MAX_PHASES = 16
+MAX_TOP = 64                       # alternatives of log_probs
 ENCODE_MAX_RADIUS = 25.0
 ENCODE_RADII = (13.0, 15.0)        # trial radii of the encoder: the best integer pair on Gaussian blocks
 
@@ -56,6 +57,15 @@ _SIGNATURES = {
     "tetra_kv_attend_workspace_bytes": (_sz, []),
     "tetra_sample": (_int, [_vp, _i64, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "tetra_sample_workspace_bytes": (_sz, [_int, _int]),
+    "tetra_kv_append_at": (_int, [_vp, _vp, _vp, _vp, _int, _int, _vp]),
+    "tetra_kv_attend_shared": (_int, [_vp, _vp, _i64, _vp, _int, _int, _int, _f32, _vp, _vp, _int, _vp, _i64, _vp, _sz, _vp]),
+    "tetra_kv_attend_shared_workspace_bytes": (_sz, []),
+    "tetra_kv_weigh": (_int, [_vp, _vp, _i64, _vp, _int, _int, _int, _f32, _int, _vp, _vp, _int, _f32, _vp, _sz, _vp]),
+    "tetra_kv_weigh_workspace_bytes": (_sz, [_vp, _int, _int]),
+    "tetra_kv_evict": (_int, [_vp, _vp, _vp, _int, _int, _vp, _int, _vp, _sz, _vp]),
+    "tetra_kv_evict_workspace_bytes": (_sz, [_vp, _vp]),
+    "tetra_log_probs": (_int, [_vp, _int, _i64, _int, _int, _vp, _vp, _int, _vp, _vp, _int, _vp, _vp, _vp, _sz, _vp]),
+    "tetra_log_probs_workspace_bytes": (_sz, [_int, _int, _int]),
     "tetra_encode": (_int, [_vp, _vp, _sz, ctypes.c_double, ctypes.c_double, _vp, _vp]),
 }
 EXPORTED = tuple(_SIGNATURES)
@@ -387,11 +397,13 @@ def _row_stride(t, rows, heads, dim, what):
 
 
 def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm=None, k_norm=None,
-              eps: float = 1e-6, stream=None):
+              eps: float = 1e-6, stream=None, shifts=None):
     """Appends the rows k, v [rows, kv_heads, head_dim] (fp32 or fp16; rows starts[s] .. starts[s + 1] - 1
     are sequence s's last tokens) to the cache, keys normed (k_norm fp32 [head_dim], optional) and rotated
     (rope from rope_table(), or None); q [rows, q_heads, head_dim] goes the same way into q_out (fp16,
-    contiguous).  q and q_out may be None.  max_new: at least the largest count of rows of a sequence."""
+    contiguous).  q and q_out may be None.  max_new: at least the largest count of rows of a sequence.
+    shifts (int32 [seqs], optional): how many places further on each sequence's rows are turned, for sequences
+    that kv_evict took so many tokens from."""
     what = "tetra_kv_append"
     f32, f16, i32 = _kinds or _kinds_of_torch()
     heads, dim, seqs = cache.sizes
@@ -404,6 +416,8 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
         rope_rows = rope.numel() // dim
         ok = ok and rope.dtype is f32 and rope.shape[-1] == dim and rope.is_contiguous()
     ok = ok and (q is None) == (q_out is None)
+    if shifts is not None:
+        ok = ok and shifts.dtype is i32 and shifts.numel() == seqs and shifts.is_contiguous()
     if ok and q is not None:
         size = q_out.numel()
         q_heads = size // (rows * dim) if rows else 0
@@ -414,8 +428,12 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
     a = KVInput(_ptr(q), k.data_ptr(), v.data_ptr(), q_stride, _row_stride(k, rows, heads, dim, what),
                 _row_stride(v, rows, heads, dim, what), kind is f16, _ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), rope_rows,
                 q_heads, _ptr(q_out))
-    _check(_call("tetra_kv_append", ctypes.addressof(cache), ctypes.addressof(a), starts.data_ptr(), rows, max_new,
-                 _stream(stream)), what)
+    if shifts is None:
+        st = _call("tetra_kv_append", ctypes.addressof(cache), ctypes.addressof(a), starts.data_ptr(), rows, max_new, _stream(stream))
+    else:
+        st = _call("tetra_kv_append_at", ctypes.addressof(cache), ctypes.addressof(a), starts.data_ptr(), shifts.data_ptr(),
+                   rows, max_new, _stream(stream))
+    _check(st, what)
 
 
 def kv_read(cache: KVCache, count: int, k_out, v_out, stream=None):
@@ -475,3 +493,143 @@ def sample(logits, temperature, top_k, top_p, min_p, u, tokens, workspace, strea
     _check(_call("tetra_sample", logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
                  temperature.data_ptr(), top_k.data_ptr(), top_p.data_ptr(), min_p.data_ptr(), u.data_ptr(),
                  tokens.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)), "tetra_sample")
+
+
+# ------------------------------- shared prefixes, eviction, log probabilities
+
+def _here(*tensors):
+    """Whether all tensors (or None) lie on the current GPU, whose memory alone a launch may name."""
+    at = tensors[0].get_device()
+    if at < 0:
+        return False
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            return False
+    if _device is None:
+        _first_stream()
+    if _device is None:
+        import torch
+        return at == torch.cuda.current_device()
+    return at == _device()
+
+
+def _space(name, *args):
+    """A workspace (a torch uint8 tensor) of as many bytes as the function `name` says."""
+    import torch
+    n = int(_call(name, *args))
+    _expect(n > 0, name)
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def _rows_of(cache, q, starts, what):
+    """rows, q heads and row stride of q [rows, q_heads, head_dim], once q and starts fit the cache."""
+    _, f16, i32 = _kinds or _kinds_of_torch()
+    dim, seqs = cache.sizes[1:]
+    rows = q.shape[0]
+    heads = q.numel() // (rows * dim) if rows else 0
+    _expect(q.dtype is f16 and heads and starts.dtype is i32 and starts.numel() == seqs + 1 and starts.is_contiguous(), what)
+    return rows, heads, _row_stride(q, rows, heads, dim, what)
+
+
+def kv_attend_shared_workspace():
+    """A workspace for kv_attend_shared on the current device (a torch uint8 tensor)."""
+    return _space("tetra_kv_attend_shared_workspace_bytes")
+
+
+def kv_attend_shared(cache: KVCache, q, starts, max_new: int, groups, shared, out, workspace, scale: float = None,
+                     stream=None):
+    """kv_attend (without a window) of a batch whose sequences groups[g] .. groups[g + 1] - 1 (int32 [n + 1])
+    begin with the same shared[g] tokens (int32 [n]) in the same pages, which are read once for all of them;
+    workspace from kv_attend_shared_workspace(), one per stream."""
+    what = "tetra_kv_attend_shared"
+    rows, heads, stride = _rows_of(cache, q, starts, what)
+    _, f16, i32 = _kinds
+    n = shared.numel()
+    _expect(out.dtype is f16 and groups.dtype is i32 and shared.dtype is i32 and groups.numel() == n + 1
+            and groups.is_contiguous() and shared.is_contiguous() and workspace.is_contiguous(), what)
+    out_stride = _row_stride(out, rows, heads, cache.sizes[1], what)
+    _expect(_here(q, starts, groups, shared, out, workspace, *cache.tensors), what)
+    _check(_call("tetra_kv_attend_shared", ctypes.addressof(cache), q.data_ptr(), stride, starts.data_ptr(), rows, max_new,
+                 heads, cache.sizes[1] ** -0.5 if scale is None else scale, groups.data_ptr(), shared.data_ptr(), n,
+                 out.data_ptr(), out_stride, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                 _stream(stream)), what)
+
+
+def kv_weigh_workspace(cache: KVCache, rows: int, q_heads: int):
+    """A workspace for kv_weigh of up to `rows` rows (a torch uint8 tensor)."""
+    return _space("tetra_kv_weigh_workspace_bytes", ctypes.addressof(cache), rows, q_heads)
+
+
+def _mass_tokens(t, cache, what):
+    """Tokens that t fp32 [seqs, kv_heads, tokens] has places for."""
+    f32 = (_kinds or _kinds_of_torch())[0]
+    heads, _, seqs = cache.sizes
+    _expect(t.dtype is f32 and t.dim() == 3 and t.is_contiguous() and t.shape[0] == seqs and t.shape[1] == heads, what)
+    return t.shape[2]
+
+
+def kv_weigh(cache: KVCache, q, starts, max_new: int, mass, mass_out, workspace, scale: float = None, window: int = 0,
+             decay: float = 1.0, stream=None):
+    """mass_out fp32 [seqs, kv_heads, tokens] = decay * mass (the same, or None for zeros; may be mass_out) + the
+    attention weight that each cached token gets from the rows q (rows, scale and window as in kv_attend); workspace
+    from kv_weigh_workspace(), one per stream."""
+    what = "tetra_kv_weigh"
+    rows, heads, stride = _rows_of(cache, q, starts, what)
+    tokens = _mass_tokens(mass_out, cache, what)
+    _expect((mass is None or _mass_tokens(mass, cache, what) == tokens) and workspace.is_contiguous()
+            and _here(q, starts, mass_out, workspace, mass, *cache.tensors), what)
+    _check(_call("tetra_kv_weigh", ctypes.addressof(cache), q.data_ptr(), stride, starts.data_ptr(), rows, max_new, heads,
+                 cache.sizes[1] ** -0.5 if scale is None else scale, window, _ptr(mass), mass_out.data_ptr(), tokens, decay,
+                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), what)
+
+
+def kv_evict_workspace(cache: KVCache, to: KVCache):
+    """A workspace for kv_evict from `cache` into `to` (a torch uint8 tensor)."""
+    return _space("tetra_kv_evict_workspace_bytes", ctypes.addressof(cache), ctypes.addressof(to))
+
+
+def kv_evict(cache: KVCache, to: KVCache, mass, mass_out, workspace, recent: int = 0, stream=None):
+    """Of every sequence and head of `cache` the last `recent` tokens and those of most mass (fp32 [seqs, kv_heads,
+    tokens], from kv_weigh) go into the pages of `to`, whose lens say how many stay; mass_out (fp32 [seqs, kv_heads,
+    tokens], or None) gets what they have by their new places; workspace from kv_evict_workspace(), one per stream."""
+    what = "tetra_kv_evict"
+    tokens = _mass_tokens(mass, cache, what)
+    out_tokens = 0 if mass_out is None else _mass_tokens(mass_out, cache, what)
+    _expect(workspace.is_contiguous() and _here(mass, mass_out, workspace, *cache.tensors, *to.tensors), what)
+    _check(_call("tetra_kv_evict", ctypes.addressof(cache), ctypes.addressof(to), mass.data_ptr(), tokens, recent,
+                 _ptr(mass_out), out_tokens, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                 _stream(stream)), what)
+
+
+def log_probs_workspace(rows: int, vocab: int, top: int = 0):
+    """A workspace for log_probs over rows of vocab logits with `top` alternatives (a torch uint8 tensor)."""
+    return _space("tetra_log_probs_workspace_bytes", rows, vocab, top)
+
+
+def log_probs(logits, tokens, out, workspace, entropy=None, top_tokens=None, top_out=None, temperature=None, stream=None):
+    """out fp32 [rows, given] = log probabilities of tokens int32 [rows, given] (or [rows]; both None: none) under
+    logits fp32 or fp16 [rows, vocab] at the rows' temperature (fp32 [rows], or None for 1); entropy fp32 [rows], and
+    the likeliest tokens top_tokens int32 [rows, top] with their log probabilities top_out fp32 [rows, top], where
+    wanted; workspace from log_probs_workspace(), one per stream."""
+    what = "tetra_log_probs"
+    f32, f16, i32 = _kinds or _kinds_of_torch()
+    rows, vocab = logits.shape
+    half = logits.dtype is f16
+    ok = (half or logits.dtype is f32) and (logits.stride(1) == 1 or vocab == 1) and workspace.is_contiguous() and rows > 0
+    given = top = 0
+    for t, kind in ((tokens, i32), (out, f32), (entropy, f32), (top_tokens, i32), (top_out, f32), (temperature, f32)):
+        ok = ok and (t is None or (t.dtype is kind and t.is_contiguous()))
+    for t in (entropy, temperature):
+        ok = ok and (t is None or t.numel() == rows)
+    ok = ok and (tokens is None) == (out is None) and (top_tokens is None) == (top_out is None)
+    if ok and tokens is not None:
+        given = tokens.numel() // rows
+        ok = tokens.numel() == out.numel() == given * rows and tokens.shape[0] == out.shape[0] == rows
+    if ok and top_tokens is not None:
+        top = top_tokens.numel() // rows
+        ok = top_tokens.numel() == top_out.numel() == top * rows and top_tokens.shape[0] == top_out.shape[0] == rows
+    _expect(ok and _here(logits, workspace, tokens, out, entropy, top_tokens, top_out, temperature), what)
+    _check(_call("tetra_log_probs", logits.data_ptr(), half, logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                 _ptr(temperature), _ptr(tokens) if given else None, given, _ptr(out) if given else None, _ptr(entropy), top,
+                 _ptr(top_tokens) if top else None, _ptr(top_out) if top else None, workspace.data_ptr(),
+                 workspace.numel() * workspace.element_size(), _stream(stream)), what)

@@ -7,19 +7,19 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetra.so")
 
-SOURCES = ["tables.cpp", "tetra.hip", "serve.hip"]
+SOURCES = ["tables.cpp", "tetra.hip", "serve.hip", "batch.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950",
     "-O3",
     "-std=c++17",
     "-fPIC",
-    "-shared",
     # packed FP32 VALU ops stay off on this target
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall",
@@ -67,14 +67,14 @@ def generate_tables(verbose: bool = False) -> str:
 def build(verbose: bool = False) -> str:
     """Compiles every source into libtetra.so next to this file; returns its path."""
     inc = generate_tables(verbose)
+    objects = [os.path.join(BUILD_DIR, name + ".o") for name in SOURCES]
+    with ThreadPoolExecutor(len(SOURCES)) as pool:
+        done = [pool.submit(_run, [hipcc(), *HIP_FLAGS, "-I", inc, "-c", os.path.join(CSRC, name), "-o", to], verbose)
+                for name, to in zip(SOURCES, objects)]
+        for d in done:
+            d.result()
     tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIP_FLAGS, "-I", inc, *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed with status {res.returncode}")
+    _run([hipcc(), *HIP_FLAGS, "-shared", *objects, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     return LIB
 

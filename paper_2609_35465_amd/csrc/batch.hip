@@ -1,0 +1,150 @@
+// What a server does with a batch's cache and logits beside attention and
+// sampling, for MI355X (gfx950): the weights of cached tokens, eviction by them,
+// log probabilities.  The entry points of include/tetra.h: host code here
+// validates arguments and launches the kernels of weigh.h, evict.h and score.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/tetra.h"
+#include "evict.h"
+#include "host.h"
+#include "score.h"
+#include "weigh.h"
+
+using namespace tetra_host;
+
+namespace {
+
+constexpr size_t kMinWorkspace = 256;
+
+size_t rounded(size_t bytes) { return std::max(kMinWorkspace, (bytes + 255) / 256 * 256); }
+
+// a cache's sizes alone, as tetra_kv_cache limits them
+bool sizes_ok(const tetra_kv_cache* c) {
+    if (!c || c->num_pages < 1 || c->kv_heads < 1 || c->seqs < 1 || c->max_pages < 1) return false;
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return false;
+    return c->max_pages <= kMaxTokens / c->page_tokens && (c->head_dim == 64 || c->head_dim == 128);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int q_heads) {
+    if (!sizes_ok(cache) || rows < 1 || q_heads < 1 || q_heads % cache->kv_heads) return 0;
+    return rounded(sizeof(float) * rows * q_heads);
+}
+
+int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                   int max_new, int q_heads, float scale, int window, const float* mass, float* mass_out,
+                   int mass_tokens, float decay, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    tetra_dev::WeighArgs a;
+    if (int st = cache_of(cache, &a.c)) return st;
+    if (!q || !starts || !mass_out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
+    if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale) || mass_tokens < 1) return TETRA_EINVAL;
+    if (!(decay >= 0.f && decay <= 1.f)) return TETRA_EINVAL;
+    if (q_stride < static_cast<long long>(q_heads) * cache->head_dim || rows > kMaxGrid / q_heads) return TETRA_EINVAL;
+    if (!aligned(q, 16) || q_stride % 8 || !aligned(starts, 4) || !aligned(mass, 4) || !aligned(mass_out, 4) ||
+        !aligned(workspace, 256))
+        return TETRA_EALIGN;
+    if (workspace_bytes < tetra_kv_weigh_workspace_bytes(cache, rows, q_heads)) return TETRA_EINVAL;
+    const long long grid = (mass_tokens + 255ll) / 256 * a.c.kv_heads;
+    if (grid > kMaxGrid / a.c.seqs) return TETRA_EINVAL;
+    a.q = q;
+    a.starts = starts;
+    a.mass = mass;
+    a.out = mass_out;
+    a.logs = static_cast<float*>(workspace);
+    a.q_stride = q_stride;
+    a.scale = scale * 1.44269504f;
+    a.decay = decay;
+    a.rows = rows;
+    a.max_new = max_new;
+    a.q_heads = q_heads;
+    a.group = q_heads / a.c.kv_heads;
+    a.window = window;
+    a.mass_tokens = mass_tokens;
+    const dim3 g1(static_cast<unsigned>(rows * q_heads)), g2(static_cast<unsigned>(grid * a.c.seqs));
+    if (cache->head_dim == 64) {
+        hipLaunchKernelGGL((tetra_dev::weigh_logs_kernel<64>), g1, dim3(64), 0, stream, a);
+        hipLaunchKernelGGL((tetra_dev::weigh_add_kernel<64>), g2, dim3(256), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((tetra_dev::weigh_logs_kernel<128>), g1, dim3(64), 0, stream, a);
+        hipLaunchKernelGGL((tetra_dev::weigh_add_kernel<128>), g2, dim3(256), 0, stream, a);
+    }
+    return launch_status();
+}
+
+size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to) {
+    if (!sizes_ok(from) || !sizes_ok(to)) return 0;
+    return rounded(sizeof(int) * from->seqs * from->kv_heads * to->max_pages * to->page_tokens);
+}
+
+int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const float* mass, int mass_tokens, int recent,
+                   float* mass_out, int out_tokens, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    tetra_dev::EvictArgs a;
+    if (int st = cache_of(from, &a.from)) return st;
+    if (int st = cache_of(to, &a.to)) return st;
+    if (from->kv_heads != to->kv_heads || from->head_dim != to->head_dim || from->page_tokens != to->page_tokens ||
+        from->seqs != to->seqs)
+        return TETRA_EINVAL;
+    if (!mass || !workspace || mass_tokens < 1 || recent < 0 || (mass_out && out_tokens < 1) || mass_out == mass)
+        return TETRA_EINVAL;
+    if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(workspace, 256)) return TETRA_EALIGN;
+    if (workspace_bytes < tetra_kv_evict_workspace_bytes(from, to)) return TETRA_EINVAL;
+    const long long units = static_cast<long long>(a.from.seqs) * a.from.kv_heads;
+    if (units > kMaxGrid / 2 / a.to.max_pages) return TETRA_EINVAL;
+    a.mass = mass;
+    a.out = mass_out;
+    a.tokens = static_cast<int*>(workspace);
+    a.capacity = to->max_pages * to->page_tokens;
+    a.mass_tokens = mass_tokens;
+    a.out_tokens = out_tokens;
+    a.recent = recent;
+    hipLaunchKernelGGL(tetra_dev::evict_choose_kernel, dim3(static_cast<unsigned>(units)), dim3(tetra_dev::kEvictThreads), 0,
+                       stream, a);
+    const dim3 g(static_cast<unsigned>(units * a.to.max_pages * 2));
+    if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, dim3(256), 0, stream, a);
+    return launch_status();
+}
+
+size_t tetra_log_probs_workspace_bytes(int rows, int vocab, int top) {
+    if (rows < 1 || vocab < 1 || vocab > kMaxVocab || top < 0 || top > tetra_dev::kMostTop) return 0;
+    return kMinWorkspace;
+}
+
+int tetra_log_probs(const void* logits, int half, long long stride, int rows, int vocab, const float* temperature,
+                    const int* tokens, int given, float* out, float* entropy, int top, int* top_tokens, float* top_out,
+                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!logits || !workspace || (half != 0 && half != 1) || rows < 1 || vocab < 1 || vocab > kMaxVocab || stride < vocab)
+        return TETRA_EINVAL;
+    if (given < 0 || top < 0 || top > tetra_dev::kMostTop) return TETRA_EINVAL;
+    if ((given && (!tokens || !out)) || (top && (!top_tokens || !top_out))) return TETRA_EINVAL;
+    if (!given && !top && !entropy) return TETRA_EINVAL;
+    if (!aligned(logits, half ? 2 : 4) || !aligned(temperature, 4) || !aligned(tokens, 4) || !aligned(out, 4) ||
+        !aligned(entropy, 4) || !aligned(top_tokens, 4) || !aligned(top_out, 4) || !aligned(workspace, 256))
+        return TETRA_EALIGN;
+    if (workspace_bytes < tetra_log_probs_workspace_bytes(rows, vocab, top)) return TETRA_EINVAL;
+    tetra_dev::ScoreArgs a;
+    a.logits = logits;
+    a.stride = stride;
+    a.temperature = temperature;
+    a.tokens = tokens;
+    a.out = out;
+    a.entropy = entropy;
+    a.top_out = top_out;
+    a.top_tokens = top_tokens;
+    a.rows = rows;
+    a.vocab = vocab;
+    a.given = given;
+    a.top = top;
+    const dim3 g(static_cast<unsigned>(rows)), b(256);
+    if (half) hipLaunchKernelGGL(tetra_dev::score_kernel<_Float16>, g, b, 0, stream, a);
+    else hipLaunchKernelGGL(tetra_dev::score_kernel<float>, g, b, 0, stream, a);
+    return launch_status();
+}
+
+}  // extern "C"

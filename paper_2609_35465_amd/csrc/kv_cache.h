@@ -61,6 +61,7 @@ struct AppendArgs {
     const float *q_norm, *k_norm;
     const float* rope;
     const int* starts;
+    const int* shifts;   // or NULL
     uint16_t* q_out;
     float eps;
     int rope_rows, rows, max_new, q_heads;
@@ -154,6 +155,15 @@ __device__ __forceinline__ f32x2 load2(const void* p, long long at) {
     }
 }
 
+// The place in the rotation's table of a sequence's token: moved by its shift, if
+// the call has any.
+struct Turn {
+    int shift;
+    __device__ __forceinline__ Turn(const AppendArgs& a, int seq)
+        : shift(a.shifts ? min(max(a.shifts[seq], 0), (1 << 30) - 1) : 0) {}
+    __device__ __forceinline__ int of(int position) const { return min(position, 1 << 30) + shift; }
+};
+
 // A head of D dimensions lies in D / 8 lanes: lane `sub` holds dimensions
 // 4 sub .. 4 sub + 3 (x[0..3]) and their partners D / 2 further (x[4..7]).
 template <int D, bool HALF>
@@ -226,7 +236,7 @@ __device__ __forceinline__ float grown_scale(float amax, float before, float* ld
 
 // `entry`: where the table names the page; it is on its way with the values
 template <int D, bool HALF>
-__device__ void append_keys(const AppendArgs& a, const Span& s, int number, const int* entry, int head, float* lds) {
+__device__ void append_keys(const AppendArgs& a, const Span& s, const Turn& turn, int number, const int* entry, int head, float* lds) {
     const int page = *entry;
     constexpr int kLanes = D / 8, kPerPass = 64 / kLanes, kPasses = kGroupTokens / kPerPass;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -247,7 +257,7 @@ __device__ void append_keys(const AppendArgs& a, const Span& s, int number, cons
     if (page < 0 || page >= a.c.num_pages) return;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-        norm_and_rotate<D>(x[p], a.k_norm, a.eps, a.rope, a.rope_rows, token0 + p * kPerPass, sub);
+        norm_and_rotate<D>(x[p], a.k_norm, a.eps, a.rope, a.rope_rows, turn.of(token0 + p * kPerPass), sub);
 #pragma unroll
         for (int i = 0; i < 8; ++i) amax = larger(amax, x[p][i]);
     }
@@ -346,7 +356,7 @@ __device__ void append_queries(const AppendArgs& a, int unit) {
     if (first < end) load_head<D, HALF>(x0, a.q, row * a.q_stride + first * D, sub);
     const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, row, [](int start, int) { return start; });
     if (at.seq < 0 || row < at.s.row0 || row >= at.s.row0 + at.s.n) return;
-    const int position = at.s.first + row - at.s.row0;
+    const int position = Turn(a, at.seq).of(at.s.first + row - at.s.row0);
     auto finish = [&](float (&x)[8], int h) {
         norm_and_rotate<D>(x, a.q_norm, a.eps, a.rope, a.rope_rows, position, sub);
         f16x4 lo, hi;
@@ -389,7 +399,7 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a) {
         return;
     const int* entry = a.c.pages + static_cast<size_t>(at.seq) * a.c.max_pages + number;
     if (rest & 1) append_values<D, HALF>(a, s, number, entry, rest >> 1, lds);
-    else append_keys<D, HALF>(a, s, number, entry, rest >> 1, lds);
+    else append_keys<D, HALF>(a, s, Turn(a, at.seq), number, entry, rest >> 1, lds);
 }
 
 // The last `count` tokens of every sequence as fp16, [seqs][count][kv_heads][D]

@@ -5,52 +5,17 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 
 #include "../../include/tetra.h"
 #include "attend.h"
+#include "host.h"
 #include "kv_cache.h"
 #include "sample.h"
 
 namespace {
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int launch_status() { return hipGetLastError() == hipSuccess ? TETRA_OK : TETRA_EDEVICE; }
-
-constexpr int kMaxTokens = 1 << 30;    // of a sequence, so that token numbers have room above them in an int
-
-// a cache's sizes and pointers, as the kernels take them
-int cache_of(const tetra_kv_cache* c, tetra_dev::KvCache* out) {
-    if (!c || !c->k || !c->v || !c->scales || !c->pages || !c->lens) return TETRA_EINVAL;
-    if (c->num_pages < 1 || c->kv_heads < 1 || c->seqs < 1 || c->max_pages < 1) return TETRA_EINVAL;
-    int shift = 4;
-    while (shift < 7 && 1 << shift != c->page_tokens) ++shift;
-    if (1 << shift != c->page_tokens) return TETRA_EINVAL;
-    if (c->max_pages > kMaxTokens >> shift) return TETRA_EINVAL;
-    if (c->head_dim != 64 && c->head_dim != 128) return c->head_dim < 1 ? TETRA_EINVAL : TETRA_EUNSUPPORTED;
-    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->scales, 8) || !aligned(c->pages, 4) ||
-        !aligned(c->lens, 4))
-        return TETRA_EALIGN;
-    *out = {c->k, c->v, c->scales, c->pages, c->lens, c->num_pages, c->page_tokens, shift, c->kv_heads, c->seqs,
-            c->max_pages};
-    return TETRA_OK;
-}
-
-// compute units of the current device, asked for once per device
-int device_cus(int* cus) {
-    static std::atomic<int> known[64];
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return TETRA_EDEVICE;
-    n = known[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return TETRA_EDEVICE;
-        known[dev].store(n, std::memory_order_relaxed);
-    }
-    *cus = n;
-    return TETRA_OK;
-}
+using namespace tetra_host;
 
 constexpr int kFewGroupsPerCU = 2;
 constexpr size_t kMinAttendWorkspace = 4096;
@@ -62,8 +27,6 @@ size_t attend_workspace(int cus) {
     return ((few_parts(cus) + 2 * static_cast<size_t>(cus) * tetra_dev::kManySlot<128, 4>) * sizeof(float) + 255) / 256 * 256;
 }
 
-constexpr long long kMaxGrid = 0x7FFFFFFFll;
-constexpr int kMaxVocab = 1 << 22;     // so that a row's sum of weights, 2^62 at most, fits 64 bits
 
 // How a call of tetra_kv_attend is spread; the lengths, and with them the
 // pieces, are the device's own matter.
@@ -175,12 +138,8 @@ int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
     return launch_status();
 }
 
-}  // namespace
-
-extern "C" {
-
-int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, int rows, int max_new,
-                    hipStream_t stream) {
+int append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, const int* shifts, int rows, int max_new,
+           hipStream_t stream) {
     tetra_dev::AppendArgs a;
     if (int st = cache_of(cache, &a.c)) return st;
     if (!in || !in->k || !in->v || !starts || rows < 1 || max_new < 1 || max_new > rows) return TETRA_EINVAL;
@@ -192,7 +151,7 @@ int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const
     if (in->k_stride < kv_width || in->v_stride < kv_width || (in->q && in->q_stride < q_width)) return TETRA_EINVAL;
     if (!aligned(in->k, 16) || !aligned(in->v, 16) || in->k_stride % 8 || in->v_stride % 8 || !aligned(starts, 4) ||
         (in->q && (!aligned(in->q, 16) || in->q_stride % 8 || !aligned(in->q_out, 16))) || !aligned(in->q_norm, 16) ||
-        !aligned(in->k_norm, 16) || !aligned(in->rope, 16))
+        !aligned(in->k_norm, 16) || !aligned(in->rope, 16) || !aligned(shifts, 4))
         return TETRA_EALIGN;
     a.q = in->q;
     a.k = in->k;
@@ -204,6 +163,7 @@ int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const
     a.k_norm = in->k_norm;
     a.rope = in->rope;
     a.starts = starts;
+    a.shifts = shifts;
     a.q_out = in->q_out;
     a.eps = in->eps;
     a.rope_rows = in->rope_rows;
@@ -232,6 +192,21 @@ int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const
     }
 #undef TETRA_APPEND
     return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int tetra_kv_append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, int rows, int max_new,
+                    hipStream_t stream) {
+    return append(cache, in, starts, nullptr, rows, max_new, stream);
+}
+
+int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, const int* shifts,
+                       int rows, int max_new, hipStream_t stream) {
+    if (!shifts) return TETRA_EINVAL;
+    return append(cache, in, starts, shifts, rows, max_new, stream);
 }
 
 int tetra_kv_read(const tetra_kv_cache* cache, int count, uint16_t* k_out, uint16_t* v_out, hipStream_t stream) {
@@ -288,6 +263,18 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
     return cache->head_dim == 64 ? attend_launch<64>(a, cus, stream) : attend_launch<128>(a, cus, stream);
+}
+
+size_t tetra_kv_attend_shared_workspace_bytes(void) { return tetra_kv_attend_workspace_bytes(); }
+
+int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                           int max_new, int q_heads, float scale, const int* groups, const int* shared, int num_groups,
+                           uint16_t* out, long long out_stride, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream) {
+    if (!cache || !groups || !shared || num_groups < 1 || num_groups > cache->seqs) return TETRA_EINVAL;
+    if (!aligned(groups, 4) || !aligned(shared, 4)) return TETRA_EALIGN;
+    return tetra_kv_attend(cache, q, q_stride, starts, rows, max_new, q_heads, scale, 0, out, out_stride, workspace,
+                           workspace_bytes, stream);
 }
 
 size_t tetra_sample_workspace_bytes(int rows, int vocab) {
