@@ -670,7 +670,7 @@ size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv
  *   logits: device fp32 (half 0) or fp16 (half 1), `stride` elements from a row
  *           to the next
  *   temperature: device fp32 [rows], or NULL for 1; T <= 0 and NaN (rows that
- *           are sampled greedily) count as 1
+ *           are sampled greedily) count as 1, T > 2^100 as 2^100
  *   tokens: device int32 [rows][given], out: fp32 the same (given 0: NULL)
  *   entropy: device fp32 [rows], or NULL
  *   top_tokens, top_out: device int32 and fp32 [rows][top], top 0..64 (0: NULL)

@@ -28,6 +28,15 @@ bool sizes_ok(const tetra_kv_cache* c) {
     return c->max_pages <= kMaxTokens / c->page_tokens && (c->head_dim == 64 || c->head_dim == 128);
 }
 
+template <class T, bool TOP>
+int score_launch(const tetra_dev::ScoreArgs& a, hipStream_t stream) {
+    if (static_cast<long long>(a.rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
+    hipLaunchKernelGGL((tetra_dev::score_kernel<T, TOP>), dim3(static_cast<unsigned>(a.rows * a.parts)), dim3(256), 0, stream, a);
+    if (a.parts > 1)
+        hipLaunchKernelGGL((tetra_dev::score_join_kernel<T, TOP>), dim3(static_cast<unsigned>(a.rows)), dim3(256), 0, stream, a);
+    return launch_status();
+}
+
 }  // namespace
 
 extern "C" {
@@ -112,8 +121,10 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
 }
 
 size_t tetra_log_probs_workspace_bytes(int rows, int vocab, int top) {
-    if (rows < 1 || vocab < 1 || vocab > kMaxVocab || top < 0 || top > tetra_dev::kMostTop) return 0;
-    return kMinWorkspace;
+    int cus = 0;
+    if (rows < 1 || vocab < 1 || vocab > kMaxVocab || top < 0 || top > tetra_dev::kMostTop || device_cus(&cus)) return 0;
+    const int parts = tetra_dev::score_shape(rows, vocab, cus).parts;
+    return parts > 1 ? rounded(static_cast<size_t>(rows) * parts * (16 + 8 * top)) : kMinWorkspace;
 }
 
 int tetra_log_probs(const void* logits, int half, long long stride, int rows, int vocab, const float* temperature,
@@ -127,6 +138,9 @@ int tetra_log_probs(const void* logits, int half, long long stride, int rows, in
     if (!aligned(logits, half ? 2 : 4) || !aligned(temperature, 4) || !aligned(tokens, 4) || !aligned(out, 4) ||
         !aligned(entropy, 4) || !aligned(top_tokens, 4) || !aligned(top_out, 4) || !aligned(workspace, 256))
         return TETRA_EALIGN;
+    int cus = 0;
+    if (workspace_bytes < kMinWorkspace) return TETRA_EINVAL;
+    if (int st = device_cus(&cus)) return st;
     if (workspace_bytes < tetra_log_probs_workspace_bytes(rows, vocab, top)) return TETRA_EINVAL;
     tetra_dev::ScoreArgs a;
     a.logits = logits;
@@ -141,10 +155,13 @@ int tetra_log_probs(const void* logits, int half, long long stride, int rows, in
     a.vocab = vocab;
     a.given = given;
     a.top = top;
-    const dim3 g(static_cast<unsigned>(rows)), b(256);
-    if (half) hipLaunchKernelGGL(tetra_dev::score_kernel<_Float16>, g, b, 0, stream, a);
-    else hipLaunchKernelGGL(tetra_dev::score_kernel<float>, g, b, 0, stream, a);
-    return launch_status();
+    const tetra_dev::ScoreShape shape = tetra_dev::score_shape(rows, vocab, cus);
+    a.parts = shape.parts;
+    a.part = shape.part;
+    a.sums = static_cast<float*>(workspace);
+    a.places = reinterpret_cast<uint64_t*>(a.sums + 4 * static_cast<size_t>(rows) * shape.parts);
+    if (half) return top ? score_launch<_Float16, true>(a, stream) : score_launch<_Float16, false>(a, stream);
+    return top ? score_launch<float, true>(a, stream) : score_launch<float, false>(a, stream);
 }
 
 }  // extern "C"
