@@ -28,6 +28,33 @@ bool sizes_ok(const tetra_kv_cache* c) {
     return c->max_pages <= kMaxTokens / c->page_tokens && (c->head_dim == 64 || c->head_dim == 128);
 }
 
+constexpr int kWeighGroupsPerCU = 2;
+
+// floats of kv_weigh's workspace
+struct WeighSpace {
+    int workers;
+    size_t spans, logs, bytes;
+    WeighSpace(int rows, int q_heads, int cus) {
+        workers = cus * kWeighGroupsPerCU;
+        logs = (static_cast<size_t>(rows) * q_heads + 63) / 64 * 64;
+        spans = logs * tetra_dev::kWeighSpans * 2;
+        bytes = rounded(sizeof(float) * (spans + logs + 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock));
+    }
+};
+
+template <int D>
+int weigh_launch(const tetra_dev::WeighArgs& a, hipStream_t stream) {
+    const dim3 g(static_cast<unsigned>(a.workers)), b(256);
+    const long long logs = (static_cast<long long>(a.rows) * a.q_heads + 3) / 4;
+    hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(logs)), b, 0, stream, a);
+    hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, b, 0, stream, a);
+    // several chunks of a sequence's rows only where it may have more than one tile of them
+    if (static_cast<long long>(a.max_new) * a.group > tetra_dev::kWeighRows)
+        hipLaunchKernelGGL(tetra_dev::weigh_join_kernel, g, b, 0, stream, a);
+    return launch_status();
+}
+
 template <class T, bool TOP>
 int score_launch(const tetra_dev::ScoreArgs& a, hipStream_t stream) {
     if (static_cast<long long>(a.rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
@@ -42,8 +69,10 @@ int score_launch(const tetra_dev::ScoreArgs& a, hipStream_t stream) {
 extern "C" {
 
 size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int q_heads) {
-    if (!sizes_ok(cache) || rows < 1 || q_heads < 1 || q_heads % cache->kv_heads) return 0;
-    return rounded(sizeof(float) * rows * q_heads);
+    int cus = 0;
+    if (!sizes_ok(cache) || rows < 1 || q_heads < 1 || q_heads % cache->kv_heads || rows > kMaxGrid / q_heads || device_cus(&cus))
+        return 0;
+    return WeighSpace(rows, q_heads, cus).bytes;
 }
 
 int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
@@ -58,14 +87,21 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     if (!aligned(q, 16) || q_stride % 8 || !aligned(starts, 4) || !aligned(mass, 4) || !aligned(mass_out, 4) ||
         !aligned(workspace, 256))
         return TETRA_EALIGN;
-    if (workspace_bytes < tetra_kv_weigh_workspace_bytes(cache, rows, q_heads)) return TETRA_EINVAL;
-    const long long grid = (mass_tokens + 255ll) / 256 * a.c.kv_heads;
-    if (grid > kMaxGrid / a.c.seqs) return TETRA_EINVAL;
+    // items of a launch are counted in an int: the blocks of all heads, and kWeighItems times the workgroups
+    const long long tokens = std::max<long long>(static_cast<long long>(a.c.max_pages) << a.c.page_shift, mass_tokens);
+    if ((tokens + 255) / 256 * a.c.kv_heads > (1 << 30) / a.c.seqs) return TETRA_EINVAL;
+    int cus = 0;
+    if (workspace_bytes < kMinWorkspace) return TETRA_EINVAL;
+    if (int st = device_cus(&cus)) return st;
+    const WeighSpace space(rows, q_heads, cus);
+    if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     a.q = q;
     a.starts = starts;
     a.mass = mass;
     a.out = mass_out;
-    a.logs = static_cast<float*>(workspace);
+    a.spans = static_cast<float*>(workspace);
+    a.logs = a.spans + space.spans;
+    a.parts = a.logs + space.logs;
     a.q_stride = q_stride;
     a.scale = scale * 1.44269504f;
     a.decay = decay;
@@ -75,15 +111,8 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
     a.mass_tokens = mass_tokens;
-    const dim3 g1(static_cast<unsigned>(rows * q_heads)), g2(static_cast<unsigned>(grid * a.c.seqs));
-    if (cache->head_dim == 64) {
-        hipLaunchKernelGGL((tetra_dev::weigh_logs_kernel<64>), g1, dim3(64), 0, stream, a);
-        hipLaunchKernelGGL((tetra_dev::weigh_add_kernel<64>), g2, dim3(256), 0, stream, a);
-    } else {
-        hipLaunchKernelGGL((tetra_dev::weigh_logs_kernel<128>), g1, dim3(64), 0, stream, a);
-        hipLaunchKernelGGL((tetra_dev::weigh_add_kernel<128>), g2, dim3(256), 0, stream, a);
-    }
-    return launch_status();
+    a.workers = space.workers;
+    return cache->head_dim == 64 ? weigh_launch<64>(a, stream) : weigh_launch<128>(a, stream);
 }
 
 size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to) {

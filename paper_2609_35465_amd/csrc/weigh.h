@@ -1,15 +1,33 @@
 // The attention weight that cached tokens get from a call's rows (kv_weigh).
 // Included by batch.hip.
 //
-//   mass'[s][h][j] = decay mass[s][h][j] + sum_i exp(s_ij) / sum_t exp(s_it)
+//   mass'[s][h][j] = decay mass[s][h][j] + sum_i 2^(s_ij - L_i), L_i = log2 sum_t 2^(s_it)
 //
-// over the rows i (token, q head of the cache head h) of sequence s that see
-// token j.
+// over the rows i (token, q head of the cache head h: in that order) of sequence
+// s that see token j, with s_ij = scale log2(e) q_i . k_j.  L must be known before
+// the sum over rows, so the scores are found twice: once for L (a row's largest
+// score and sum over each span of tokens, then joined), once for the weights.
+//
+// Both times the keys stay and the rows pass by: a wave holds 64 tokens in fp16
+// as operands of v_mfma_f32_32x32x16_f16, S^T = K Q^T, and a workgroup's four waves
+// share the rows, 32 at a time, from LDS.  A lane then has scores of one row (lane
+// % 32) and 32 tokens: 8 (i / 4) + 4 (lane / 32) + i % 4 of each 32.  A row's
+// maximum and sum stay within a lane and its other half; a token's sum over the
+// rows is one addition a score, and one exchange over the lanes at the end.
 #pragma once
 
-#include "kv_cache.h"
+#include <type_traits>
+
+#include "attend.h"
 
 namespace tetra_dev {
+
+constexpr int kWeighBlock = 256;          // tokens of a workgroup, 64 of a wave
+constexpr int kWeighRows = 32;            // rows of a tile
+constexpr int kWeighSpans = 64;           // of a sequence's tokens, for the sums, at most
+constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
+constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
+constexpr float kWeighNone = -3e38f;      // a maximum over no score
 
 struct WeighArgs {
     KvCache c;
@@ -17,78 +35,444 @@ struct WeighArgs {
     const int* starts;
     const float* mass;
     float* out;
-    float* logs;      // of every row and q head: log2 of the sum of its weights
+    float* spans;         // [rows][q_heads][kWeighSpans][2]: largest score and sum of a row over a span
+    float* logs;          // [rows][q_heads]: L, +inf where a row sees nothing
+    float* parts;         // [2 kWeighItems workers][kWeighBlock]: a block's sums over some of its rows
     long long q_stride;
-    float scale;      // scale log2(e)
+    float scale;          // scale log2(e)
     float decay;
     int rows, max_new, q_heads, group, window, mass_tokens;
+    int workers;          // workgroups of each launch but that of the logs
 };
 
-template <int D>
-__device__ float weigh_score(const WeighArgs& a, const uint16_t* q, int seq, int token, int head, bool* there) {
-    const int page = a.c.pages[static_cast<size_t>(seq) * a.c.max_pages + (token >> a.c.page_shift)];
-    *there = page >= 0 && page < a.c.num_pages;
-    if (!*there) return -INFINITY;
-    const size_t ph = static_cast<size_t>(page) * a.c.kv_heads + head;
-    const int8_t* k = a.c.k + (ph * a.c.page_tokens + (token & (a.c.page_tokens - 1))) * D;
-    float s = 0.f;
-    for (int d = 0; d < D; ++d) s += static_cast<float>(__builtin_bit_cast(_Float16, q[d])) * static_cast<float>(k[d]);
-    return s * a.c.scales[2 * ph] * a.scale;
+// What a sequence asks for.
+struct WeighSeq {
+    Span s;
+    int all;              // its rows, those past max_new among them
+    int end;              // tokens that may be seen: below this
+    int written;          // tokens that have a place in mass_out
+    int blocks, tiles;    // of its tokens, of its rows
+
+    __device__ __forceinline__ WeighSeq() : s{0, 0, 0, 0}, all(0), end(0), written(0), blocks(0), tiles(0) {}
+    __device__ __forceinline__ WeighSeq(const WeighArgs& a, int seq) {
+        const int start = a.starts[seq], next = a.starts[seq + 1], len = a.c.lens[seq];
+        s = span_between(start, next, len, a.rows, a.max_new);
+        all = max(min(max(next, 0), a.rows) - s.row0, 0);
+        const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
+        end = static_cast<int>(min(static_cast<long long>(s.len), kept));
+        written = min(max(len, 0), a.mass_tokens);
+        // a sequence that keeps what it has needs no visit where it has that already
+        if (all == 0 && a.mass == a.out) written = 0;
+        blocks = (max(s.n ? end : 0, written) + kWeighBlock - 1) / kWeighBlock;
+        tiles = (s.n * a.group + kWeighRows - 1) / kWeighRows;
+    }
+};
+
+// Items of a launch: a sequence's (head, block or span of blocks, chunk of row tiles).
+struct WeighItem {
+    int seq, head, block, blocks, tile, tiles;      // blocks `block` .. block + blocks - 1, tiles likewise
+    int chunks;                                     // of the block
+    int slot;                                       // of the item's part, where there are several chunks
+    WeighSeq q;
+};
+
+enum WeighPass { kWeighSpanSums, kWeighTokens, kWeighJoin };
+
+// Row tiles of a chunk, so that there are some kWeighItems items a workgroup: then no
+// more than twice that many have a part of a block's sums to leave.
+struct WeighPlan {
+    int chunk, total;             // row tiles of a chunk; items
+    int lane_items, lane_slots;   // of a lane's sequence, the first 64
+
+    __device__ __forceinline__ static int span_blocks(const WeighSeq& q) {
+        return max(1, (q.blocks + kWeighSpans - 1) / kWeighSpans);
+    }
+    __device__ __forceinline__ static int spans_of(const WeighSeq& q) {
+        return (q.blocks + span_blocks(q) - 1) / span_blocks(q);
+    }
+    __device__ __forceinline__ int chunks_of(const WeighSeq& q) const { return max(1, (q.tiles + chunk - 1) / chunk); }
+    __device__ __forceinline__ int slots_of(const WeighArgs& a, const WeighSeq& q) const {
+        const int n = chunks_of(q);
+        return n > 1 ? n * q.blocks * a.c.kv_heads : 0;
+    }
+    template <WeighPass PASS>
+    __device__ __forceinline__ int items_of(const WeighArgs& a, const WeighSeq& q) const {
+        if (PASS == kWeighSpanSums) return q.s.n ? spans_of(q) * a.c.kv_heads * chunks_of(q) : 0;
+        if (PASS == kWeighTokens) return q.blocks * a.c.kv_heads * chunks_of(q);
+        return chunks_of(q) > 1 ? q.blocks * a.c.kv_heads : 0;
+    }
+
+    template <WeighPass PASS>
+    __device__ __forceinline__ WeighPlan(const WeighArgs& a, WeighSeq& mine, std::integral_constant<WeighPass, PASS>) {
+        const int lane = threadIdx.x & 63;
+        unsigned long long steps = 0;
+        for (int i = lane; i < a.c.seqs; i += 64) {
+            const WeighSeq q(a, i);
+            if (i < 64) mine = q;
+            steps += static_cast<unsigned long long>(q.blocks) * q.tiles * a.c.kv_heads;
+        }
+        steps = wave_all(Sum(), steps);
+        const unsigned long long most = static_cast<unsigned long long>(kWeighItems) * a.workers;
+        chunk = static_cast<int>(max(1ull, min((steps + most - 1) / most, 1ull << 26)));
+        if (PASS == kWeighSpanSums) chunk = min(chunk, kWeighMostTiles);
+        lane_items = items_of<PASS>(a, mine);
+        lane_slots = slots_of(a, mine);
+        total = wave_all(Sum(), lane_items);
+        for (int i0 = 64; i0 < a.c.seqs; i0 += 64) {
+            int n = 0;
+            if (i0 + lane < a.c.seqs) n = items_of<PASS>(a, WeighSeq(a, i0 + lane));
+            total += wave_all(Sum(), n);
+        }
+    }
+
+    // item x of all; the sequences a lane each
+    template <WeighPass PASS>
+    __device__ __forceinline__ WeighItem find(const WeighArgs& a, const WeighSeq& first, int x,
+                                              std::integral_constant<WeighPass, PASS>) const {
+        const int lane = threadIdx.x & 63;
+        WeighItem w;
+        w.seq = -1;
+        int before = 0, slots = 0;
+        for (int i0 = 0; i0 < a.c.seqs; i0 += 64) {
+            WeighSeq q = first;
+            int n = lane_items, m = lane_slots;
+            if (i0) {
+                q = WeighSeq();
+                if (i0 + lane < a.c.seqs) q = WeighSeq(a, i0 + lane);
+                n = items_of<PASS>(a, q);
+                m = slots_of(a, q);
+            }
+            const int upto = wave_upto(Sum(), n) + before, slots_upto = wave_upto(Sum(), m) + slots;
+            const unsigned long long has = __ballot(upto > x);
+            if (has) {
+                const int l = __builtin_ctzll(has);
+                w.seq = i0 + l;
+                w.q.s = {lane_of(q.s.row0, l), lane_of(q.s.n, l), lane_of(q.s.first, l), lane_of(q.s.len, l)};
+                w.q.all = lane_of(q.all, l);
+                w.q.end = lane_of(q.end, l);
+                w.q.written = lane_of(q.written, l);
+                w.q.blocks = lane_of(q.blocks, l);
+                w.q.tiles = lane_of(q.tiles, l);
+                const int at = x - lane_of(upto - n, l), per = PASS == kWeighJoin ? 1 : chunks_of(w.q);
+                const int place = at / per, part = at - place * per;
+                w.chunks = chunks_of(w.q);
+                w.head = place % a.c.kv_heads;
+                w.block = place / a.c.kv_heads;
+                w.blocks = 1;
+                if (PASS == kWeighSpanSums) {
+                    w.blocks = span_blocks(w.q);
+                    w.block *= w.blocks;
+                    w.blocks = min(w.blocks, w.q.blocks - w.block);
+                }
+                w.tile = part * chunk;
+                w.tiles = min(chunk, w.q.tiles - w.tile);
+                w.slot = lane_of(slots_upto - m, l) + (place * w.chunks) + part;
+                return w;
+            }
+            before = lane_of(upto, 63);
+            slots = lane_of(slots_upto, 63);
+        }
+        return w;
+    }
+};
+
+// Items of a workgroup: every `workers`-th, every other round from the other end, so
+// that a prompt's first blocks, which all rows see, and its last, which few do, come
+// to the same workgroups.
+__device__ __forceinline__ int weigh_item(const WeighArgs& a, int round) {
+    const int w = blockIdx.x;
+    return round * a.workers + (round & 1 ? a.workers - 1 - w : w);
 }
 
-__device__ __forceinline__ int weigh_end(const KvCache& c, int len) {
-    return static_cast<int>(min(static_cast<long long>(max(len, 0)), static_cast<long long>(c.max_pages) << c.page_shift));
+// sums over the 32 lanes of a half, of 32 numbers: lane e % 32 gets that of v[e]
+__device__ __forceinline__ float weigh_scatter(float (&v)[32]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[j]), __builtin_bit_cast(uint32_t, v[j + 16]), false, false);
+        v[j] = __builtin_bit_cast(float, static_cast<uint32_t>(r[0])) + __builtin_bit_cast(float, static_cast<uint32_t>(r[1]));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const bool up = lane & 8;
+        const float keep = up ? v[j + 8] : v[j], give = up ? v[j] : v[j + 8];
+        v[j] = keep + dpp<0x128, 0xF>(give);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool up = lane & 4;
+        const float keep = up ? v[j + 4] : v[j], give = up ? v[j] : v[j + 4];
+        v[j] = keep + dpp<0x141, 0xF>(give);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const bool up = lane & 2;
+        const float keep = up ? v[j + 2] : v[j], give = up ? v[j] : v[j + 2];
+        v[j] = keep + dpp<0x4E, 0xF>(give);
+    }
+    const bool up = lane & 1;
+    const float keep = up ? v[1] : v[0], give = up ? v[0] : v[1];
+    return keep + dpp<0xB1, 0xF>(give);
 }
 
-// a wave a row and q head
-template <int D>
-__global__ __launch_bounds__(64) void weigh_logs_kernel(WeighArgs a) {
-    const int row = blockIdx.x / a.q_heads, h = blockIdx.x % a.q_heads, lane = threadIdx.x;
+// a block's new mass: what token t had, and `sum`
+__device__ __forceinline__ void weigh_write(const WeighArgs& a, const WeighItem& w, int t, float sum) {
+    if (t >= w.q.written) return;
+    const size_t at = (static_cast<size_t>(w.seq) * a.c.kv_heads + w.head) * a.mass_tokens + t;
+    float before = 0.f;
+    if (a.mass && (w.q.all == 0 || t < w.q.s.first)) before = a.mass[at] * (w.q.all ? a.decay : 1.f);
+    a.out[at] = before + sum;
+}
+
+template <int D, WeighPass PASS>
+__global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
+    constexpr int kSlices = D / 8, kPer = kSlices * kWeighRows / 256;       // 8 dimensions of a row; a thread's pieces of a tile
+    constexpr std::integral_constant<WeighPass, PASS> pass;
+    __shared__ __align__(16) _Float16 rows[2][kSlices][kWeighRows][8];
+    __shared__ float sums[PASS == kWeighSpanSums ? 4 : 1][PASS == kWeighSpanSums ? kWeighMostTiles * kWeighRows : 1][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lrow = lane & 31, half = lane >> 5;
+    const float inverse_group = 1.f / static_cast<float>(a.group);
+    WeighSeq first;
+    const WeighPlan plan(a, first, pass);
+    const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
+    for (int round = 0;; ++round) {
+        if (static_cast<long long>(round) * a.workers >= plan.total) break;
+        const int x = weigh_item(a, round);
+        if (x >= plan.total) continue;
+        const WeighItem w = plan.find(a, first, x, pass);
+        const Span& s = w.q.s;
+        const int* table = a.c.pages + static_cast<size_t>(w.seq) * a.c.max_pages;
+        const int all_rows = s.n * a.group;
+        if constexpr (PASS == kWeighSpanSums) {
+            __syncthreads();
+            for (int i = lane; i < w.tiles * kWeighRows; i += 64) {
+                sums[wave][i][0] = kWeighNone;
+                sums[wave][i][1] = 0.f;
+            }
+        }
+        float total[32];
+        if constexpr (PASS == kWeighTokens)
+            for (float& t : total) t = 0.f;
+        for (int block = w.block; block < w.block + w.blocks; ++block) {
+            // the rows that see something of the block: tiles tile0 .. tile1 - 1
+            const int t_begin = block * kWeighBlock, t_end = min(t_begin + kWeighBlock, w.q.end);
+            int row_a = max(0, t_begin - s.first), row_b = s.n;
+            if (a.window > 0)
+                row_b = static_cast<int>(max(0ll, min(static_cast<long long>(row_b), static_cast<long long>(t_end) - 1 + a.window - s.first)));
+            int tile0 = max(w.tile, static_cast<int>(min(static_cast<long long>(row_a) * a.group, static_cast<long long>(all_rows)) / kWeighRows));
+            int tile1 = min(w.tile + w.tiles, static_cast<int>((static_cast<long long>(row_b) * a.group + kWeighRows - 1) / kWeighRows));
+            if (t_end <= t_begin) tile1 = tile0;
+            if (tile0 >= tile1) continue;
+            // the wave's 64 tokens
+            const int mine = t_begin + 64 * wave;
+            f16x8 k[2][D / 16];
+            float unit[4];                        // of 16 tokens each: scale of the scores
+            unsigned there = 0;                   // which of those have a page
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int token = mine + 32 * t + lrow;
+                const int page = token < t_end ? table[token >> a.c.page_shift] : -1;
+                const bool is = page >= 0 && page < a.c.num_pages;
+                const size_t ph = static_cast<size_t>(is ? page : 0) * a.c.kv_heads + w.head;
+                const int8_t* kp = a.c.k + ph * stride + (token & (a.c.page_tokens - 1)) * D + 16 * half;
+                u32x4 raw[D / 32];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) raw[c] = *reinterpret_cast<const u32x4*>(kp + 32 * c);
+                const float scale = a.c.scales[2 * ph] * a.scale;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    k[t][2 * c] = to_half8(raw[c][0], raw[c][1]);
+                    k[t][2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    unit[2 * t + g] = lane_of(scale, 16 * g);
+                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << (2 * t + g);
+                }
+            }
+            // Row r of the sequence is token r / group, head r % group; a tile's first row as both, uniform.
+            const int step_t = kWeighRows / a.group, step_g = kWeighRows - step_t * a.group;
+            struct TileAt {
+                int t, g;
+            };
+            auto at_tile = [&](int tile) {
+                const int r = tile * kWeighRows, t = r / a.group;
+                return TileAt{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(r - t * a.group)};
+            };
+            auto step = [&](TileAt& p) {
+                p.t += step_t;
+                p.g += step_g;
+                if (p.g >= a.group) {
+                    p.g -= a.group;
+                    ++p.t;
+                }
+            };
+            auto row_of = [&](const TileAt& p, int i, int& token) {
+                const int j = static_cast<int>((static_cast<float>(p.g + i) + 0.5f) * inverse_group);
+                token = p.t + j;
+                return w.head * a.group + p.g + i - j * a.group;
+            };
+            // a tile on its way, and the place of the next to load
+            u32x4 piece[kPer];
+            float log = 0.f, next_log = 0.f;
+            TileAt ahead = at_tile(tile0), now = ahead;
+            auto load = [&] {
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const int p = tid + 256 * u, i = p / kSlices;
+                    int token;
+                    const int h = row_of(ahead, i, token);
+                    piece[u] = u32x4{0, 0, 0, 0};
+                    if (token < s.n)
+                        piece[u] = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + p % kSlices * 8);
+                }
+                if constexpr (PASS == kWeighTokens) {
+                    int token;
+                    const int h = row_of(ahead, lrow, token);
+                    next_log = token < s.n ? a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + h] : INFINITY;
+                }
+                step(ahead);
+            };
+            // row i of slice c lies at i ^ c, so that neither a slice's rows nor a row's slices meet in a bank
+            auto store = [&](int b) {
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const int p = tid + 256 * u, i = p / kSlices, c = p % kSlices;
+                    *reinterpret_cast<f16x8*>(rows[b][c][i ^ c]) = query8(piece[u], 0);
+                }
+            };
+            load();
+            __syncthreads();                      // the block before is done with the rows
+            store(0);
+            log = next_log;
+            if (tile0 + 1 < tile1) load();
+            for (int tile = tile0; tile < tile1; ++tile) {
+                const int b = (tile - tile0) & 1;
+                __syncthreads();
+                const float my_log = log;
+                if (tile + 1 < tile1) {
+                    store(b ^ 1);
+                    log = next_log;
+                    if (tile + 2 < tile1) load();
+                }
+                f32x16 z[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int slice = 4 * c + 2 * half + u;
+                        const f16x8 q = *reinterpret_cast<const f16x8*>(rows[b][slice][lrow ^ slice]);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][2 * c + u], q, z[t], 0, 0, 0);
+                    }
+                // what the lane's row sees
+                int token;
+                row_of(now, lrow, token);
+                step(now);
+                const int position = s.first + token;
+                const bool is = token < s.n;
+                const int see_end = is ? min(position + 1, t_end) : 0;
+                const int see_begin = a.window > 0 ? max(position, 0) - a.window + 1 : 0;
+                const bool partly = __any(is && (mine < see_begin || mine + 64 > see_end)) || there != 15u;
+                if constexpr (PASS == kWeighSpanSums) {
+                    float top = kWeighNone;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int t = e / 16, i = e % 16;
+                        float v = z[t][i] * unit[2 * t + i / 8];
+                        if (partly) {
+                            const int at = mine + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+                            if (at < see_begin || at >= see_end || !(there >> (2 * t + i / 8) & 1)) v = -INFINITY;
+                        }
+                        z[t][i] = v;
+                        top = fmaxf(top, v);
+                    }
+                    const int r = (tile - w.tile) * kWeighRows + lrow;
+                    const float m0 = sums[wave][r][0], l0 = sums[wave][r][1];
+                    const float m = fmaxf(with_half(Larger(), top), m0);
+                    float l = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) l += fast_exp2(z[e / 16][e % 16] - m);
+                    l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
+                    if (half == 0) {
+                        sums[wave][r][0] = m;
+                        sums[wave][r][1] = l;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int t = e / 16, i = e % 16;
+                        float v = fast_exp2(__builtin_fmaf(z[t][i], unit[2 * t + i / 8], -my_log));
+                        if (partly) {
+                            const int at = mine + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+                            if (at < see_begin || at >= see_end || !(there >> (2 * t + i / 8) & 1)) v = 0.f;
+                        }
+                        total[e] += v;
+                    }
+                }
+            }
+        }
+        if constexpr (PASS == kWeighSpanSums) {
+            __syncthreads();
+            for (int r = tid; r < w.tiles * kWeighRows; r += 256) {
+                const int row = w.tile * kWeighRows + r;
+                if (row >= all_rows) break;
+                float m = kWeighNone, l = 0.f;
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, sums[i][r][0]);
+                for (int i = 0; i < 4; ++i) l += sums[i][r][1] * fast_exp2(sums[i][r][0] - m);
+                const int token = row / a.group, h = w.head * a.group + row - token * a.group;
+                float* to = a.spans + ((static_cast<size_t>(s.row0 + token) * a.q_heads + h) * kWeighSpans + w.block / WeighPlan::span_blocks(w.q)) * 2;
+                to[0] = m;
+                to[1] = l;
+            }
+        } else {
+            const float sum = weigh_scatter(total);
+            const int t = 64 * wave + 32 * (lrow >> 4) + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
+            if (w.chunks == 1) weigh_write(a, w, w.block * kWeighBlock + t, sum);
+            else a.parts[static_cast<size_t>(w.slot) * kWeighBlock + t] = sum;
+        }
+    }
+}
+
+// L of every row and head: a wave each, a span a lane
+__global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
+    const int lane = threadIdx.x & 63;
+    const long long x = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int row = static_cast<int>(x / a.q_heads);
+    if (row >= a.rows) return;
     const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, row, [](int start, int) { return start; });
     if (at.seq < 0 || row < at.s.row0 || row >= at.s.row0 + at.s.n) return;
-    const int position = at.s.first + row - at.s.row0, end = min(position + 1, weigh_end(a.c, at.s.len));
-    const int begin = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
-    const uint16_t* q = a.q + row * a.q_stride + h * D;
-    float m = -3e38f, l = 0.f;
-    bool there, bad = false;
-    for (int t = begin + lane; t < end; t += 64) {
-        const float s = weigh_score<D>(a, q, at.seq, t, h / a.group, &there);
-        if (!there) continue;
-        bad |= !(fabsf(s) < INFINITY);
-        const float n = fmaxf(m, s);
-        l = l * exp2f(m - n) + exp2f(s - n);
-        m = n;
+    const WeighSeq q(a, at.seq);
+    float m = kWeighNone, l = 0.f;
+    if (lane < WeighPlan::spans_of(q)) {
+        const f32x2 p = *reinterpret_cast<const f32x2*>(a.spans + (x * kWeighSpans + lane) * 2);
+        m = p[0];
+        l = p[1];
     }
     float top = m;
     for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
-    l = wave_all(Sum(), l * exp2f(m - top));
-    if (lane == 0) a.logs[static_cast<size_t>(row) * a.q_heads + h] = l > 0.f ? top + log2f(l) : 0.f;
-    if (__any(bad) && lane == 0) a.logs[static_cast<size_t>(row) * a.q_heads + h] = NAN;
+    l = wave_all(Sum(), l * fast_exp2(m - top));
+    if (lane == 0) a.logs[x] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
-// a thread a token of a cache head
-template <int D>
-__global__ __launch_bounds__(256) void weigh_add_kernel(WeighArgs a) {
-    const int blocks = (a.mass_tokens + 255) / 256, seq = blockIdx.x / (blocks * a.c.kv_heads);
-    const int head = blockIdx.x / blocks % a.c.kv_heads, t = blockIdx.x % blocks * 256 + threadIdx.x;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
-    const int all = max(min(max(a.starts[seq + 1], 0), a.rows) - s.row0, 0);
-    if (t >= a.mass_tokens || t >= a.c.lens[seq]) return;
-    const size_t place = (static_cast<size_t>(seq) * a.c.kv_heads + head) * a.mass_tokens + t;
-    float sum = 0.f;
-    if (t < weigh_end(a.c, s.len))
-        for (int i = max(0, t - s.first); i < s.n; ++i) {
-            const int position = s.first + i;
-            if (a.window > 0 && t <= position - a.window) break;
-            for (int g = 0; g < a.group; ++g) {
-                bool there;
-                const int h = head * a.group + g;
-                const float x = weigh_score<D>(a, a.q + (s.row0 + i) * a.q_stride + h * D, seq, t, head, &there);
-                if (there) sum += exp2f(x - a.logs[static_cast<size_t>(s.row0 + i) * a.q_heads + h]);
-            }
-        }
-    const float before = a.mass && (all == 0 || t < s.first) ? a.mass[place] * (all ? a.decay : 1.f) : 0.f;
-    a.out[place] = before + sum;
+// blocks whose rows were several items': the parts, in their order
+__global__ __launch_bounds__(256) void weigh_join_kernel(WeighArgs a) {
+    constexpr std::integral_constant<WeighPass, kWeighJoin> pass;
+    WeighSeq first;
+    const WeighPlan plan(a, first, pass);
+    for (int x = blockIdx.x; x < plan.total; x += a.workers) {
+        const WeighItem w = plan.find(a, first, x, pass);
+        const float* part = a.parts + static_cast<size_t>(w.slot) * kWeighBlock + threadIdx.x;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < w.chunks; ++i) sum += part[i * kWeighBlock];
+        weigh_write(a, w, w.block * kWeighBlock + threadIdx.x, sum);
+    }
 }
 
 }  // namespace tetra_dev
