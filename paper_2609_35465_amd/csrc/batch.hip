@@ -45,9 +45,8 @@ struct WeighSpace {
 template <int D>
 int weigh_launch(const tetra_dev::WeighArgs& a, hipStream_t stream) {
     const dim3 g(static_cast<unsigned>(a.workers)), b(256);
-    const long long logs = (static_cast<long long>(a.rows) * a.q_heads + 3) / 4;
     hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, b, 0, stream, a);
-    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(logs)), b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), b, 0, stream, a);
     hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, b, 0, stream, a);
     // several chunks of a sequence's rows only where it may have more than one tile of them
     if (static_cast<long long>(a.max_new) * a.group > tetra_dev::kWeighRows)

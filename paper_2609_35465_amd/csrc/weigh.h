@@ -35,7 +35,7 @@ struct WeighArgs {
     const int* starts;
     const float* mass;
     float* out;
-    float* spans;         // [rows][q_heads][kWeighSpans][2]: largest score and sum of a row over a span
+    float* spans;         // [kWeighSpans][rows][q_heads][2]: largest score and sum of a row over a span
     float* logs;          // [rows][q_heads]: L, +inf where a row sees nothing
     float* parts;         // [2 kWeighItems workers][kWeighBlock]: a block's sums over some of its rows
     long long q_stride;
@@ -377,44 +377,47 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                 const int position = s.first + token;
                 const bool is = token < s.n;
                 const int see_end = is ? min(position + 1, t_end) : 0;
-                const int see_begin = a.window > 0 ? max(position, 0) - a.window + 1 : 0;
+                const int see_begin = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
                 const bool partly = __any(is && (mine < see_begin || mine + 64 > see_end)) || there != 15u;
-                if constexpr (PASS == kWeighSpanSums) {
-                    float top = kWeighNone;
+                // token e of the lane is seen if e's place in the wave's 64 is in [lo, lo + n), of groups with a page
+                const unsigned lo = static_cast<unsigned>(see_begin - mine - 4 * half);
+                const unsigned n = static_cast<unsigned>(max(see_end - see_begin, 0));
+                unsigned seen[4];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int t = e / 16, i = e % 16;
-                        float v = z[t][i] * unit[2 * t + i / 8];
-                        if (partly) {
-                            const int at = mine + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
-                            if (at < see_begin || at >= see_end || !(there >> (2 * t + i / 8) & 1)) v = -INFINITY;
+                for (int g = 0; g < 4; ++g) seen[g] = there >> g & 1 ? n : 0;
+                auto unseen = [&](int e) { return static_cast<unsigned>(32 * (e / 16) + 8 * (e % 16 / 4) + e % 4) - lo >= seen[e / 8]; };
+                auto finish = [&](auto masked) {
+                    if constexpr (PASS == kWeighSpanSums) {
+                        float top = kWeighNone;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            float v = z[e / 16][e % 16] * unit[e / 8];
+                            if constexpr (masked) v = unseen(e) ? -INFINITY : v;
+                            z[e / 16][e % 16] = v;
+                            top = fmaxf(top, v);
                         }
-                        z[t][i] = v;
-                        top = fmaxf(top, v);
-                    }
-                    const int r = (tile - w.tile) * kWeighRows + lrow;
-                    const float m0 = sums[wave][r][0], l0 = sums[wave][r][1];
-                    const float m = fmaxf(with_half(Larger(), top), m0);
-                    float l = 0.f;
+                        const int r = (tile - w.tile) * kWeighRows + lrow;
+                        const float m0 = sums[wave][r][0], l0 = sums[wave][r][1];
+                        const float m = fmaxf(with_half(Larger(), top), m0);
+                        float l = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) l += fast_exp2(z[e / 16][e % 16] - m);
-                    l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
-                    if (half == 0) {
-                        sums[wave][r][0] = m;
-                        sums[wave][r][1] = l;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int t = e / 16, i = e % 16;
-                        float v = fast_exp2(__builtin_fmaf(z[t][i], unit[2 * t + i / 8], -my_log));
-                        if (partly) {
-                            const int at = mine + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
-                            if (at < see_begin || at >= see_end || !(there >> (2 * t + i / 8) & 1)) v = 0.f;
+                        for (int e = 0; e < 32; ++e) l += fast_exp2(z[e / 16][e % 16] - m);
+                        l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
+                        if (half == 0) {
+                            sums[wave][r][0] = m;
+                            sums[wave][r][1] = l;
                         }
-                        total[e] += v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            float v = fast_exp2(__builtin_fmaf(z[e / 16][e % 16], unit[e / 8], -my_log));
+                            if constexpr (masked) v = unseen(e) ? 0.f : v;
+                            total[e] += v;
+                        }
                     }
-                }
+                };
+                if (partly) finish(std::true_type());
+                else finish(std::false_type());
             }
         }
         if constexpr (PASS == kWeighSpanSums) {
@@ -426,9 +429,9 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, sums[i][r][0]);
                 for (int i = 0; i < 4; ++i) l += sums[i][r][1] * fast_exp2(sums[i][r][0] - m);
                 const int token = row / a.group, h = w.head * a.group + row - token * a.group;
-                float* to = a.spans + ((static_cast<size_t>(s.row0 + token) * a.q_heads + h) * kWeighSpans + w.block / WeighPlan::span_blocks(w.q)) * 2;
-                to[0] = m;
-                to[1] = l;
+                const size_t span = w.block / WeighPlan::span_blocks(w.q);
+                float* to = a.spans + ((span * a.rows + s.row0 + token) * a.q_heads + h) * 2;
+                *reinterpret_cast<f32x2*>(to) = f32x2{m, l};
             }
         } else {
             const float sum = weigh_scatter(total);
@@ -439,25 +442,36 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
     }
 }
 
-// L of every row and head: a wave each, a span a lane
+// L of a row: a head a lane, the spans in turns over four waves
 __global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long x = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int row = static_cast<int>(x / a.q_heads);
-    if (row >= a.rows) return;
+    __shared__ f32x2 part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
     const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, row, [](int start, int) { return start; });
     if (at.seq < 0 || row < at.s.row0 || row >= at.s.row0 + at.s.n) return;
-    const WeighSeq q(a, at.seq);
-    float m = kWeighNone, l = 0.f;
-    if (lane < WeighPlan::spans_of(q)) {
-        const f32x2 p = *reinterpret_cast<const f32x2*>(a.spans + (x * kWeighSpans + lane) * 2);
-        m = p[0];
-        l = p[1];
+    const int spans = WeighPlan::spans_of(WeighSeq(a, at.seq));
+    const size_t step = static_cast<size_t>(a.rows) * a.q_heads;
+    for (int h0 = 0; h0 < a.q_heads; h0 += 64) {
+        const int h = h0 + lane;
+        const f32x2* p = reinterpret_cast<const f32x2*>(a.spans) + static_cast<size_t>(row) * a.q_heads + h;
+        float m = kWeighNone, l = 0.f;
+        if (h < a.q_heads)
+#pragma unroll 4
+            for (int i = wave; i < spans; i += 4) {
+                const f32x2 x = p[i * step];
+                const float n = fmaxf(m, x[0]);
+                l = l * fast_exp2(m - n) + x[1] * fast_exp2(x[0] - n);
+                m = n;
+            }
+        __syncthreads();
+        part[wave][lane] = f32x2{m, l};
+        __syncthreads();
+        if (wave == 0 && h < a.q_heads) {
+            for (int i = 1; i < 4; ++i) m = fmaxf(m, part[i][lane][0]);
+            l = 0.f;
+            for (int i = 0; i < 4; ++i) l += part[i][lane][1] * fast_exp2(part[i][lane][0] - m);
+            a.logs[static_cast<size_t>(row) * a.q_heads + h] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+        }
     }
-    float top = m;
-    for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
-    l = wave_all(Sum(), l * fast_exp2(m - top));
-    if (lane == 0) a.logs[x] = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
 }
 
 // blocks whose rows were several items': the parts, in their order
