@@ -28,7 +28,10 @@ bool sizes_ok(const tetra_kv_cache* c) {
     return c->max_pages <= kMaxTokens / c->page_tokens && (c->head_dim == 64 || c->head_dim == 128);
 }
 
-constexpr int kWeighGroupsPerCU = 2;
+constexpr int kWeighGroupsPerCU = 2, kWeighFewGroupsPerCU = 4;
+
+// sequences of at most one row tile each: known from max_new
+bool weigh_few(int max_new, int group) { return static_cast<long long>(max_new) * group <= tetra_dev::kWeighRows; }
 
 // floats of kv_weigh's workspace
 struct WeighSpace {
@@ -38,19 +41,31 @@ struct WeighSpace {
         workers = cus * kWeighGroupsPerCU;
         logs = (static_cast<size_t>(rows) * q_heads + 63) / 64 * 64;
         spans = logs * tetra_dev::kWeighSpans * 2;
-        bytes = rounded(sizeof(float) * (spans + logs + 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock));
+        bytes = rounded(256 + sizeof(float) * (spans + logs + 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock));
     }
 };
 
 template <int D>
-int weigh_launch(const tetra_dev::WeighArgs& a, hipStream_t stream) {
-    const dim3 g(static_cast<unsigned>(a.workers)), b(256);
-    hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, b, 0, stream, a);
-    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), b, 0, stream, a);
-    hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, b, 0, stream, a);
-    // several chunks of a sequence's rows only where it may have more than one tile of them
-    if (static_cast<long long>(a.max_new) * a.group > tetra_dev::kWeighRows)
+int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
+    const bool few = weigh_few(a.max_new, a.group);
+    const dim3 b(256), g(static_cast<unsigned>(cus * (few ? kWeighFewGroupsPerCU : kWeighGroupsPerCU)));
+    a.workers = static_cast<int>(few ? 4 * g.x : g.x);
+    a.block = few ? 64 : tetra_dev::kWeighBlock;
+    a.spans_most = few ? tetra_dev::kWeighSpans : tetra_dev::kWeighSpans / 4;
+    const bool one = static_cast<long long>(a.max_new) * a.group <= 16;
+#define TETRA_WEIGH_FEW(PASS) \
+    if (one) hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 1>), g, b, 0, stream, a); \
+    else hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 2>), g, b, 0, stream, a)
+    if (few) { TETRA_WEIGH_FEW(tetra_dev::kWeighSpanSums); }
+    else hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, b, 0, stream, a);
+    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), dim3(64 * tetra_dev::kLogWaves), 0, stream, a);
+    if (few) {
+        TETRA_WEIGH_FEW(tetra_dev::kWeighTokens);
+    } else {
+        hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, b, 0, stream, a);
         hipLaunchKernelGGL(tetra_dev::weigh_join_kernel, g, b, 0, stream, a);
+    }
+#undef TETRA_WEIGH_FEW
     return launch_status();
 }
 
@@ -88,7 +103,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
         return TETRA_EALIGN;
     // items of a launch are counted in an int: the blocks of all heads, and kWeighItems times the workgroups
     const long long tokens = std::max<long long>(static_cast<long long>(a.c.max_pages) << a.c.page_shift, mass_tokens);
-    if ((tokens + 255) / 256 * a.c.kv_heads > (1 << 30) / a.c.seqs) return TETRA_EINVAL;
+    if ((tokens + 63) / 64 * a.c.kv_heads > (1 << 30) / a.c.seqs) return TETRA_EINVAL;
     int cus = 0;
     if (workspace_bytes < kMinWorkspace) return TETRA_EINVAL;
     if (int st = device_cus(&cus)) return st;
@@ -98,7 +113,8 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.starts = starts;
     a.mass = mass;
     a.out = mass_out;
-    a.spans = static_cast<float*>(workspace);
+    a.span = static_cast<int*>(workspace);
+    a.spans = static_cast<float*>(workspace) + 64;
     a.logs = a.spans + space.spans;
     a.parts = a.logs + space.logs;
     a.q_stride = q_stride;
@@ -110,8 +126,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
     a.mass_tokens = mass_tokens;
-    a.workers = space.workers;
-    return cache->head_dim == 64 ? weigh_launch<64>(a, stream) : weigh_launch<128>(a, stream);
+    return cache->head_dim == 64 ? weigh_launch<64>(a, cus, stream) : weigh_launch<128>(a, cus, stream);
 }
 
 size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to) {

@@ -24,7 +24,7 @@ namespace tetra_dev {
 
 constexpr int kWeighBlock = 256;          // tokens of a workgroup, 64 of a wave
 constexpr int kWeighRows = 32;            // rows of a tile
-constexpr int kWeighSpans = 64;           // of a sequence's tokens, for the sums, at most
+constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sums, at most
 constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
@@ -42,7 +42,9 @@ struct WeighArgs {
     float scale;          // scale log2(e)
     float decay;
     int rows, max_new, q_heads, group, window, mass_tokens;
-    int workers;          // workgroups of each launch but that of the logs
+    int workers;          // workgroups, or waves, that share the items of a launch
+    int block, spans_most;   // tokens of a block; spans of a sequence at most
+    int* span;               // the blocks of a span, at least, for the kernel of the logs
 };
 
 // What a sequence asks for.
@@ -63,7 +65,7 @@ struct WeighSeq {
         written = min(max(len, 0), a.mass_tokens);
         // a sequence that keeps what it has needs no visit where it has that already
         if (all == 0 && a.mass == a.out) written = 0;
-        blocks = (max(s.n ? end : 0, written) + kWeighBlock - 1) / kWeighBlock;
+        blocks = (max(s.n ? end : 0, written) + a.block - 1) / a.block;
         tiles = (s.n * a.group + kWeighRows - 1) / kWeighRows;
     }
 };
@@ -82,13 +84,15 @@ enum WeighPass { kWeighSpanSums, kWeighTokens, kWeighJoin };
 // more than twice that many have a part of a block's sums to leave.
 struct WeighPlan {
     int chunk, total;             // row tiles of a chunk; items
+    int span;                     // blocks of a span, at least
     int lane_items, lane_slots;   // of a lane's sequence, the first 64
 
-    __device__ __forceinline__ static int span_blocks(const WeighSeq& q) {
-        return max(1, (q.blocks + kWeighSpans - 1) / kWeighSpans);
+    __device__ __forceinline__ static int span_blocks(const WeighArgs& a, const WeighSeq& q, int least) {
+        return max(least, (q.blocks + a.spans_most - 1) / a.spans_most);
     }
-    __device__ __forceinline__ static int spans_of(const WeighSeq& q) {
-        return (q.blocks + span_blocks(q) - 1) / span_blocks(q);
+    __device__ __forceinline__ static int spans_of(const WeighArgs& a, const WeighSeq& q, int least) {
+        const int n = span_blocks(a, q, least);
+        return (q.blocks + n - 1) / n;
     }
     __device__ __forceinline__ int chunks_of(const WeighSeq& q) const { return max(1, (q.tiles + chunk - 1) / chunk); }
     __device__ __forceinline__ int slots_of(const WeighArgs& a, const WeighSeq& q) const {
@@ -97,21 +101,33 @@ struct WeighPlan {
     }
     template <WeighPass PASS>
     __device__ __forceinline__ int items_of(const WeighArgs& a, const WeighSeq& q) const {
-        if (PASS == kWeighSpanSums) return q.s.n ? spans_of(q) * a.c.kv_heads * chunks_of(q) : 0;
+        if (PASS == kWeighSpanSums) return spans_of(a, q, span) * a.c.kv_heads * chunks_of(q);
         if (PASS == kWeighTokens) return q.blocks * a.c.kv_heads * chunks_of(q);
         return chunks_of(q) > 1 ? q.blocks * a.c.kv_heads : 0;
     }
 
-    template <WeighPass PASS>
-    __device__ __forceinline__ WeighPlan(const WeighArgs& a, WeighSeq& mine, std::integral_constant<WeighPass, PASS>) {
+    template <WeighPass PASS, bool FEW>
+    __device__ __forceinline__ WeighPlan(const WeighArgs& a, WeighSeq& mine, std::integral_constant<WeighPass, PASS>,
+                                         std::integral_constant<bool, FEW>) {
         const int lane = threadIdx.x & 63;
-        unsigned long long steps = 0;
+        unsigned long long steps = 0, blocks = 0;
+        int live = 0;
         for (int i = lane; i < a.c.seqs; i += 64) {
             const WeighSeq q(a, i);
             if (i < 64) mine = q;
             steps += static_cast<unsigned long long>(q.blocks) * q.tiles * a.c.kv_heads;
+            blocks += q.blocks;
+            live += q.blocks > 0;
         }
         steps = wave_all(Sum(), steps);
+        span = 1;
+        if (FEW) {
+            // an item a wave, of equal spans: each sequence and head may have one that is not full
+            const long long ends = static_cast<long long>(wave_all(Sum(), live)) * a.c.kv_heads;
+            const long long room = max(static_cast<long long>(a.workers) - ends, static_cast<long long>(a.workers / 2));
+            blocks = wave_all(Sum(), blocks) * a.c.kv_heads;
+            span = static_cast<int>(max(1ll, min((static_cast<long long>(blocks) + room - 1) / room, 1ll << 24)));
+        }
         const unsigned long long most = static_cast<unsigned long long>(kWeighItems) * a.workers;
         chunk = static_cast<int>(max(1ull, min((steps + most - 1) / most, 1ull << 26)));
         if (PASS == kWeighSpanSums) chunk = min(chunk, kWeighMostTiles);
@@ -160,7 +176,7 @@ struct WeighPlan {
                 w.block = place / a.c.kv_heads;
                 w.blocks = 1;
                 if (PASS == kWeighSpanSums) {
-                    w.blocks = span_blocks(w.q);
+                    w.blocks = span_blocks(a, w.q, span);
                     w.block *= w.blocks;
                     w.blocks = min(w.blocks, w.q.blocks - w.block);
                 }
@@ -184,35 +200,29 @@ __device__ __forceinline__ int weigh_item(const WeighArgs& a, int round) {
     return round * a.workers + (round & 1 ? a.workers - 1 - w : w);
 }
 
-// sums over the 32 lanes of a half, of 32 numbers: lane e % 32 gets that of v[e]
-__device__ __forceinline__ float weigh_scatter(float (&v)[32]) {
+// sums over N (16 or 32) neighbouring lanes of N numbers: lane e of them gets that of v[e]
+template <int N>
+__device__ __forceinline__ float weigh_scatter(float (&v)[N]) {
     const int lane = threadIdx.x & 63;
+    if constexpr (N == 32)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[j]), __builtin_bit_cast(uint32_t, v[j + 16]), false, false);
-        v[j] = __builtin_bit_cast(float, static_cast<uint32_t>(r[0])) + __builtin_bit_cast(float, static_cast<uint32_t>(r[1]));
-    }
+        for (int j = 0; j < 16; ++j) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[j]), __builtin_bit_cast(uint32_t, v[j + 16]), false, false);
+            v[j] = __builtin_bit_cast(float, static_cast<uint32_t>(r[0])) + __builtin_bit_cast(float, static_cast<uint32_t>(r[1]));
+        }
+    auto halve = [&](int bit, auto other) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const bool up = lane & 8;
-        const float keep = up ? v[j + 8] : v[j], give = up ? v[j] : v[j + 8];
-        v[j] = keep + dpp<0x128, 0xF>(give);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool up = lane & 4;
-        const float keep = up ? v[j + 4] : v[j], give = up ? v[j] : v[j + 4];
-        v[j] = keep + dpp<0x141, 0xF>(give);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const bool up = lane & 2;
-        const float keep = up ? v[j + 2] : v[j], give = up ? v[j] : v[j + 2];
-        v[j] = keep + dpp<0x4E, 0xF>(give);
-    }
-    const bool up = lane & 1;
-    const float keep = up ? v[1] : v[0], give = up ? v[0] : v[1];
-    return keep + dpp<0xB1, 0xF>(give);
+        for (int j = 0; j < bit; ++j) {
+            const bool up = lane & bit;
+            const float keep = up ? v[j + bit] : v[j], give = up ? v[j] : v[j + bit];
+            v[j] = keep + other(give);
+        }
+    };
+    halve(8, [](float x) { return dpp<0x128, 0xF>(x); });
+    halve(4, [](float x) { return dpp<0x141, 0xF>(x); });
+    halve(2, [](float x) { return dpp<0x4E, 0xF>(x); });
+    halve(1, [](float x) { return dpp<0xB1, 0xF>(x); });
+    return v[0];
 }
 
 // a block's new mass: what token t had, and `sum`
@@ -234,7 +244,8 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
     const int lrow = lane & 31, half = lane >> 5;
     const float inverse_group = 1.f / static_cast<float>(a.group);
     WeighSeq first;
-    const WeighPlan plan(a, first, pass);
+    const WeighPlan plan(a, first, pass, std::false_type());
+    if (PASS == kWeighSpanSums && blockIdx.x == 0 && threadIdx.x == 0) *a.span = plan.span;
     const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
     for (int round = 0;; ++round) {
         if (static_cast<long long>(round) * a.workers >= plan.total) break;
@@ -429,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, sums[i][r][0]);
                 for (int i = 0; i < 4; ++i) l += sums[i][r][1] * fast_exp2(sums[i][r][0] - m);
                 const int token = row / a.group, h = w.head * a.group + row - token * a.group;
-                const size_t span = w.block / WeighPlan::span_blocks(w.q);
+                const size_t span = w.block / WeighPlan::span_blocks(a, w.q, plan.span);
                 float* to = a.spans + ((span * a.rows + s.row0 + token) * a.q_heads + h) * 2;
                 *reinterpret_cast<f32x2*>(to) = f32x2{m, l};
             }
@@ -442,13 +453,148 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
     }
 }
 
-// L of a row: a head a lane, the spans in turns over four waves
-__global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
-    __shared__ f32x2 part[4][64];
+// The same for sequences of up to 16 RT rows (single tokens), on v_mfma_f32_16x16x32_f16:
+// every wave for itself, a span of blocks of 64 tokens at a time, the rows in its
+// registers and the next block's keys on their way.  Tile t of four takes token 16 g +
+// 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the scores of
+// 16 neighbouring tokens, all of one page, for row lane % 16.
+template <int D, WeighPass PASS, int RT>
+__global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
+    constexpr std::integral_constant<WeighPass, kWeighSpanSums> pass;       // spans are the items both times
+    constexpr int C = D / 64;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x + gridDim.x * (threadIdx.x >> 6));
+    const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
+    WeighSeq first;
+    const WeighPlan plan(a, first, pass, std::true_type());
+    if (PASS == kWeighSpanSums && wave == 0 && lane == 0) *a.span = plan.span;
+    for (int x = wave; x < plan.total; x += a.workers) {
+        const WeighItem w = plan.find(a, first, x, pass);
+        const Span& s = w.q.s;
+        const int* table = a.c.pages + static_cast<size_t>(w.seq) * a.c.max_pages;
+        const int blocks_end = w.block + w.blocks;
+        auto page_at = [&](int t) { return t < w.q.end ? table[t >> a.c.page_shift] : -1; };
+        struct Keys {
+            u32x4 raw[4][C];
+            float scale;
+            bool there;
+        };
+        auto load = [&](Keys& k, int t0, int pk, int ps) {
+            const int tk = t0 + 16 * (r >> 2);
+            pk = pk < 0 || pk >= a.c.num_pages ? 0 : pk;
+            k.there = ps >= 0 && ps < a.c.num_pages;
+            const int8_t* kp = a.c.k + (static_cast<size_t>(pk) * a.c.kv_heads + w.head) * stride +
+                               ((tk & (a.c.page_tokens - 1)) + (r & 3)) * D + 16 * g;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < C; ++c) k.raw[t][c] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * c);
+            k.scale = a.c.scales[2 * (static_cast<size_t>(k.there ? ps : 0) * a.c.kv_heads + w.head)];
+        };
+        Keys k;
+        load(k, w.block * 64, page_at(w.block * 64 + 16 * (r >> 2)), page_at(w.block * 64 + 16 * g));
+        f16x8 q[RT][D / 32];
+        bool is[RT];
+        size_t row[RT];
+        int see_all[RT], see_begin[RT];
+        float m[RT], l[RT], log[RT];
+#pragma unroll
+        for (int n = 0; n < RT; ++n) {
+            const int i = 16 * n + r, token = i / a.group, h = w.head * a.group + i - token * a.group;
+            is[n] = token < s.n;
+            row[n] = static_cast<size_t>(s.row0 + token) * a.q_heads + h;
+            const int position = s.first + token;
+            see_all[n] = is[n] ? position + 1 : 0;
+            see_begin[n] = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                u32x4 v = {0, 0, 0, 0};
+                if (is[n])
+                    v = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + 64 * (c / 2) + 16 * g + 8 * (c % 2));
+                q[n][c] = query8(v, 0);
+            }
+            m[n] = kWeighNone;
+            l[n] = 0.f;
+            log[n] = INFINITY;
+            if (PASS == kWeighTokens && is[n]) log[n] = a.logs[row[n]];
+        }
+        for (int block = w.block; block < blocks_end; ++block) {
+            const int t0 = block * 64, mine = t0 + 16 * g;
+            const bool more = block + 1 < blocks_end;
+            int pk = -1, ps = -1;
+            if (more) {
+                pk = page_at(t0 + 64 + 16 * (r >> 2));
+                ps = page_at(t0 + 64 + 16 * g);
+            }
+            f32x4 z[RT][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int n = 0; n < RT; ++n) z[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const f16x8 k0 = to_half8(k.raw[t][c][0], k.raw[t][c][1]), k1 = to_half8(k.raw[t][c][2], k.raw[t][c][3]);
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) {
+                        z[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * c], z[n][t], 0, 0, 0);
+                        z[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * c + 1], z[n][t], 0, 0, 0);
+                    }
+                }
+            }
+            const float unit = k.scale * a.scale;
+            const bool there = k.there;
+            if (more) load(k, t0 + 64, pk, ps);
+            float total[16];
+#pragma unroll
+            for (int n = 0; n < RT; ++n) {
+                // the lane's tokens that its row sees: e in [lo, lo + seen)
+                const unsigned lo = static_cast<unsigned>(see_begin[n] - mine);
+                const unsigned seen = there ? static_cast<unsigned>(max(min(see_all[n], w.q.end) - see_begin[n], 0)) : 0u;
+                if constexpr (PASS == kWeighSpanSums) {
+                    float top = m[n];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float v = z[n][e / 4][e % 4] * unit;
+                        total[e] = static_cast<unsigned>(e) - lo >= seen ? -INFINITY : v;
+                        top = fmaxf(top, total[e]);
+                    }
+                    top = over_groups(Larger(), top);
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += fast_exp2(total[e] - top);
+                    l[n] = l[n] * fast_exp2(m[n] - top) + sum;      // of this lane's tokens
+                    m[n] = top;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float v = fast_exp2(__builtin_fmaf(z[n][e / 4][e % 4], unit, -log[n]));
+                        v = static_cast<unsigned>(e) - lo >= seen ? 0.f : v;
+                        total[e] = n ? total[e] + v : v;
+                    }
+                }
+            }
+            if constexpr (PASS == kWeighTokens) weigh_write(a, w, mine + r, weigh_scatter(total));
+        }
+        if constexpr (PASS == kWeighSpanSums) {
+            const size_t span = w.block / WeighPlan::span_blocks(a, w.q, plan.span);
+#pragma unroll
+            for (int n = 0; n < RT; ++n) {
+                const float sum = over_groups(Sum(), l[n]);
+                if (is[n] && g == 0)
+                    *reinterpret_cast<f32x2*>(a.spans + (span * a.rows * a.q_heads + row[n]) * 2) = f32x2{m[n], sum};
+            }
+        }
+    }
+}
+
+// L of a row: a head a lane, the spans in turns over the waves
+constexpr int kLogWaves = 8;
+__global__ __launch_bounds__(kLogWaves * 64) void weigh_logs_kernel(WeighArgs a) {
+    __shared__ f32x2 part[kLogWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
     const Place at = locate(a.starts, a.c.lens, a.rows, a.max_new, a.c.seqs, row, [](int start, int) { return start; });
     if (at.seq < 0 || row < at.s.row0 || row >= at.s.row0 + at.s.n) return;
-    const int spans = WeighPlan::spans_of(WeighSeq(a, at.seq));
+    const int spans = WeighPlan::spans_of(a, WeighSeq(a, at.seq), *a.span);
     const size_t step = static_cast<size_t>(a.rows) * a.q_heads;
     for (int h0 = 0; h0 < a.q_heads; h0 += 64) {
         const int h = h0 + lane;
@@ -456,7 +602,7 @@ __global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
         float m = kWeighNone, l = 0.f;
         if (h < a.q_heads)
 #pragma unroll 4
-            for (int i = wave; i < spans; i += 4) {
+            for (int i = wave; i < spans; i += kLogWaves) {
                 const f32x2 x = p[i * step];
                 const float n = fmaxf(m, x[0]);
                 l = l * fast_exp2(m - n) + x[1] * fast_exp2(x[0] - n);
@@ -466,9 +612,9 @@ __global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
         part[wave][lane] = f32x2{m, l};
         __syncthreads();
         if (wave == 0 && h < a.q_heads) {
-            for (int i = 1; i < 4; ++i) m = fmaxf(m, part[i][lane][0]);
+            for (int i = 1; i < kLogWaves; ++i) m = fmaxf(m, part[i][lane][0]);
             l = 0.f;
-            for (int i = 0; i < 4; ++i) l += part[i][lane][1] * fast_exp2(part[i][lane][0] - m);
+            for (int i = 0; i < kLogWaves; ++i) l += part[i][lane][1] * fast_exp2(part[i][lane][0] - m);
             a.logs[static_cast<size_t>(row) * a.q_heads + h] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
         }
     }
@@ -478,7 +624,7 @@ __global__ __launch_bounds__(256) void weigh_logs_kernel(WeighArgs a) {
 __global__ __launch_bounds__(256) void weigh_join_kernel(WeighArgs a) {
     constexpr std::integral_constant<WeighPass, kWeighJoin> pass;
     WeighSeq first;
-    const WeighPlan plan(a, first, pass);
+    const WeighPlan plan(a, first, pass, std::false_type());
     for (int x = blockIdx.x; x < plan.total; x += a.workers) {
         const WeighItem w = plan.find(a, first, x, pass);
         const float* part = a.parts + static_cast<size_t>(w.slot) * kWeighBlock + threadIdx.x;
