@@ -155,8 +155,11 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
     a.mass_tokens = mass_tokens;
     a.out_tokens = out_tokens;
     a.recent = recent;
-    hipLaunchKernelGGL(tetra_dev::evict_choose_kernel, dim3(static_cast<unsigned>(units)), dim3(tetra_dev::kEvictThreads), 0,
-                       stream, a);
+    const dim3 u(static_cast<unsigned>(units)), t(tetra_dev::kEvictThreads);
+    if (static_cast<long long>(a.from.max_pages) << a.from.page_shift <= 8 * tetra_dev::kEvictThreads)
+        hipLaunchKernelGGL(tetra_dev::evict_choose_kernel<8>, u, t, 0, stream, a);
+    else
+        hipLaunchKernelGGL(tetra_dev::evict_choose_kernel<64>, u, t, 0, stream, a);
     const dim3 g(static_cast<unsigned>(units * a.to.max_pages * 2));
     if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, dim3(256), 0, stream, a);
