@@ -69,6 +69,23 @@ int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
     return launch_status();
 }
 
+// Places of kv_evict's workspace.  A sequence and head whose weights a workgroup holds in
+// registers is one workgroup's; longer ones are cut in parts, up to four workgroups
+// a CU: 8 heads of 131,072 tokens @@
+struct EvictSpace {
+    int parts;            // 0: not cut
+    size_t tokens, state, bytes;
+    EvictSpace(const tetra_kv_cache* from, const tetra_kv_cache* to) {
+        const size_t units = static_cast<size_t>(from->seqs) * from->kv_heads;
+        parts = 0;
+        if (static_cast<long long>(from->max_pages) * from->page_tokens > tetra_dev::kEvictHeld * tetra_dev::kEvictThreads)
+            parts = static_cast<int>(std::max<size_t>(1, std::min<size_t>(tetra_dev::kEvictParts, 512 / units)));
+        tokens = units * to->max_pages * to->page_tokens;
+        state = (2 * units * (2 + parts) + 63) / 64 * 64;
+        bytes = rounded(sizeof(int) * (tokens + state + 3 * units * parts * tetra_dev::kEvictBins));
+    }
+};
+
 template <class T, bool TOP>
 int score_launch(const tetra_dev::ScoreArgs& a, hipStream_t stream) {
     if (static_cast<long long>(a.rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
@@ -131,7 +148,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
 
 size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to) {
     if (!sizes_ok(from) || !sizes_ok(to)) return 0;
-    return rounded(sizeof(int) * from->seqs * from->kv_heads * to->max_pages * to->page_tokens);
+    return EvictSpace(from, to).bytes;
 }
 
 int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const float* mass, int mass_tokens, int recent,
@@ -145,9 +162,10 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
     if (!mass || !workspace || mass_tokens < 1 || recent < 0 || (mass_out && out_tokens < 1) || mass_out == mass)
         return TETRA_EINVAL;
     if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(workspace, 256)) return TETRA_EALIGN;
-    if (workspace_bytes < tetra_kv_evict_workspace_bytes(from, to)) return TETRA_EINVAL;
+    const EvictSpace space(from, to);
+    if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     const long long units = static_cast<long long>(a.from.seqs) * a.from.kv_heads;
-    if (units > kMaxGrid / 2 / a.to.max_pages) return TETRA_EINVAL;
+    if (units > kMaxGrid / 16 / a.to.max_pages) return TETRA_EINVAL;
     a.mass = mass;
     a.out = mass_out;
     a.tokens = static_cast<int*>(workspace);
@@ -155,14 +173,22 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
     a.mass_tokens = mass_tokens;
     a.out_tokens = out_tokens;
     a.recent = recent;
+    a.state = a.tokens + space.tokens;
+    a.bins = reinterpret_cast<unsigned*>(a.state + space.state);
+    a.parts = space.parts;
     const dim3 u(static_cast<unsigned>(units)), t(tetra_dev::kEvictThreads);
-    if (static_cast<long long>(a.from.max_pages) << a.from.page_shift <= 8 * tetra_dev::kEvictThreads)
-        hipLaunchKernelGGL(tetra_dev::evict_choose_kernel<8>, u, t, 0, stream, a);
-    else
-        hipLaunchKernelGGL(tetra_dev::evict_choose_kernel<64>, u, t, 0, stream, a);
-    const dim3 g(static_cast<unsigned>(units * a.to.max_pages * 2));
-    if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, dim3(256), 0, stream, a);
+    if (space.parts == 0) {
+        hipLaunchKernelGGL(tetra_dev::evict_choose_kernel, u, t, 0, stream, a);
+    } else {
+        const dim3 p(static_cast<unsigned>(units * space.parts));
+        hipLaunchKernelGGL(tetra_dev::evict_part_kernel<0>, p, t, 0, stream, a);
+        hipLaunchKernelGGL(tetra_dev::evict_part_kernel<1>, p, t, 0, stream, a);
+        hipLaunchKernelGGL(tetra_dev::evict_part_kernel<2>, p, t, 0, stream, a);
+        hipLaunchKernelGGL(tetra_dev::evict_part_kernel<3>, p, t, 0, stream, a);
+    }
+    const dim3 g(static_cast<unsigned>(units * a.to.max_pages));
+    if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, dim3(512), 0, stream, a);
+    else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, dim3(512), 0, stream, a);
     return launch_status();
 }
 

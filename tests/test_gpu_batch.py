@@ -507,6 +507,19 @@ def test_evict_long(recent, kept):
     _check_evict(Cache(42, [20001, 1500], 2, 64, 64), [kept, 700], recent)
 
 
+@pytest.mark.parametrize("seqs", [3, 100, 300])
+def test_evict_tables_for_long_sequences(seqs):
+    """Tables with room for more than 8,192 tokens: rows are cut in parts, few or one of them where sequences are many;
+    short ones leave parts without tokens."""
+    rng = np.random.default_rng(3)
+    lens = [int(n) for n in rng.integers(0, 300, seqs)]
+    lens[1] = 9000
+    kept = [int(n) for n in rng.integers(0, 300, seqs)]
+    kept[1] = 4000
+    print(f"[evict wide] seqs={seqs}", flush=True)
+    _check_evict(Cache(52, lens, 2, 16, 64, max_pages=700), kept, 12)
+
+
 def test_evict_ties_and_not_finite_weights():
     """Equal weights go by the first token; NaN is the least, zeros of both signs are equal, infinities as they are."""
     c = Cache(43, [700, 700, 700, 700], 2, 16, 64)
