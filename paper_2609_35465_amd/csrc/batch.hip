@@ -186,9 +186,9 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
         hipLaunchKernelGGL(tetra_dev::evict_part_kernel<2>, p, t, 0, stream, a);
         hipLaunchKernelGGL(tetra_dev::evict_part_kernel<3>, p, t, 0, stream, a);
     }
-    const dim3 g(static_cast<unsigned>(units * a.to.max_pages));
-    if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, dim3(512), 0, stream, a);
-    else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, dim3(512), 0, stream, a);
+    const dim3 g(static_cast<unsigned>((units * a.to.max_pages * 2 * (to->page_tokens / tetra_dev::kGroupTokens) + 3) / 4)), m(256);
+    if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, m, 0, stream, a);
+    else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, m, 0, stream, a);
     return launch_status();
 }
 

@@ -199,17 +199,16 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a) 
         }
         const int b = kEvictBins - 2 - 2 * tid;
         unsigned hi = 0, lo = 0, hi_before = 0, lo_before = 0;
+        u32x2 c[kEvictParts];                  // all on their way at once
 #pragma unroll
-        for (int p = 0; p < kEvictParts; ++p)
-            if (p < a.parts) {
-                const u32x2 c = *reinterpret_cast<const u32x2*>(bins(PASS - 1, p) + b);
-                if (p < mine) {
-                    hi_before += c[1];
-                    lo_before += c[0];
-                }
-                hi += c[1];
-                lo += c[0];
-            }
+        for (int p = 0; p < kEvictParts; ++p) c[p] = *reinterpret_cast<const u32x2*>(bins(PASS - 1, min(p, a.parts - 1)) + b);
+#pragma unroll
+        for (int p = 0; p < kEvictParts; ++p) {
+            hi += p < a.parts ? c[p][1] : 0;
+            lo += p < a.parts ? c[p][0] : 0;
+            hi_before += p < mine ? c[p][1] : 0;
+            lo_before += p < mine ? c[p][0] : 0;
+        }
         const unsigned upto = wave_upto(Sum(), hi + lo);
         if (lane == 63) above[wave] = upto;
         __syncthreads();
@@ -307,83 +306,135 @@ __device__ __forceinline__ uint32_t moved4(uint32_t q, float ratio) {
     return w;
 }
 
-// A new page of a head: half of the workgroup its keys, the other its values.  Keys are
-// rows of D bytes, moved in pieces of 16.  Of values a thread takes a dimension of 16
-// places, whose bytes lie in as many groups of 16 old tokens as the kept ones do: they are
-// loaded one by one, all at once.
+// 16 places of a new page and head, keys or values: a wave each, for itself.  Every wave
+// finds the page's scale from the scales of all its tokens, while what it moves is on its
+// way.  Keys are rows of D bytes, moved in pieces of 16.  Of values a lane takes a
+// dimension of the 16 places, whose bytes lie in as many groups of 16 old tokens as the
+// kept ones do: it loads those groups' 16 bytes and picks from them with byte permutes,
+// whose selectors are the same for all dimensions.  (Bytes loaded one by one took 73
+// cycles of a CU for each load of a wave.)
 template <int D>
-__global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a) {
-    __shared__ int from[128], where[128];
-    __shared__ float ratio[2][128], largest[2][4];
-    const int kind = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
-    int rest = blockIdx.x;
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
+    const int lane = threadIdx.x & 63, B = a.to.page_tokens, groups = B / kGroupTokens;
+    unsigned rest = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = rest % groups;
+    rest /= groups;
+    const int kind = rest & 1;
+    rest >>= 1;
     const int head = rest % a.from.kv_heads;
     rest /= a.from.kv_heads;
     const int seq = rest / a.to.max_pages, number = rest - seq * a.to.max_pages;
-    const int B = a.to.page_tokens, first = number * B;
+    if (seq >= a.from.seqs) return;
     const int page = a.to.pages[static_cast<size_t>(seq) * a.to.max_pages + number];
     const EvictShape s = evict_shape(a, seq);
-    const int n = min(B, s.kept - first);
-    if (n <= 0 || page < 0 || page >= a.to.num_pages) return;
-    const int* tokens = a.tokens + (static_cast<size_t>(seq) * a.from.kv_heads + head) * a.capacity + first;
-    float mine = 0.f;
-    int token = -1, source = 0;
-    if (tid < n) {
-        const int t = tokens[tid], p = a.from.pages[static_cast<size_t>(seq) * a.from.max_pages + (t >> a.from.page_shift)];
-        if (p >= 0 && p < a.from.num_pages) {
-            token = t;
-            source = p;
-            mine = a.from.scales[2 * (static_cast<size_t>(p) * a.from.kv_heads + head) + kind];
-        }
-    }
-    const float top = wave_all(Max(), mine);
-    if ((tid & 63) == 0) largest[kind][tid >> 6] = top;
-    __syncthreads();
-    const float grown = fmaxf(fmaxf(largest[kind][0], largest[kind][1]), fmaxf(largest[kind][2], largest[kind][3]));
-    if (tid < B) {
-        if (kind == 0) {
-            from[tid] = token;
-            where[tid] = source;
-        }
-        ratio[kind][tid] = grown > 0.f ? mine / grown : 0.f;
-    }
-    __syncthreads();
-    const size_t stride = static_cast<size_t>(B) * D, to = (static_cast<size_t>(page) * a.to.kv_heads + head) * stride;
-    if (tid == 0) a.to.scales[2 * (static_cast<size_t>(page) * a.to.kv_heads + head) + kind] = grown;
-    auto page_of = [&](int i) { return (static_cast<size_t>(where[i]) * a.from.kv_heads + head) * stride; };
+    const int n = min(B, s.kept - number * B), n_group = min(kGroupTokens, n - kGroupTokens * group);
+    if (n_group <= 0 || page < 0 || page >= a.to.num_pages) return;
+    const int* tokens = a.tokens + (static_cast<size_t>(seq) * a.from.kv_heads + head) * a.capacity + static_cast<size_t>(number) * B;
+    const int* table = a.from.pages + static_cast<size_t>(seq) * a.from.max_pages;
+    const size_t stride = static_cast<size_t>(B) * D;
+    auto page_of = [&](int t) {
+        const int p = table[t >> a.from.page_shift];
+        return p >= 0 && p < a.from.num_pages ? p : -1;
+    };
+    auto head_of = [&](int p) { return static_cast<size_t>(p) * a.from.kv_heads + head; };
+    auto scale_of = [&](int p) { return p >= 0 ? a.from.scales[2 * head_of(p) + kind] : 0.f; };
+    // the wave's tokens, in each 16 lanes; then the page's
+    const int i = lane & 15, t = i < n_group ? tokens[kGroupTokens * group + i] : -1;
+    const int t_lo = lane < n ? tokens[lane] : -1, t_hi = lane + 64 < n ? tokens[lane + 64] : -1;
+    const int p = t >= 0 ? page_of(t) : -1;
+    const int p_lo = t_lo >= 0 ? page_of(t_lo) : -1, p_hi = t_hi >= 0 ? page_of(t_hi) : -1;
+    constexpr int kPer = kGroupTokens * D / 16 / 64;
+    u32x4 piece[kPer];
+    const int t0 = __builtin_amdgcn_readfirstlane(t), p0 = __builtin_amdgcn_readfirstlane(p);
     if (kind == 0) {
-        constexpr int kPieces = D / 16;
-#pragma unroll 4
-        for (int e = tid; e < n * kPieces; e += 256) {
-            const int i = e / kPieces, c = e % kPieces, t = from[i];
-            u32x4 q = {0, 0, 0, 0};
-            if (t >= 0) q = *reinterpret_cast<const u32x4*>(a.from.k + page_of(i) + (t & (B - 1)) * D + 16 * c);
-            const float f = ratio[0][i];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int at = (64 * u + lane) / (D / 16), tj = __shfl(t, at, 64), pj = __shfl(p, at, 64);
+            piece[u] = u32x4{0, 0, 0, 0};
+            if (pj >= 0)
+                piece[u] = *reinterpret_cast<const u32x4*>(a.from.k + head_of(pj) * stride + (tj & (B - 1)) * D + 16 * (lane % (D / 16)));
+        }
+    } else {
+        auto old_group = [&](int tj, int pj, u32x4 (&to)[kPer]) {
+#pragma unroll
+            for (int u = 0; u < kPer; ++u)
+                to[u] = *reinterpret_cast<const u32x4*>(a.from.v + head_of(pj) * stride + (tj & (B - 1) & ~15) * D + (64 * u + lane) * 16);
+        };
+        if (p0 >= 0 && (t0 & 15) == 0 && __all(t == t0 + i)) {
+            old_group(t0, p0, piece);
+        } else {
+            // Where the next old group begins among the places (those without a page left out), four on their way at
+            // once.  Lane 4 k + w has how word w of an old group goes into word k: its byte, or the one that is there.
+            const int before = __shfl(t, i ? i - 1 : 0, 64);
+            unsigned begins = __ballot(p >= 0 && (i == 0 || t >> 4 != before >> 4)) & 0xFFFF;
+            int word_t[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) word_t[b] = __shfl(t, (lane & 12) + b, 64);
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) piece[u] = u32x4{0, 0, 0, 0};
+            while (begins) {
+                u32x4 old[4][kPer];
+                int group_t[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    group_t[m] = -1;
+                    if (begins) {
+                        const int j = __builtin_ctz(begins);
+                        begins &= begins - 1;
+                        group_t[m] = __builtin_amdgcn_readlane(t, j);
+                        old_group(group_t[m], __builtin_amdgcn_readlane(p, j), old[m]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (group_t[m] < 0) break;
+                    uint32_t choice = 0x07060504u;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (word_t[b] >> 2 == (group_t[m] >> 4) * 4 + (lane & 3))
+                            choice = (choice & ~(0xFFu << (8 * b))) | static_cast<uint32_t>(word_t[b] & 3) << (8 * b);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t c = __builtin_amdgcn_readlane(choice, 4 * k + w);
+#pragma unroll
+                            for (int u = 0; u < kPer; ++u) piece[u][k] = __builtin_amdgcn_perm(piece[u][k], old[m][u][w], c);
+                        }
+                }
+            }
+        }
+    }
+    const float mine = scale_of(p), grown = wave_all(Max(), fmaxf(scale_of(p_lo), scale_of(p_hi)));
+    const float ratio = grown > 0.f ? mine / grown : 0.f;
+    const size_t to = static_cast<size_t>(page) * a.to.kv_heads + head;
+    if (group == 0 && lane == 0) a.to.scales[2 * to + kind] = grown;
+    if (kind == 0) {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int at = (64 * u + lane) / (D / 16);
+            const float f = __shfl(ratio, at, 64);
             if (f != 1.f)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) q[k] = moved4(q[k], f);
-            *reinterpret_cast<u32x4*>(a.to.k + to + i * D + 16 * c) = q;
+                for (int k = 0; k < 4; ++k) piece[u][k] = moved4(piece[u][k], f);
+            if (at < n_group)
+                *reinterpret_cast<u32x4*>(a.to.k + to * stride + (kGroupTokens * group + at) * D + 16 * (lane % (D / 16))) = piece[u];
         }
         return;
     }
-    constexpr int kGroups = 256 / D;                            // groups of 16 places at once: of a wave all the same
-    const int d = tid % D;
-    for (int g = __builtin_amdgcn_readfirstlane(tid / D); 16 * g < n; g += kGroups) {
-        int x[16];
+    if (__any(ratio != 1.f && i < n_group))
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const int t = 16 * g + j < n ? __builtin_amdgcn_readfirstlane(from[16 * g + j]) : -1;
-            x[j] = 0;
-            if (t >= 0) x[j] = a.from.v[page_of(16 * g + j) + (t & (B - 1) & ~15) * D + d * 16 + (t & 15)];
-        }
-        u32x4 q = {0, 0, 0, 0};
+            const float f = lane_of(ratio, j);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int v = requantized(x[j], 16 * g + j < n ? ratio[1][16 * g + j] : 0.f);
-            q[j / 4] |= static_cast<uint32_t>(v & 0xFF) << (8 * (j % 4));
+            for (int u = 0; u < kPer; ++u) {
+                const int q = requantized(static_cast<int8_t>(piece[u][j / 4] >> (8 * (j % 4))), f);
+                piece[u][j / 4] = (piece[u][j / 4] & ~(0xFFu << (8 * (j % 4)))) | static_cast<uint32_t>(q & 0xFF) << (8 * (j % 4));
+            }
         }
-        *reinterpret_cast<u32x4*>(a.to.v + to + 16 * g * D + d * 16) = q;
-    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+        *reinterpret_cast<u32x4*>(a.to.v + to * stride + kGroupTokens * group * D + (64 * u + lane) * 16) = piece[u];
 }
 
 }  // namespace tetra_dev
