@@ -10,6 +10,8 @@
 // (token, q head of the group) in that order.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_cache.h"
 
 namespace tetra_dev {
@@ -27,6 +29,19 @@ struct AttendArgs {
     int rows, max_new, q_heads, group, window;
     int few_tile;     // tokens of a tile of attend_few: 64 for each wave of its workgroups
     int few_most;     // sequences of up to so many rows (token, q head of a group) go through attend_few_kernel
+    // of a batch with shared prefixes (shared.h)
+    const struct SharedSeq* seqs;
+    float *results, *stats;
+    int num_seqs;
+};
+
+// Where a batch shares prefixes, what takes the place of its sequences: the groups, whose
+// rows all see the shared tokens, and the sequences with their own tokens.
+struct SharedSeq {
+    int row0, n, first, len;     // as in Span
+    int begin, end;              // the tokens that its rows may see
+    int table;                   // the sequence whose pages those are
+    int side;                    // of the results: 0 shared, 1 own
 };
 
 constexpr float kNoScore = -3e38f;   // a maximum over no score
@@ -140,6 +155,43 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs& a, const Span& s) {
     return r;
 }
 
+// A sequence as the kernels below know it, for a plain batch (its span) and for one with
+// shared prefixes.
+template <bool SHARED>
+using AttendSeq = std::conditional_t<SHARED, SharedSeq, Span>;
+
+template <bool SHARED>
+__device__ __forceinline__ int num_seqs(const AttendArgs& a) { return SHARED ? a.num_seqs : a.c.seqs; }
+
+template <bool SHARED>
+__device__ __forceinline__ AttendSeq<SHARED> seq_at(const AttendArgs& a, int i) {
+    if constexpr (SHARED) return a.seqs[i];
+    else return span_of(a.starts, a.c.lens, a.rows, a.max_new, i);
+}
+__device__ __forceinline__ Reach reach_of(const AttendArgs&, const SharedSeq& s) { return {s.begin, s.end}; }
+__device__ __forceinline__ int table_of(const Span&, int seq) { return seq; }
+__device__ __forceinline__ int table_of(const SharedSeq& s, int) { return s.table; }
+
+// the same in every lane: that of lane l, or one that is known to be
+__device__ __forceinline__ Span of_lane(const Span& s, int l) {
+    return {lane_of(s.row0, l), lane_of(s.n, l), lane_of(s.first, l), lane_of(s.len, l)};
+}
+__device__ __forceinline__ SharedSeq of_lane(const SharedSeq& s, int l) {
+    return {lane_of(s.row0, l), lane_of(s.n, l), lane_of(s.first, l), lane_of(s.len, l),
+            lane_of(s.begin, l), lane_of(s.end, l), lane_of(s.table, l), lane_of(s.side, l)};
+}
+
+// Sums of a row and head of a batch with shared prefixes, not yet divided: `o` are those
+// of dimensions d .. d + 3.
+__device__ __forceinline__ void put_result(const AttendArgs& a, const SharedSeq& s, int token, int head, int dim, int d, f32x4 o) {
+    const size_t at = (static_cast<size_t>(s.side) * a.rows + s.row0 + token) * a.q_heads + head;
+    *reinterpret_cast<f32x4*>(a.results + at * dim + d) = o;
+}
+__device__ __forceinline__ void put_stats(const AttendArgs& a, const SharedSeq& s, int token, int head, float m, float l) {
+    const size_t at = (static_cast<size_t>(s.side) * a.rows + s.row0 + token) * a.q_heads + head;
+    *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{m, l};
+}
+
 // tiles of a sequence's unit (one at least, so that rows without keys are
 // written) and its units
 __device__ __forceinline__ int few_tiles(const AttendArgs& a, const Reach& r) {
@@ -147,12 +199,14 @@ __device__ __forceinline__ int few_tiles(const AttendArgs& a, const Reach& r) {
 }
 
 // row tiles of a sequence: none if it goes through attend_many_kernel
-__device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Span& s) {
+template <class Seq>
+__device__ __forceinline__ int few_row_tiles(const AttendArgs& a, const Seq& s) {
     const int rows = s.n * a.group;
     return rows > a.few_most ? 0 : (rows + kFewRows - 1) / kFewRows;
 }
 
-__device__ __forceinline__ int few_work(const AttendArgs& a, const Span& s) {
+template <class Seq>
+__device__ __forceinline__ int few_work(const AttendArgs& a, const Seq& s) {
     return few_row_tiles(a, s) * a.c.kv_heads * few_tiles(a, reach_of(a, s));
 }
 
@@ -294,23 +348,24 @@ __device__ __forceinline__ void few_segment(const AttendArgs& a, FewState<D>& st
     }
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, bool SHARED = false>
 struct FewLds {
     float sums[WAVES][kFewRows][D + 4];
     float stat[WAVES][kFewRows][2];
     int lds[WAVES], found[2];
-    Span span;
+    AttendSeq<SHARED> span;
 };
 
 // workgroup w of `launched`, WAVES waves each (a.few_tile is 64 WAVES)
-template <int D, int WAVES>
-__device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launched, FewLds<D, WAVES>& sh) {
+template <int D, int WAVES, bool SHARED = false>
+__device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launched, FewLds<D, WAVES, SHARED>& sh) {
     constexpr int kTile = 64 * WAVES;      // tokens, and threads
     auto& sums = sh.sums;
     auto& stat = sh.stat;
     auto& lds = sh.lds;
     auto& found = sh.found;
-    Span& found_span = sh.span;
+    auto& found_span = sh.span;
+    const int seqs = num_seqs<SHARED>(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     // The total, and the sequence that holds this workgroup's first tile with the
@@ -327,17 +382,17 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
         }
         return upto;
     };
-    Span mine = {};
+    AttendSeq<SHARED> mine = {};
     int n0 = 0;
-    if (tid < a.c.seqs) {
-        mine = span_of(a.starts, a.c.lens, a.rows, a.max_new, tid);
+    if (tid < seqs) {
+        mine = seq_at<SHARED>(a, tid);
         n0 = few_work(a, mine);
     }
     int all, upto = scan(n0, all), total = all;
-    if (a.c.seqs > kTile) {
+    if (seqs > kTile) {
         int more = 0;
-        for (int i = tid + kTile; i < a.c.seqs; i += kTile)
-            more += few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
+        for (int i = tid + kTile; i < seqs; i += kTile)
+            more += few_work(a, seq_at<SHARED>(a, i));
         total += few_sum<WAVES>(more, lds);
     }
     const FewPlan plan(__builtin_amdgcn_readfirstlane(total), launched);
@@ -351,28 +406,24 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
         }
         before += all;
         s0 += kTile;
-        if (before > from || s0 >= a.c.seqs) break;
+        if (before > from || s0 >= seqs) break;
         n = 0;
-        if (s0 + tid < a.c.seqs) {
-            mine = span_of(a.starts, a.c.lens, a.rows, a.max_new, s0 + tid);
+        if (s0 + tid < seqs) {
+            mine = seq_at<SHARED>(a, s0 + tid);
             n = few_work(a, mine);
         }
         upto = scan(n, all) + before;
     }
     __syncthreads();
     int seq = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
-    Span s;
-    s.row0 = __builtin_amdgcn_readfirstlane(found_span.row0);
-    s.n = __builtin_amdgcn_readfirstlane(found_span.n);
-    s.first = __builtin_amdgcn_readfirstlane(found_span.first);
-    s.len = __builtin_amdgcn_readfirstlane(found_span.len);
+    AttendSeq<SHARED> s = of_lane(found_span, 0);
     bool first = true;
-    for (int x = from; x < to && seq < a.c.seqs; ++seq) {
-        if (!first) s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+    for (int x = from; x < to && seq < seqs; ++seq) {
+        if (!first) s = seq_at<SHARED>(a, seq);
         const Reach reach = reach_of(a, s);
         const int tiles = few_tiles(a, reach), rows = s.n * a.group;
         const int row_tiles = few_row_tiles(a, s), units = row_tiles * a.c.kv_heads;
-        const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
+        const int* table = a.c.pages + static_cast<size_t>(table_of(s, seq)) * a.c.max_pages;
         for (int unit = (x - base) / tiles; unit < units && x < to; ++unit) {
             const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
             const int tile0 = x - base - unit * tiles, tile1 = min(tiles, tile0 + to - x);
@@ -423,6 +474,11 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, int w, int launc
                 }
                 if (whole) {
                     const int t = (row0 + er) / a.group, eh = head * a.group + row0 + er - t * a.group;
+                    if constexpr (SHARED) {
+                        put_result(a, s, t, eh, D, ed, o);
+                        if (ed == 0) put_stats(a, s, t, eh, m, sum);
+                        continue;
+                    }
                     const float inv = sum > 0.f ? 1.f / sum : 0.f;
                     f16x4 v;
                     for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
@@ -455,7 +511,7 @@ struct JoinShape {
     int launched, row_tiles_most, spans, span;
 };
 
-template <int D>
+template <int D, bool SHARED = false>
 __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, const JoinShape& shape) {
     const int launched = shape.launched, row_tiles_most = shape.row_tiles_most, spans = shape.spans, span = shape.span;
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
@@ -464,7 +520,7 @@ __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, cons
     const int tid = threadIdx.x;
     const int rest = block / spans, per_seq = a.c.kv_heads * row_tiles_most;
     const int seq = rest / per_seq, unit = rest - seq * per_seq;
-    const Span s = span_of(a.starts, a.c.lens, a.rows, a.max_new, seq);
+    const AttendSeq<SHARED> s = seq_at<SHARED>(a, seq);
     const int rows = s.n * a.group, row_tiles = few_row_tiles(a, s);
     if (unit >= row_tiles * a.c.kv_heads) return;
     const int head = unit / row_tiles, row0 = (unit - head * row_tiles) * kFewRows;
@@ -472,8 +528,8 @@ __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, cons
     const int tiles = few_tiles(a, reach_of(a, s));
     if (tiles == 1 || row0 + r0 >= rows) return;
     unsigned long long work = 0;        // of all sequences, and above that of those before this one
-    for (int i = tid; i < a.c.seqs; i += 256) {
-        const unsigned n = few_work(a, span_of(a.starts, a.c.lens, a.rows, a.max_new, i));
+    for (int i = tid; i < num_seqs<SHARED>(a); i += 256) {
+        const unsigned n = few_work(a, seq_at<SHARED>(a, i));
         work += n;
         if (i < seq) work += static_cast<unsigned long long>(n) << 32;
     }
@@ -512,8 +568,13 @@ __device__ __forceinline__ void attend_join(const AttendArgs& a, int block, cons
         o = o * fo + *reinterpret_cast<const f32x4*>(&sums[i][d]) * fp;
         m = mnew;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
     const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
+    if constexpr (SHARED) {
+        put_result(a, s, t, h, D, d, o);
+        if (d == 0) put_stats(a, s, t, h, m, l);
+        return;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
     f16x4 v;
     for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
     *reinterpret_cast<f16x4*>(a.out + (s.row0 + t) * a.out_stride + h * D + d) = v;
@@ -581,30 +642,30 @@ __host__ __device__ __forceinline__ int many_splits(int units, int tiles, int sl
     return s >= 2.f && work * (1.f - 1.f / s) > 6.f + part * s ? static_cast<int>(s) : 1;
 }
 
-template <int NW>
-__device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Span& s) {
+template <int NW, class Seq>
+__device__ __forceinline__ int many_row_tiles(const AttendArgs& a, const Seq& s) {
     const int rows = s.n * a.group;
     return rows > a.few_most ? (rows + 32 * NW - 1) / (32 * NW) : 0;
 }
 
 // What a workgroup of units finds for itself: its row tile's sequence and rows.
+template <bool SHARED>
 struct ManyUnit {
-    Span s;
+    AttendSeq<SHARED> s;
     int seq, row0;      // seq -1: none
 };
 
 // Every wave looks for itself, the sequences a lane each: first the plan, then
 // row tile `rank_of(plan)` of all.  slots 0: no unit is cut.
-template <int D, int NW, int KS, class F>
-__device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots, F rank_of, ManyUnit& unit) {
+template <int D, int NW, int KS, bool SHARED, class F>
+__device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots, F rank_of, ManyUnit<SHARED>& unit) {
     const int lane = threadIdx.x & 63;
-    auto span_at = [&](int i) {
-        return i < a.c.seqs ? span_of(a.starts, a.c.lens, a.rows, a.max_new, i) : Span{0, 0, 0, 0};
-    };
-    Span mine = span_at(lane);                     // of the first 64 sequences
+    const int seqs = num_seqs<SHARED>(a);
+    auto span_at = [&](int i) { return i < seqs ? seq_at<SHARED>(a, i) : AttendSeq<SHARED>{}; };
+    AttendSeq<SHARED> mine = span_at(lane);        // of the first 64 sequences
     int row_tiles = 0, most = 0;
-    for (int i0 = 0; i0 < a.c.seqs; i0 += 64) {
-        const Span s = i0 ? span_at(i0 + lane) : mine;
+    for (int i0 = 0; i0 < seqs; i0 += 64) {
+        const AttendSeq<SHARED> s = i0 ? span_at(i0 + lane) : mine;
         const int t = many_row_tiles<NW>(a, s);
         const Reach r = reach_of(a, s);
         row_tiles += t;
@@ -617,7 +678,7 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots, F 
     const int rank = rank_of(p);
     unit.seq = -1;
     if (rank < 0) return p;
-    for (int i0 = 0, before = 0; i0 < a.c.seqs; i0 += 64) {
+    for (int i0 = 0, before = 0; i0 < seqs; i0 += 64) {
         if (i0) mine = span_at(i0 + lane);
         const int n = many_row_tiles<NW>(a, mine);
         const int upto = wave_upto(Sum(), n) + before;
@@ -626,7 +687,7 @@ __device__ __forceinline__ ManyPlan many_plan(const AttendArgs& a, int slots, F 
             const int l = __builtin_ctzll(has);
             unit.seq = i0 + l;
             unit.row0 = (rank - lane_of(upto - n, l)) * 32 * NW;
-            unit.s = {lane_of(mine.row0, l), lane_of(mine.n, l), lane_of(mine.first, l), lane_of(mine.len, l)};
+            unit.s = of_lane(mine, l);
             return p;
         }
         before = lane_of(upto, 63);
@@ -651,21 +712,22 @@ struct ManyLds {
 
 // NW waves for the rows, KS teams of them for the keys: each takes every KS-th tile
 // of its unit in buffers of its own, and the first adds the others' sums at the
-// end.  With one team, workgroups from `blocks` on, `few` of them, run attend_few:
-// in a batch of prompts and single tokens both go side by side.
-template <int D, int NW, int KS, bool ONE>
+// end.  With one team, or prefixes shared, workgroups from `blocks` on, `few` of them, run
+// attend_few: in a batch of prompts and single tokens both go side by side.
+template <int D, int NW, int KS, bool ONE, bool SHARED = false>
 __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs a, int slots, int blocks, int few) {
     constexpr int kRows = 32 * NW, kThreads = 64 * NW;
     constexpr int kStep = KS * kManyTile;                       // tokens from a team's tile to its next
     constexpr int kKeys = 4 * D, kPer = 8 * D / kThreads;       // 16-byte pieces of a tile's keys; a thread's pieces of both
     constexpr int kGroups = ONE ? 1 : 4, kWindow = 64 / kGroups;   // scales of a tile; tiles whose scales 64 lanes hold
     static_assert(8 * D % kThreads == 0, "whole pieces a thread");
-    using Few = FewLds<D, NW>;
+    using Few = FewLds<D, NW * KS, SHARED>;
     constexpr size_t kLds = sizeof(ManyLds<D>) * KS;
-    __shared__ __align__(16) char lds[KS == 1 && kLds < sizeof(Few) ? sizeof(Few) : kLds];
-    if constexpr (KS == 1)
+    constexpr bool kFewBeside = KS == 1 || SHARED;
+    __shared__ __align__(16) char lds[kFewBeside && kLds < sizeof(Few) ? sizeof(Few) : kLds];
+    if constexpr (kFewBeside)
         if (static_cast<int>(blockIdx.x) >= blocks)
-            return attend_few<D, NW>(a, blockIdx.x - blocks, few, *reinterpret_cast<Few*>(lds));
+            return attend_few<D, NW * KS, SHARED>(a, blockIdx.x - blocks, few, *reinterpret_cast<Few*>(lds));
     const int lane = threadIdx.x & 63;
     const int team = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
     const int tid = threadIdx.x - team * kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -673,12 +735,12 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     auto& vt = reinterpret_cast<ManyLds<D>*>(lds)[team].v;
     // the last row tiles first: those have the most keys
     const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads;
-    ManyUnit unit;
+    ManyUnit<SHARED> unit;
     const ManyPlan plan =
-        many_plan<D, NW, KS>(a, slots, [&](const ManyPlan& p) { return p.row_tiles - 1 - rest / p.splits; }, unit);
+        many_plan<D, NW, KS, SHARED>(a, slots, [&](const ManyPlan& p) { return p.row_tiles - 1 - rest / p.splits; }, unit);
     if (unit.seq < 0) return;
     const int splits = plan.splits, split = rest % splits, seq = unit.seq, row0 = unit.row0;
-    const Span s = unit.s;
+    const auto s = unit.s;
     const int rows = s.n * a.group;
     const Reach reach = reach_of(a, s);
     const int token0 = s.first + row0 / a.group, token1 = s.first + (min(row0 + kRows, rows) - 1) / a.group;
@@ -687,7 +749,7 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     const int tile0 = split_from(split, unit_tiles, splits), n = split_from(split + 1, unit_tiles, splits) - tile0;
     const int piece = reach_begin + tile0 * kManyTile, end = min(reach_end, piece + n * kManyTile);
     const int begin = piece + team * kManyTile, mine = (n - team + KS - 1) / KS;      // the team's first tile, and its tiles
-    const int* table = a.c.pages + static_cast<size_t>(seq) * a.c.max_pages;
+    const int* table = a.c.pages + static_cast<size_t>(table_of(s, seq)) * a.c.max_pages;
     const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
 
     // the lane's row, and what the wave's rows see: all of [all_begin, all_end), none outside [any_begin, any_end)
@@ -948,6 +1010,15 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
                     f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         return;
     }
+    if constexpr (SHARED) {
+        if (half == 0) put_stats(a, s, rtoken, h, m + kSlack, l);      // attend_few's weights are 2^kSlack larger
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                put_result(a, s, rtoken, h, D, 32 * d + 2 * i + 4 * half, f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]});
+        return;
+    }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     uint16_t* out = a.out + (s.row0 + rtoken) * a.out_stride + h * D + 4 * half;
 #pragma unroll
@@ -967,16 +1038,16 @@ template <int D>
 constexpr int kJoinRows = 1024 / D;
 
 // Workgroups from `blocks` on run attend_join.
-template <int D, int NW, int KS>
+template <int D, int NW, int KS, bool SHARED = false>
 __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int slots, int blocks, JoinShape shape) {
     constexpr int kRows = 32 * NW, kParts = kRows / kJoinRows<D>;
-    if (static_cast<int>(blockIdx.x) >= blocks) return attend_join<D>(a, blockIdx.x - blocks, shape);
+    if (static_cast<int>(blockIdx.x) >= blocks) return attend_join<D, SHARED>(a, blockIdx.x - blocks, shape);
     const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts, head = rest % a.c.kv_heads;
-    ManyUnit found;
-    const ManyPlan plan = many_plan<D, NW, KS>(
+    ManyUnit<SHARED> found;
+    const ManyPlan plan = many_plan<D, NW, KS, SHARED>(
         a, slots, [&](const ManyPlan& p) { return p.splits == 1 ? -1 : p.row_tiles - 1 - rest / a.c.kv_heads; }, found);
     if (found.seq < 0) return;
-    const Span s = found.s;
+    const auto s = found.s;
     const int row0 = found.row0, r = part * kJoinRows<D> + static_cast<int>(threadIdx.x) / (D / 4);
     if (row0 + r >= s.n * a.group) return;
     const float* unit = a.pieces +
@@ -995,8 +1066,13 @@ __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, int
         l += f * p[kRows + r];
         o += f * *reinterpret_cast<const f32x4*>(p + 2 * kRows + r * D + d);
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
     const int t = (row0 + r) / a.group, h = head * a.group + row0 + r - t * a.group;
+    if constexpr (SHARED) {
+        put_result(a, s, t, h, D, d, o);
+        if (d == 0) put_stats(a, s, t, h, m + kSlack, l);
+        return;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
     f16x4 v;
     for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(o[i] * inv);
     *reinterpret_cast<f16x4*>(a.out + (s.row0 + t) * a.out_stride + h * D + d) = v;

@@ -6,12 +6,14 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "../../include/tetra.h"
 #include "attend.h"
 #include "host.h"
 #include "kv_cache.h"
 #include "sample.h"
+#include "shared.h"
 
 namespace {
 
@@ -138,6 +140,101 @@ int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
     return launch_status();
 }
 
+// the arguments of tetra_kv_attend, checked
+int attend_args(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
+                int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
+                void* workspace, size_t workspace_bytes, tetra_dev::AttendArgs& a, int& cus) {
+    if (int st = cache_of(cache, &a.c)) return st;
+    if (!q || !starts || !out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
+    if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale)) return TETRA_EINVAL;
+    const long long width = static_cast<long long>(q_heads) * cache->head_dim;
+    if (q_stride < width || out_stride < width || rows > kMaxGrid / q_heads) return TETRA_EINVAL;
+    if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 || out_stride % 8 || !aligned(starts, 4) ||
+        !aligned(workspace, 256))
+        return TETRA_EALIGN;
+    if (workspace_bytes < kMinAttendWorkspace) return TETRA_EINVAL;
+    if (int st = device_cus(&cus)) return st;
+    if (workspace_bytes < attend_workspace(cus)) return TETRA_EINVAL;
+    a.q = q;
+    a.starts = starts;
+    a.out = out;
+    a.partials = static_cast<float*>(workspace);
+    a.pieces = a.partials + few_parts(cus);
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.scale = std::fabs(scale) * 1.44269504f;
+    a.q_flip = scale < 0.f ? 0x80008000u : 0u;
+    a.rows = rows;
+    a.max_new = max_new;
+    a.q_heads = q_heads;
+    a.group = q_heads / a.c.kv_heads;
+    a.window = window;
+    return TETRA_OK;
+}
+
+// What a call with shared prefixes may be to go by its groups: rows of a sequence and cache
+// head, rows times q heads, and groups and sequences.
+constexpr int kSharedMost = 64, kSharedRows = 65536, kSharedList = 131072;
+
+// bytes of kv_attend_shared's workspace, behind those of kv_attend
+struct SharedSpace {
+    size_t list, group, results, stats, bytes;
+    explicit SharedSpace(int cus) {
+        list = attend_workspace(cus);
+        group = list + sizeof(tetra_dev::SharedSeq) * kSharedList;
+        results = group + sizeof(tetra_dev::SharedGroup) * kSharedList;
+        stats = results + 2 * sizeof(float) * 128 * kSharedRows;
+        bytes = stats + 4 * sizeof(float) * kSharedRows;
+    }
+};
+
+bool shared_pays(const tetra_dev::AttendArgs& a, int dim) {
+    const long long most = static_cast<long long>(a.max_new) * a.group;
+    if (most > kSharedMost || a.rows > kSharedRows / a.q_heads || a.num_seqs > kSharedList) return false;
+    static const long long MB = getenv("SHMB") ? atoi(getenv("SHMB")) : 32;
+    const long long tokens = (static_cast<long long>(a.c.max_pages) << a.c.page_shift) * a.c.seqs;
+    return tokens * a.c.kv_heads * 2 * dim >= MB << 20;
+}
+
+template <int D, int KS>
+int shared_launch_teams(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
+    tetra_dev::AttendArgs& a = x.a;
+    static const int FM = getenv("SHFM") ? atoi(getenv("SHFM")) : 32;
+    static const int FG = getenv("SHFG") ? atoi(getenv("SHFG")) : 1;
+    const int most = a.max_new * a.group, slots = KS == 1 ? 2 * cus : cus, few = FG * (KS == 1 ? 2 * cus : cus) / 1;
+    a.few_most = std::max(most, FM);
+    a.few_tile = 256 * KS;
+    const long long all = static_cast<long long>(a.rows) * a.group;
+    const long long units = (all / 128 + std::min<long long>(x.num_groups, all / (a.few_most + 1))) * a.c.kv_heads;   // at most
+    const long long blocks = units ? std::max<long long>(units, slots) : 0;
+    const long long join_many = std::min<long long>(units, slots / 2) * (128 / tetra_dev::kJoinRows<D>);
+    tetra_dev::JoinShape shape{few, (a.few_most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows, 1, 1};
+    const long long few_units = static_cast<long long>(shape.row_tiles_most) * a.c.kv_heads * a.num_seqs;
+    const int rows_most = tetra_dev::kFewRows;
+    while (shape.span < 8 && few_units * rows_most > 2ll * shape.span * cus) shape.span *= 2;
+    shape.spans = (rows_most + shape.span - 1) / shape.span;
+    const long long join = join_many + few_units * shape.spans;
+    const long long last = static_cast<long long>(a.rows) * ((a.q_heads + 1024 / D - 1) / (1024 / D));
+    if (blocks + few > kMaxGrid || join > kMaxGrid || last > kMaxGrid) return TETRA_EINVAL;
+    hipLaunchKernelGGL(tetra_dev::shared_list_kernel, dim3(1), dim3(tetra_dev::kListThreads), 0, stream, x);
+    const dim3 g(static_cast<unsigned>(blocks + few)), b(256 * KS);
+    const int many = static_cast<int>(blocks);
+    if (a.c.page_tokens >= tetra_dev::kManyTile)
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, KS, true, true>), g, b, 0, stream, a, slots, many, few);
+    else
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, KS, false, true>), g, b, 0, stream, a, slots, many, few);
+    hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4, KS, true>), dim3(static_cast<unsigned>(join)), dim3(256), 0, stream, a,
+                       slots, static_cast<int>(join_many), shape);
+    hipLaunchKernelGGL((tetra_dev::shared_join_kernel<D>), dim3(static_cast<unsigned>(last)), dim3(256), 0, stream, x);
+    return launch_status();
+}
+
+template <int D>
+int shared_launch(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
+    static const int KS = getenv("SHKS") ? atoi(getenv("SHKS")) : 2;
+    return KS == 1 ? shared_launch_teams<D, 1>(x, cus, stream) : shared_launch_teams<D, 2>(x, cus, stream);
+}
+
 int append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, const int* shifts, int rows, int max_new,
            hipStream_t stream) {
     tetra_dev::AppendArgs a;
@@ -236,45 +333,45 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
                     int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
                     void* workspace, size_t workspace_bytes, hipStream_t stream) {
     tetra_dev::AttendArgs a;
-    if (int st = cache_of(cache, &a.c)) return st;
-    if (!q || !starts || !out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
-    if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale)) return TETRA_EINVAL;
-    const long long width = static_cast<long long>(q_heads) * cache->head_dim;
-    if (q_stride < width || out_stride < width || rows > kMaxGrid / q_heads) return TETRA_EINVAL;
-    if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 || out_stride % 8 || !aligned(starts, 4) ||
-        !aligned(workspace, 256))
-        return TETRA_EALIGN;
     int cus = 0;
-    if (workspace_bytes < kMinAttendWorkspace) return TETRA_EINVAL;
-    if (int st = device_cus(&cus)) return st;
-    if (workspace_bytes < attend_workspace(cus)) return TETRA_EINVAL;
-    a.q = q;
-    a.starts = starts;
-    a.out = out;
-    a.partials = static_cast<float*>(workspace);
-    a.pieces = a.partials + few_parts(cus);
-    a.q_stride = q_stride;
-    a.out_stride = out_stride;
-    a.scale = std::fabs(scale) * 1.44269504f;
-    a.q_flip = scale < 0.f ? 0x80008000u : 0u;
-    a.rows = rows;
-    a.max_new = max_new;
-    a.q_heads = q_heads;
-    a.group = q_heads / a.c.kv_heads;
-    a.window = window;
+    if (int st = attend_args(cache, q, q_stride, starts, rows, max_new, q_heads, scale, window, out, out_stride, workspace,
+                             workspace_bytes, a, cus))
+        return st;
     return cache->head_dim == 64 ? attend_launch<64>(a, cus, stream) : attend_launch<128>(a, cus, stream);
 }
 
-size_t tetra_kv_attend_shared_workspace_bytes(void) { return tetra_kv_attend_workspace_bytes(); }
+size_t tetra_kv_attend_shared_workspace_bytes(void) {
+    int cus = 0;
+    if (device_cus(&cus)) return 0;
+    return SharedSpace(cus).bytes;
+}
 
 int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
                            int max_new, int q_heads, float scale, const int* groups, const int* shared, int num_groups,
                            uint16_t* out, long long out_stride, void* workspace, size_t workspace_bytes,
                            hipStream_t stream) {
-    if (!cache || !groups || !shared || num_groups < 1 || num_groups > cache->seqs) return TETRA_EINVAL;
+    tetra_dev::SharedArgs x;
+    int cus = 0;
+    if (cache && (!groups || !shared || num_groups < 1 || num_groups > cache->seqs)) return TETRA_EINVAL;
     if (!aligned(groups, 4) || !aligned(shared, 4)) return TETRA_EALIGN;
-    return tetra_kv_attend(cache, q, q_stride, starts, rows, max_new, q_heads, scale, 0, out, out_stride, workspace,
-                           workspace_bytes, stream);
+    if (int st = attend_args(cache, q, q_stride, starts, rows, max_new, q_heads, scale, 0, out, out_stride, workspace,
+                             workspace_bytes, x.a, cus))
+        return st;
+    const SharedSpace space(cus);
+    if (workspace_bytes < space.bytes) return TETRA_EINVAL;
+    x.groups = groups;
+    x.shared = shared;
+    x.num_groups = num_groups;
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    x.list = reinterpret_cast<tetra_dev::SharedSeq*>(at + space.list);
+    x.group = reinterpret_cast<tetra_dev::SharedGroup*>(at + space.group);
+    x.a.seqs = x.list;
+    x.a.num_seqs = num_groups + cache->seqs;
+    x.a.results = reinterpret_cast<float*>(at + space.results);
+    x.a.stats = reinterpret_cast<float*>(at + space.stats);
+    if (!shared_pays(x.a, cache->head_dim))
+        return cache->head_dim == 64 ? attend_launch<64>(x.a, cus, stream) : attend_launch<128>(x.a, cus, stream);
+    return cache->head_dim == 64 ? shared_launch<64>(x, cus, stream) : shared_launch<128>(x, cus, stream);
 }
 
 size_t tetra_sample_workspace_bytes(int rows, int vocab) {

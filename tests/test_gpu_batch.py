@@ -72,7 +72,22 @@ def _shared_space():
     return _SPACE[0]
 
 
-def _check_shared(c, news, q_heads, scale=None, strided=False, slack=0, seed=2, first=None, shared=None, q_size=2.0):
+def _widen(c):
+    """Gives the table room for 64 MB of keys and values."""
+    wide = max(c.max_pages, -(-(1 << 26) // (2 * c.heads * c.dim * len(c.lens) * c.page)))
+    c.table = np.pad(c.table, ((0, 0), (0, wide - c.table.shape[1])), constant_values=-1)
+    c.max_pages = wide
+
+
+def _check_shared(c, news, q_heads, **kw):
+    """With the table as it is and with one that has room for far longer sequences, by whose size calls go by groups."""
+    got = _check_shared_once(c, news, q_heads, **kw)
+    _widen(c)
+    _check_shared_once(c, news, q_heads, **kw)
+    return got
+
+
+def _check_shared_once(c, news, q_heads, scale=None, strided=False, slack=0, seed=2, first=None, shared=None, q_size=2.0):
     rng = np.random.default_rng(seed)
     starts, rows = _starts(news), int(sum(news))
     q = (rng.standard_normal((rows, q_heads, c.dim)) * q_size).astype(np.float16)
@@ -178,10 +193,13 @@ def test_shared_groups_of_any_kind(first, shared):
     _check_shared(Shared(7, [(320, [4, 50, 60, 70])], 2, 32, 128), [1, 1, 2, 1], 10, first=first, shared=shared)
 
 
-def test_shared_lengths_past_the_table():
+@pytest.mark.parametrize("roomy", [False, True])
+def test_shared_lengths_past_the_table(roomy):
+    """The table is what counts: tokens past it are not seen, and shared lengths past it are all of it."""
     c = Shared(8, [(320, [4, 50, 60])], 2, 32, 64)
-    c.max_pages = 10
-    c.table = c.table[:, :10].copy()
+    wide = 8192 if roomy else 10
+    c.table = np.pad(c.table[:, :10], ((0, 0), (0, wide - 10)), constant_values=-1)
+    c.max_pages = wide
     cache = c.upload()
     q = _dev((np.random.default_rng(1).standard_normal((3, 4, 64)) * 2).astype(np.float16))
     at, out = _dev(_starts([1, 1, 1])), [torch.empty((3, 4, 64), dtype=torch.float16, device="cuda") for _ in range(3)]
@@ -205,8 +223,11 @@ def test_shared_missing_pages_and_scales(news):
 
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("news", [(1, 1, 1, 1), (9, 1, 30, 2)])
-def test_shared_not_finite_queries_stay_alone(news, bad):
+@pytest.mark.parametrize("roomy", [False, True])
+def test_shared_not_finite_queries_stay_alone(news, bad, roomy):
     c = Shared(10, [(320, [n + 20 for n in news])], 2, 32, 64)
+    if roomy:
+        _widen(c)
     starts, rows = _starts(news), sum(news)
     q = np.random.default_rng(3).standard_normal((rows, 6, 64)).astype(np.float16)
     spoiled = q.copy()
@@ -222,9 +243,12 @@ def test_shared_not_finite_queries_stay_alone(news, bad):
     assert torch.equal(*out)
 
 
-def test_shared_rows_of_no_sequence_are_left_alone():
+@pytest.mark.parametrize("roomy", [False, True])
+def test_shared_rows_of_no_sequence_are_left_alone(roomy):
     """Starts that end before the last row, as where a graph is captured for a full batch; bad starts."""
     c = Shared(11, [(320, [24, 30, 50])], 2, 32, 64)
+    if roomy:
+        _widen(c)
     cache, q = c.upload(), _dev(np.random.default_rng(3).standard_normal((9, 6, 64)).astype(np.float16))
     groups, lengths = _dev(np.array([0, 3], np.int32)), _dev(np.array([320], np.int32))
     want = torch.full((3, 6, 64), 7.0, dtype=torch.float16, device="cuda")
@@ -790,10 +814,13 @@ def _serving_state():
     return c, spare
 
 
-def test_a_served_step_of_all_operators_in_a_graph():
+@pytest.mark.parametrize("roomy", [False, True])
+def test_a_served_step_of_all_operators_in_a_graph(roomy):
     """Append, attention over the groups, weights, log probabilities, captured once and replayed with other lengths and
     groups; every replay is what the calls give by themselves."""
     c, _ = _serving_state()
+    if roomy:
+        _widen(c)
     cache, rng = c.upload(), np.random.default_rng(0)
     x = _dev(rng.standard_normal((5, 2, 64)).astype(np.float32))
     q = _dev(rng.standard_normal((5, 6, 64)).astype(np.float32))
@@ -895,6 +922,7 @@ def test_operators_on_other_streams():
     setups = []
     for i in range(2):
         c = Shared(71 + i, [(640, [20, 50, 90, 33]), (320, [300, 7])], 2, 32, 64)
+        _widen(c)
         cache = c.upload()
         q = _dev(np.random.default_rng(i).standard_normal((6, 6, 64)).astype(np.float16))
         x = _dev(np.random.default_rng(i).standard_normal((6, 20000)).astype(np.float32))
