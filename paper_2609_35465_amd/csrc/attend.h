@@ -712,8 +712,8 @@ struct ManyLds {
 
 // NW waves for the rows, KS teams of them for the keys: each takes every KS-th tile
 // of its unit in buffers of its own, and the first adds the others' sums at the
-// end.  With one team, or prefixes shared, workgroups from `blocks` on, `few` of them, run
-// attend_few: in a batch of prompts and single tokens both go side by side.
+// end.  With one team, workgroups from `blocks` on, `few` of them, run attend_few:
+// in a batch of prompts and single tokens both go side by side.
 template <int D, int NW, int KS, bool ONE, bool SHARED = false>
 __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs a, int slots, int blocks, int few) {
     constexpr int kRows = 32 * NW, kThreads = 64 * NW;
@@ -721,13 +721,12 @@ __global__ __launch_bounds__(NW * KS * 64, 2) void attend_many_kernel(AttendArgs
     constexpr int kKeys = 4 * D, kPer = 8 * D / kThreads;       // 16-byte pieces of a tile's keys; a thread's pieces of both
     constexpr int kGroups = ONE ? 1 : 4, kWindow = 64 / kGroups;   // scales of a tile; tiles whose scales 64 lanes hold
     static_assert(8 * D % kThreads == 0, "whole pieces a thread");
-    using Few = FewLds<D, NW * KS, SHARED>;
+    using Few = FewLds<D, NW, SHARED>;
     constexpr size_t kLds = sizeof(ManyLds<D>) * KS;
-    constexpr bool kFewBeside = KS == 1 || SHARED;
-    __shared__ __align__(16) char lds[kFewBeside && kLds < sizeof(Few) ? sizeof(Few) : kLds];
-    if constexpr (kFewBeside)
+    __shared__ __align__(16) char lds[KS == 1 && kLds < sizeof(Few) ? sizeof(Few) : kLds];
+    if constexpr (KS == 1)
         if (static_cast<int>(blockIdx.x) >= blocks)
-            return attend_few<D, NW * KS, SHARED>(a, blockIdx.x - blocks, few, *reinterpret_cast<Few*>(lds));
+            return attend_few<D, NW, SHARED>(a, blockIdx.x - blocks, few, *reinterpret_cast<Few*>(lds));
     const int lane = threadIdx.x & 63;
     const int team = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
     const int tid = threadIdx.x - team * kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

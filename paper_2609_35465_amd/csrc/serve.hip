@@ -6,7 +6,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "../../include/tetra.h"
 #include "attend.h"
@@ -188,51 +187,59 @@ struct SharedSpace {
     }
 };
 
+// Whether a call goes by its groups.  That takes two launches more and the sums' way through
+// memory, some 14 us, and saves what kv_attend reads of keys and values more than once: of
+// pages that sequences share it has much from the caches.  What it may read is told by the
+// table's width, for the host does not know the lengths, and it reads it for each 16 rows
+// of a sequence.  Measured (40 heads over 8 of 128, us by groups and by kv_attend): 8
+// sequences of 4,196 tokens (69 MB) 28 and 22, 64 of 1,124 (151 MB) 29 and 27, 12 of 8,292
+// (204 MB) 33 and 39, 64 of 4,196 in 8 groups (554 MB) 43 and 56, with four rows each in one
+// group 64 and 179.
+constexpr long long kSharedBytes = 160ll << 20;
+
 bool shared_pays(const tetra_dev::AttendArgs& a, int dim) {
     const long long most = static_cast<long long>(a.max_new) * a.group;
     if (most > kSharedMost || a.rows > kSharedRows / a.q_heads || a.num_seqs > kSharedList) return false;
-    static const long long MB = getenv("SHMB") ? atoi(getenv("SHMB")) : 32;
-    const long long tokens = (static_cast<long long>(a.c.max_pages) << a.c.page_shift) * a.c.seqs;
-    return tokens * a.c.kv_heads * 2 * dim >= MB << 20;
+    const double tokens = static_cast<double>(static_cast<long long>(a.c.max_pages) << a.c.page_shift) * a.c.seqs;
+    const long long tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
+    return tokens * a.c.kv_heads * 2 * dim * tiles >= kSharedBytes;
 }
 
-template <int D, int KS>
-int shared_launch_teams(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
+// Groups of up to 32 rows of a cache head go 16 rows at a time, like the sequences' own
+// tokens, others 128 at a time (groups of 20 rows over 8,192 tokens 27 us so and 29 by 128;
+// of 40 rows 28 by 128 and 25 so, but over 32,768 51 and 58).  The latter fill one and a
+// half workgroups a CU, so that the former begin beside them: 64 sequences of 32 heads with
+// 32,768 tokens in common 74 us, two workgroups a CU 83, one 77.
+constexpr int kSharedFew = 32;
+
+template <int D>
+int shared_launch(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
     tetra_dev::AttendArgs& a = x.a;
-    static const int FM = getenv("SHFM") ? atoi(getenv("SHFM")) : 32;
-    static const int FG = getenv("SHFG") ? atoi(getenv("SHFG")) : 1;
-    const int most = a.max_new * a.group, slots = KS == 1 ? 2 * cus : cus, few = FG * (KS == 1 ? 2 * cus : cus) / 1;
-    a.few_most = std::max(most, FM);
-    a.few_tile = 256 * KS;
+    const int slots = cus + cus / 2, few = kFewGroupsPerCU * cus;
+    a.few_most = std::max(a.max_new * a.group, kSharedFew);
+    a.few_tile = 256;
     const long long all = static_cast<long long>(a.rows) * a.group;
     const long long units = (all / 128 + std::min<long long>(x.num_groups, all / (a.few_most + 1))) * a.c.kv_heads;   // at most
     const long long blocks = units ? std::max<long long>(units, slots) : 0;
     const long long join_many = std::min<long long>(units, slots / 2) * (128 / tetra_dev::kJoinRows<D>);
     tetra_dev::JoinShape shape{few, (a.few_most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows, 1, 1};
     const long long few_units = static_cast<long long>(shape.row_tiles_most) * a.c.kv_heads * a.num_seqs;
-    const int rows_most = tetra_dev::kFewRows;
-    while (shape.span < 8 && few_units * rows_most > 2ll * shape.span * cus) shape.span *= 2;
-    shape.spans = (rows_most + shape.span - 1) / shape.span;
+    while (shape.span < 8 && few_units * tetra_dev::kFewRows > 2ll * shape.span * cus) shape.span *= 2;
+    shape.spans = tetra_dev::kFewRows / shape.span;
     const long long join = join_many + few_units * shape.spans;
     const long long last = static_cast<long long>(a.rows) * ((a.q_heads + 1024 / D - 1) / (1024 / D));
     if (blocks + few > kMaxGrid || join > kMaxGrid || last > kMaxGrid) return TETRA_EINVAL;
     hipLaunchKernelGGL(tetra_dev::shared_list_kernel, dim3(1), dim3(tetra_dev::kListThreads), 0, stream, x);
-    const dim3 g(static_cast<unsigned>(blocks + few)), b(256 * KS);
+    const dim3 g(static_cast<unsigned>(blocks + few)), b(256);
     const int many = static_cast<int>(blocks);
     if (a.c.page_tokens >= tetra_dev::kManyTile)
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, KS, true, true>), g, b, 0, stream, a, slots, many, few);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, 1, true, true>), g, b, 0, stream, a, slots, many, few);
     else
-        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, KS, false, true>), g, b, 0, stream, a, slots, many, few);
-    hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4, KS, true>), dim3(static_cast<unsigned>(join)), dim3(256), 0, stream, a,
-                       slots, static_cast<int>(join_many), shape);
-    hipLaunchKernelGGL((tetra_dev::shared_join_kernel<D>), dim3(static_cast<unsigned>(last)), dim3(256), 0, stream, x);
+        hipLaunchKernelGGL((tetra_dev::attend_many_kernel<D, 4, 1, false, true>), g, b, 0, stream, a, slots, many, few);
+    hipLaunchKernelGGL((tetra_dev::attend_join_many_kernel<D, 4, 1, true>), dim3(static_cast<unsigned>(join)), b, 0, stream, a, slots,
+                       static_cast<int>(join_many), shape);
+    hipLaunchKernelGGL((tetra_dev::shared_join_kernel<D>), dim3(static_cast<unsigned>(last)), b, 0, stream, x);
     return launch_status();
-}
-
-template <int D>
-int shared_launch(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
-    static const int KS = getenv("SHKS") ? atoi(getenv("SHKS")) : 2;
-    return KS == 1 ? shared_launch_teams<D, 1>(x, cus, stream) : shared_launch_teams<D, 2>(x, cus, stream);
 }
 
 int append(const tetra_kv_cache* cache, const tetra_kv_input* in, const int* starts, const int* shifts, int rows, int max_new,

@@ -73,8 +73,8 @@ def _shared_space():
 
 
 def _widen(c):
-    """Gives the table room for 64 MB of keys and values."""
-    wide = max(c.max_pages, -(-(1 << 26) // (2 * c.heads * c.dim * len(c.lens) * c.page)))
+    """Gives the table room for 256 MB of keys and values."""
+    wide = max(c.max_pages, -(-(1 << 28) // (2 * c.heads * c.dim * len(c.lens) * c.page)))
     c.table = np.pad(c.table, ((0, 0), (0, wide - c.table.shape[1])), constant_values=-1)
     c.max_pages = wide
 
@@ -197,7 +197,7 @@ def test_shared_groups_of_any_kind(first, shared):
 def test_shared_lengths_past_the_table(roomy):
     """The table is what counts: tokens past it are not seen, and shared lengths past it are all of it."""
     c = Shared(8, [(320, [4, 50, 60])], 2, 32, 64)
-    wide = 8192 if roomy else 10
+    wide = 16384 if roomy else 10
     c.table = np.pad(c.table[:, :10], ((0, 0), (0, wide - 10)), constant_values=-1)
     c.max_pages = wide
     cache = c.upload()
