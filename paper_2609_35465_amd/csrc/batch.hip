@@ -48,7 +48,7 @@ struct WeighSpace {
 template <int D>
 int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
     const bool few = weigh_few(a.max_new, a.group);
-    const dim3 b(256), g(static_cast<unsigned>(cus * (few ? kWeighFewGroupsPerCU : kWeighGroupsPerCU)));
+    const dim3 b(256), m(64 * tetra_dev::kWeighWaves), g(static_cast<unsigned>(cus * (few ? kWeighFewGroupsPerCU : kWeighGroupsPerCU)));
     a.workers = static_cast<int>(few ? 4 * g.x : g.x);
     a.block = few ? 64 : tetra_dev::kWeighBlock;
     a.spans_most = few ? tetra_dev::kWeighSpans : tetra_dev::kWeighSpans / 4;
@@ -57,12 +57,12 @@ int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
     if (one) hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 1>), g, b, 0, stream, a); \
     else hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 2>), g, b, 0, stream, a)
     if (few) { TETRA_WEIGH_FEW(tetra_dev::kWeighSpanSums); }
-    else hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, b, 0, stream, a);
+    else hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, m, 0, stream, a);
     hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), dim3(64 * tetra_dev::kLogWaves), 0, stream, a);
     if (few) {
         TETRA_WEIGH_FEW(tetra_dev::kWeighTokens);
     } else {
-        hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, b, 0, stream, a);
+        hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighTokens>), g, m, 0, stream, a);
         hipLaunchKernelGGL(tetra_dev::weigh_join_kernel, g, b, 0, stream, a);
     }
 #undef TETRA_WEIGH_FEW

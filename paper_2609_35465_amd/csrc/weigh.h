@@ -22,10 +22,11 @@
 
 namespace tetra_dev {
 
-constexpr int kWeighBlock = 256;          // tokens of a workgroup, 64 of a wave
+constexpr int kWeighBlock = 256;          // tokens of a workgroup, 32 of a wave
+constexpr int kWeighWaves = kWeighBlock / 32;
 constexpr int kWeighRows = 32;            // rows of a tile
 constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sums, at most
-constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
+constexpr int kWeighMostTiles = 16;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
 
@@ -200,16 +201,9 @@ __device__ __forceinline__ int weigh_item(const WeighArgs& a, int round) {
     return round * a.workers + (round & 1 ? a.workers - 1 - w : w);
 }
 
-// sums over N (16 or 32) neighbouring lanes of N numbers: lane e of them gets that of v[e]
-template <int N>
-__device__ __forceinline__ float weigh_scatter(float (&v)[N]) {
+// sums over 16 neighbouring lanes of 16 numbers: lane e of them gets that of v[e]
+__device__ __forceinline__ float weigh_scatter(float (&v)[16]) {
     const int lane = threadIdx.x & 63;
-    if constexpr (N == 32)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[j]), __builtin_bit_cast(uint32_t, v[j + 16]), false, false);
-            v[j] = __builtin_bit_cast(float, static_cast<uint32_t>(r[0])) + __builtin_bit_cast(float, static_cast<uint32_t>(r[1]));
-        }
     auto halve = [&](int bit, auto other) {
 #pragma unroll
         for (int j = 0; j < bit; ++j) {
@@ -235,17 +229,20 @@ __device__ __forceinline__ void weigh_write(const WeighArgs& a, const WeighItem&
 }
 
 template <int D, WeighPass PASS>
-__global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
-    constexpr int kSlices = D / 8, kPer = kSlices * kWeighRows / 256;       // 8 dimensions of a row; a thread's pieces of a tile
+__global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a) {
+    constexpr int kThreads = 64 * kWeighWaves, kSlices = D / 8, kPieces = kSlices * kWeighRows;   // 8 dimensions of a row each
+    static_assert(kPieces <= kThreads, "a piece of a tile of rows a thread");
     constexpr std::integral_constant<WeighPass, PASS> pass;
+    constexpr bool kSums = PASS == kWeighSpanSums;
     __shared__ __align__(16) _Float16 rows[2][kSlices][kWeighRows][8];
-    __shared__ float sums[PASS == kWeighSpanSums ? 4 : 1][PASS == kWeighSpanSums ? kWeighMostTiles * kWeighRows : 1][2];
+    __shared__ float sums[kSums ? kWeighWaves : 1][kSums ? kWeighMostTiles * kWeighRows : 1][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lrow = lane & 31, half = lane >> 5;
     const float inverse_group = 1.f / static_cast<float>(a.group);
+    const int step_t = kWeighRows / a.group, step_g = kWeighRows - step_t * a.group;
     WeighSeq first;
     const WeighPlan plan(a, first, pass, std::false_type());
-    if (PASS == kWeighSpanSums && blockIdx.x == 0 && threadIdx.x == 0) *a.span = plan.span;
+    if (kSums && blockIdx.x == 0 && threadIdx.x == 0) *a.span = plan.span;
     const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
     for (int round = 0;; ++round) {
         if (static_cast<long long>(round) * a.workers >= plan.total) break;
@@ -255,15 +252,15 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
         const Span& s = w.q.s;
         const int* table = a.c.pages + static_cast<size_t>(w.seq) * a.c.max_pages;
         const int all_rows = s.n * a.group;
-        if constexpr (PASS == kWeighSpanSums) {
+        if constexpr (kSums) {
             __syncthreads();
             for (int i = lane; i < w.tiles * kWeighRows; i += 64) {
                 sums[wave][i][0] = kWeighNone;
                 sums[wave][i][1] = 0.f;
             }
         }
-        float total[32];
-        if constexpr (PASS == kWeighTokens)
+        float total[16];
+        if constexpr (!kSums)
             for (float& t : total) t = 0.f;
         for (int block = w.block; block < w.block + w.blocks; ++block) {
             // the rows that see something of the block: tiles tile0 .. tile1 - 1
@@ -275,14 +272,13 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
             int tile1 = min(w.tile + w.tiles, static_cast<int>((static_cast<long long>(row_b) * a.group + kWeighRows - 1) / kWeighRows));
             if (t_end <= t_begin) tile1 = tile0;
             if (tile0 >= tile1) continue;
-            // the wave's 64 tokens
-            const int mine = t_begin + 64 * wave;
-            f16x8 k[2][D / 16];
-            float unit[4];                        // of 16 tokens each: scale of the scores
+            // the wave's 32 tokens
+            const int mine = t_begin + 32 * wave;
+            f16x8 k[D / 16];
+            float unit[2];                        // of 16 tokens each: scale of the scores
             unsigned there = 0;                   // which of those have a page
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int token = mine + 32 * t + lrow;
+            {
+                const int token = mine + lrow;
                 const int page = token < t_end ? table[token >> a.c.page_shift] : -1;
                 const bool is = page >= 0 && page < a.c.num_pages;
                 const size_t ph = static_cast<size_t>(is ? page : 0) * a.c.kv_heads + w.head;
@@ -293,23 +289,18 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                 const float scale = a.c.scales[2 * ph] * a.scale;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
-                    k[t][2 * c] = to_half8(raw[c][0], raw[c][1]);
-                    k[t][2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
+                    k[2 * c] = to_half8(raw[c][0], raw[c][1]);
+                    k[2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    unit[2 * t + g] = lane_of(scale, 16 * g);
-                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << (2 * t + g);
+                    unit[g] = lane_of(scale, 16 * g);
+                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << g;
                 }
             }
             // Row r of the sequence is token r / group, head r % group; a tile's first row as both, uniform.
-            const int step_t = kWeighRows / a.group, step_g = kWeighRows - step_t * a.group;
             struct TileAt {
                 int t, g;
-            };
-            auto at_tile = [&](int tile) {
-                const int r = tile * kWeighRows, t = r / a.group;
-                return TileAt{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(r - t * a.group)};
             };
             auto step = [&](TileAt& p) {
                 p.t += step_t;
@@ -325,21 +316,21 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                 return w.head * a.group + p.g + i - j * a.group;
             };
             // a tile on its way, and the place of the next to load
-            u32x4 piece[kPer];
+            u32x4 piece;
             float log = 0.f, next_log = 0.f;
-            TileAt ahead = at_tile(tile0), now = ahead;
+            TileAt ahead;
+            ahead.t = __builtin_amdgcn_readfirstlane(tile0 * kWeighRows / a.group);
+            ahead.g = tile0 * kWeighRows - ahead.t * a.group;
+            TileAt now = ahead;
+            const int pi = tid / kSlices, pc = tid % kSlices;
             auto load = [&] {
-#pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int p = tid + 256 * u, i = p / kSlices;
-                    int token;
-                    const int h = row_of(ahead, i, token);
-                    piece[u] = u32x4{0, 0, 0, 0};
-                    if (token < s.n)
-                        piece[u] = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + p % kSlices * 8);
+                int token;
+                if (kPieces == kThreads || tid < kPieces) {
+                    const int h = row_of(ahead, pi, token);
+                    piece = u32x4{0, 0, 0, 0};
+                    if (token < s.n) piece = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + pc * 8);
                 }
-                if constexpr (PASS == kWeighTokens) {
-                    int token;
+                if constexpr (!kSums) {
                     const int h = row_of(ahead, lrow, token);
                     next_log = token < s.n ? a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + h] : INFINITY;
                 }
@@ -347,11 +338,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
             };
             // row i of slice c lies at i ^ c, so that neither a slice's rows nor a row's slices meet in a bank
             auto store = [&](int b) {
-#pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int p = tid + 256 * u, i = p / kSlices, c = p % kSlices;
-                    *reinterpret_cast<f16x8*>(rows[b][c][i ^ c]) = query8(piece[u], 0);
-                }
+                if (kPieces == kThreads || tid < kPieces) *reinterpret_cast<f16x8*>(rows[b][pc][pi ^ pc]) = query8(piece, 0);
             };
             load();
             __syncthreads();                      // the block before is done with the rows
@@ -367,86 +354,88 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(WeighArgs a) {
                     log = next_log;
                     if (tile + 2 < tile1) load();
                 }
-                f32x16 z[2];
+                f32x16 z;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+                for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int slice = 4 * c + 2 * half + u;
                         const f16x8 q = *reinterpret_cast<const f16x8*>(rows[b][slice][lrow ^ slice]);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][2 * c + u], q, z[t], 0, 0, 0);
+                        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[2 * c + u], q, z, 0, 0, 0);
                     }
-                // what the lane's row sees
-                int token;
-                row_of(now, lrow, token);
+                // do all of the tile's rows see all of the wave's tokens (rows past the last matter to none)?
+                const int position0 = s.first + now.t, position1 = position0 + step_t + 1;
+                const bool all = there == 3u && mine + 32 <= min(position0 + 1, t_end) &&
+                                 (a.window == 0 || position1 - a.window < mine);
+                const TileAt at = now;
                 step(now);
-                const int position = s.first + token;
-                const bool is = token < s.n;
-                const int see_end = is ? min(position + 1, t_end) : 0;
-                const int see_begin = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
-                const bool partly = __any(is && (mine < see_begin || mine + 64 > see_end)) || there != 15u;
-                // token e of the lane is seen if e's place in the wave's 64 is in [lo, lo + n), of groups with a page
-                const unsigned lo = static_cast<unsigned>(see_begin - mine - 4 * half);
-                const unsigned n = static_cast<unsigned>(max(see_end - see_begin, 0));
-                unsigned seen[4];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) seen[g] = there >> g & 1 ? n : 0;
-                auto unseen = [&](int e) { return static_cast<unsigned>(32 * (e / 16) + 8 * (e % 16 / 4) + e % 4) - lo >= seen[e / 8]; };
                 auto finish = [&](auto masked) {
-                    if constexpr (PASS == kWeighSpanSums) {
+                    unsigned lo = 0, n0 = 0, n1 = 0;       // tokens [lo, lo + n) of the lane's half, of either 16 with a page
+                    if constexpr (masked) {
+                        int token;
+                        row_of(at, lrow, token);
+                        const int position = s.first + token;
+                        const int see_end = token < s.n ? min(position + 1, t_end) : 0;
+                        const int see_begin = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
+                        lo = static_cast<unsigned>(see_begin - mine - 4 * half);
+                        const unsigned n = static_cast<unsigned>(max(see_end - see_begin, 0));
+                        n0 = there & 1 ? n : 0;
+                        n1 = there & 2 ? n : 0;
+                    }
+                    auto unseen = [&](int e) { return static_cast<unsigned>(8 * (e / 4) + e % 4) - lo >= (e / 8 ? n1 : n0); };
+                    if constexpr (kSums) {
                         float top = kWeighNone;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            float v = z[e / 16][e % 16] * unit[e / 8];
+                        for (int e = 0; e < 16; ++e) {
+                            float v = z[e] * unit[e / 8];
                             if constexpr (masked) v = unseen(e) ? -INFINITY : v;
-                            z[e / 16][e % 16] = v;
+                            z[e] = v;
                             top = fmaxf(top, v);
                         }
-                        const int r = (tile - w.tile) * kWeighRows + lrow;
-                        const float m0 = sums[wave][r][0], l0 = sums[wave][r][1];
+                        float* at_row = sums[wave][(tile - w.tile) * kWeighRows + lrow];
+                        const float m0 = at_row[0], l0 = at_row[1];
                         const float m = fmaxf(with_half(Larger(), top), m0);
                         float l = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) l += fast_exp2(z[e / 16][e % 16] - m);
+                        for (int e = 0; e < 16; ++e) l += fast_exp2(z[e] - m);
                         l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
                         if (half == 0) {
-                            sums[wave][r][0] = m;
-                            sums[wave][r][1] = l;
+                            at_row[0] = m;
+                            at_row[1] = l;
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            float v = fast_exp2(__builtin_fmaf(z[e / 16][e % 16], unit[e / 8], -my_log));
+                        for (int e = 0; e < 16; ++e) {
+                            float v = fast_exp2(__builtin_fmaf(z[e], unit[e / 8], -my_log));
                             if constexpr (masked) v = unseen(e) ? 0.f : v;
                             total[e] += v;
                         }
                     }
                 };
-                if (partly) finish(std::true_type());
-                else finish(std::false_type());
+                if (all) finish(std::false_type());
+                else finish(std::true_type());
             }
         }
-        if constexpr (PASS == kWeighSpanSums) {
+        if constexpr (kSums) {
             __syncthreads();
-            for (int r = tid; r < w.tiles * kWeighRows; r += 256) {
+            for (int r = tid; r < w.tiles * kWeighRows; r += kThreads) {
                 const int row = w.tile * kWeighRows + r;
                 if (row >= all_rows) break;
                 float m = kWeighNone, l = 0.f;
-                for (int i = 0; i < 4; ++i) m = fmaxf(m, sums[i][r][0]);
-                for (int i = 0; i < 4; ++i) l += sums[i][r][1] * fast_exp2(sums[i][r][0] - m);
+                for (int i = 0; i < kWeighWaves; ++i) m = fmaxf(m, sums[i][r][0]);
+                for (int i = 0; i < kWeighWaves; ++i) l += sums[i][r][1] * fast_exp2(sums[i][r][0] - m);
                 const int token = row / a.group, h = w.head * a.group + row - token * a.group;
                 const size_t span = w.block / WeighPlan::span_blocks(a, w.q, plan.span);
                 float* to = a.spans + ((span * a.rows + s.row0 + token) * a.q_heads + h) * 2;
                 *reinterpret_cast<f32x2*>(to) = f32x2{m, l};
             }
         } else {
-            const float sum = weigh_scatter(total);
-            const int t = 64 * wave + 32 * (lrow >> 4) + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
+            // lane e of 16 gets the sum of total[e] over them, then over the other 16 of the half
+            const float sum = with_row(Sum(), weigh_scatter(total));
+            const int t = 32 * wave + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
+            if (lrow >= 16) continue;
             if (w.chunks == 1) weigh_write(a, w, w.block * kWeighBlock + t, sum);
             else a.parts[static_cast<size_t>(w.slot) * kWeighBlock + t] = sum;
         }
@@ -588,7 +577,7 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
 }
 
 // L of a row: a head a lane, the spans in turns over the waves
-constexpr int kLogWaves = 8;
+constexpr int kLogWaves = 4;
 __global__ __launch_bounds__(kLogWaves * 64) void weigh_logs_kernel(WeighArgs a) {
     __shared__ f32x2 part[kLogWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
