@@ -22,11 +22,12 @@
 
 namespace tetra_dev {
 
-constexpr int kWeighBlock = 256;          // tokens of a workgroup, 32 of a wave
-constexpr int kWeighWaves = kWeighBlock / 32;
+constexpr int kWeighBlock = 256;          // tokens of a workgroup
+constexpr int kWeighTiles = 2;            // of 32 tokens, of a wave
+constexpr int kWeighWaves = kWeighBlock / (32 * kWeighTiles);
 constexpr int kWeighRows = 32;            // rows of a tile
 constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sums, at most
-constexpr int kWeighMostTiles = 16;       // row tiles whose sums a workgroup holds in LDS
+constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
 
@@ -229,12 +230,15 @@ __device__ __forceinline__ void weigh_write(const WeighArgs& a, const WeighItem&
 }
 
 template <int D, WeighPass PASS>
-__global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a) {
-    constexpr int kThreads = 64 * kWeighWaves, kSlices = D / 8, kPieces = kSlices * kWeighRows;   // 8 dimensions of a row each
-    static_assert(kPieces <= kThreads, "a piece of a tile of rows a thread");
+__global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a) {
+    constexpr int TT = kWeighTiles, kThreads = 64 * kWeighWaves, kSlices = D / 8;
+    constexpr int kPer = kSlices * kWeighRows / kThreads;       // a thread's pieces (8 dimensions) of a tile of rows
+    static_assert(kPer * kThreads == kSlices * kWeighRows, "whole pieces a thread");
     constexpr std::integral_constant<WeighPass, PASS> pass;
     constexpr bool kSums = PASS == kWeighSpanSums;
-    __shared__ __align__(16) _Float16 rows[2][kSlices][kWeighRows][8];
+    // a slice's rows, and one row more, so that neither a slice's rows nor a row's slices meet in a bank
+    __shared__ __align__(16) _Float16 rows[2][kSlices][kWeighRows + 1][8];
+    __shared__ float row_logs[2][kWeighRows];
     __shared__ float sums[kSums ? kWeighWaves : 1][kSums ? kWeighMostTiles * kWeighRows : 1][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lrow = lane & 31, half = lane >> 5;
@@ -259,9 +263,10 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
                 sums[wave][i][1] = 0.f;
             }
         }
-        float total[16];
+        float total[TT][16];
         if constexpr (!kSums)
-            for (float& t : total) t = 0.f;
+            for (auto& t : total)
+                for (float& v : t) v = 0.f;
         for (int block = w.block; block < w.block + w.blocks; ++block) {
             // the rows that see something of the block: tiles tile0 .. tile1 - 1
             const int t_begin = block * kWeighBlock, t_end = min(t_begin + kWeighBlock, w.q.end);
@@ -272,13 +277,14 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
             int tile1 = min(w.tile + w.tiles, static_cast<int>((static_cast<long long>(row_b) * a.group + kWeighRows - 1) / kWeighRows));
             if (t_end <= t_begin) tile1 = tile0;
             if (tile0 >= tile1) continue;
-            // the wave's 32 tokens
-            const int mine = t_begin + 32 * wave;
-            f16x8 k[D / 16];
-            float unit[2];                        // of 16 tokens each: scale of the scores
+            // the wave's tokens
+            const int mine = t_begin + 32 * TT * wave;
+            f16x8 k[TT][D / 16];
+            float unit[TT][2];                    // of 16 tokens each: scale of the scores
             unsigned there = 0;                   // which of those have a page
-            {
-                const int token = mine + lrow;
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const int token = mine + 32 * t + lrow;
                 const int page = token < t_end ? table[token >> a.c.page_shift] : -1;
                 const bool is = page >= 0 && page < a.c.num_pages;
                 const size_t ph = static_cast<size_t>(is ? page : 0) * a.c.kv_heads + w.head;
@@ -289,13 +295,13 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
                 const float scale = a.c.scales[2 * ph] * a.scale;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
-                    k[2 * c] = to_half8(raw[c][0], raw[c][1]);
-                    k[2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
+                    k[t][2 * c] = to_half8(raw[c][0], raw[c][1]);
+                    k[t][2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    unit[g] = lane_of(scale, 16 * g);
-                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << g;
+                    unit[t][g] = lane_of(scale, 16 * g);
+                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << (2 * t + g);
                 }
             }
             // Row r of the sequence is token r / group, head r % group; a tile's first row as both, uniform.
@@ -316,63 +322,66 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
                 return w.head * a.group + p.g + i - j * a.group;
             };
             // a tile on its way, and the place of the next to load
-            u32x4 piece;
-            float log = 0.f, next_log = 0.f;
+            u32x4 piece[kPer];
+            float next_log = 0.f;
             TileAt ahead;
             ahead.t = __builtin_amdgcn_readfirstlane(tile0 * kWeighRows / a.group);
             ahead.g = tile0 * kWeighRows - ahead.t * a.group;
             TileAt now = ahead;
-            const int pi = tid / kSlices, pc = tid % kSlices;
+            const int pc = tid % kSlices;
             auto load = [&] {
                 int token;
-                if (kPieces == kThreads || tid < kPieces) {
-                    const int h = row_of(ahead, pi, token);
-                    piece = u32x4{0, 0, 0, 0};
-                    if (token < s.n) piece = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + pc * 8);
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const int h = row_of(ahead, (tid + u * kThreads) / kSlices, token);
+                    piece[u] = u32x4{0, 0, 0, 0};
+                    if (token < s.n) piece[u] = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + pc * 8);
                 }
-                if constexpr (!kSums) {
+                if (!kSums && wave == 0) {
                     const int h = row_of(ahead, lrow, token);
                     next_log = token < s.n ? a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + h] : INFINITY;
                 }
                 step(ahead);
             };
-            // row i of slice c lies at i ^ c, so that neither a slice's rows nor a row's slices meet in a bank
             auto store = [&](int b) {
-                if (kPieces == kThreads || tid < kPieces) *reinterpret_cast<f16x8*>(rows[b][pc][pi ^ pc]) = query8(piece, 0);
+#pragma unroll
+                for (int u = 0; u < kPer; ++u)
+                    *reinterpret_cast<f16x8*>(rows[b][pc][(tid + u * kThreads) / kSlices]) = query8(piece[u], 0);
+                if (!kSums && wave == 0) row_logs[b][lrow] = next_log;
             };
             load();
             __syncthreads();                      // the block before is done with the rows
             store(0);
-            log = next_log;
             if (tile0 + 1 < tile1) load();
             for (int tile = tile0; tile < tile1; ++tile) {
                 const int b = (tile - tile0) & 1;
                 __syncthreads();
-                const float my_log = log;
                 if (tile + 1 < tile1) {
                     store(b ^ 1);
-                    log = next_log;
                     if (tile + 2 < tile1) load();
                 }
-                f32x16 z;
+                const float my_log = kSums ? 0.f : row_logs[b][lrow];
+                f32x16 z[TT];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = 0.f;
+                for (int t = 0; t < TT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int slice = 4 * c + 2 * half + u;
-                        const f16x8 q = *reinterpret_cast<const f16x8*>(rows[b][slice][lrow ^ slice]);
-                        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[2 * c + u], q, z, 0, 0, 0);
+                        const f16x8 q = *reinterpret_cast<const f16x8*>(rows[b][4 * c + 2 * half + u][lrow]);
+#pragma unroll
+                        for (int t = 0; t < TT; ++t) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][2 * c + u], q, z[t], 0, 0, 0);
                     }
                 // do all of the tile's rows see all of the wave's tokens (rows past the last matter to none)?
                 const int position0 = s.first + now.t, position1 = position0 + step_t + 1;
-                const bool all = there == 3u && mine + 32 <= min(position0 + 1, t_end) &&
+                const bool all = there == (1u << 2 * TT) - 1 && mine + 32 * TT <= min(position0 + 1, t_end) &&
                                  (a.window == 0 || position1 - a.window < mine);
                 const TileAt at = now;
                 step(now);
                 auto finish = [&](auto masked) {
-                    unsigned lo = 0, n0 = 0, n1 = 0;       // tokens [lo, lo + n) of the lane's half, of either 16 with a page
+                    unsigned lo = 0, n = 0;                // tokens [lo, lo + n) of the lane's half, of those with a page
                     if constexpr (masked) {
                         int token;
                         row_of(at, lrow, token);
@@ -380,26 +389,30 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
                         const int see_end = token < s.n ? min(position + 1, t_end) : 0;
                         const int see_begin = a.window > 0 ? max(0, max(position, 0) - a.window + 1) : 0;
                         lo = static_cast<unsigned>(see_begin - mine - 4 * half);
-                        const unsigned n = static_cast<unsigned>(max(see_end - see_begin, 0));
-                        n0 = there & 1 ? n : 0;
-                        n1 = there & 2 ? n : 0;
+                        n = static_cast<unsigned>(max(see_end - see_begin, 0));
                     }
-                    auto unseen = [&](int e) { return static_cast<unsigned>(8 * (e / 4) + e % 4) - lo >= (e / 8 ? n1 : n0); };
+                    auto unseen = [&](int t, int e) {
+                        return static_cast<unsigned>(32 * t + 8 * (e / 4) + e % 4) - lo >= n || !(there >> (2 * t + e / 8) & 1);
+                    };
                     if constexpr (kSums) {
                         float top = kWeighNone;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float v = z[e] * unit[e / 8];
-                            if constexpr (masked) v = unseen(e) ? -INFINITY : v;
-                            z[e] = v;
-                            top = fmaxf(top, v);
-                        }
+                        for (int t = 0; t < TT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                float v = z[t][e] * unit[t][e / 8];
+                                if constexpr (masked) v = unseen(t, e) ? -INFINITY : v;
+                                z[t][e] = v;
+                                top = fmaxf(top, v);
+                            }
                         float* at_row = sums[wave][(tile - w.tile) * kWeighRows + lrow];
                         const float m0 = at_row[0], l0 = at_row[1];
                         const float m = fmaxf(with_half(Larger(), top), m0);
                         float l = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) l += fast_exp2(z[e] - m);
+                        for (int t = 0; t < TT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) l += fast_exp2(z[t][e] - m);
                         l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
                         if (half == 0) {
                             at_row[0] = m;
@@ -407,11 +420,13 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float v = fast_exp2(__builtin_fmaf(z[e], unit[e / 8], -my_log));
-                            if constexpr (masked) v = unseen(e) ? 0.f : v;
-                            total[e] += v;
-                        }
+                        for (int t = 0; t < TT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                float v = fast_exp2(__builtin_fmaf(z[t][e], unit[t][e / 8], -my_log));
+                                if constexpr (masked) v = unseen(t, e) ? 0.f : v;
+                                total[t][e] += v;
+                            }
                     }
                 };
                 if (all) finish(std::false_type());
@@ -433,11 +448,14 @@ __global__ __launch_bounds__(64 * kWeighWaves, 4) void weigh_kernel(WeighArgs a)
             }
         } else {
             // lane e of 16 gets the sum of total[e] over them, then over the other 16 of the half
-            const float sum = with_row(Sum(), weigh_scatter(total));
-            const int t = 32 * wave + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
-            if (lrow >= 16) continue;
-            if (w.chunks == 1) weigh_write(a, w, w.block * kWeighBlock + t, sum);
-            else a.parts[static_cast<size_t>(w.slot) * kWeighBlock + t] = sum;
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const float sum = with_row(Sum(), weigh_scatter(total[t]));
+                const int place = 32 * (TT * wave + t) + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
+                if (lrow >= 16) continue;
+                if (w.chunks == 1) weigh_write(a, w, w.block * kWeighBlock + place, sum);
+                else a.parts[static_cast<size_t>(w.slot) * kWeighBlock + place] = sum;
+            }
         }
     }
 }
