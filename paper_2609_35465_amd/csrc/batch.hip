@@ -41,7 +41,9 @@ struct WeighSpace {
         workers = cus * kWeighGroupsPerCU;
         logs = (static_cast<size_t>(rows) * q_heads + 63) / 64 * 64;
         spans = logs * tetra_dev::kWeighSpans * 2;
-        bytes = rounded(256 + sizeof(float) * (spans + logs + 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock));
+        // single tokens' scores, or prompts' parts
+        const size_t parts = 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock;
+        bytes = rounded(256 + sizeof(float) * (spans + logs + std::max<size_t>(parts, tetra_dev::kWeighScores)));
     }
 };
 
@@ -133,7 +135,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.span = static_cast<int*>(workspace);
     a.spans = static_cast<float*>(workspace) + 64;
     a.logs = a.spans + space.spans;
-    a.parts = a.logs + space.logs;
+    a.parts = a.scores = a.logs + space.logs;
     a.q_stride = q_stride;
     a.scale = scale * 1.44269504f;
     a.decay = decay;
@@ -143,6 +145,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
     a.mass_tokens = mass_tokens;
+    a.score_rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_new) * a.group, tetra_dev::kWeighRows));
     return cache->head_dim == 64 ? weigh_launch<64>(a, cus, stream) : weigh_launch<128>(a, cus, stream);
 }
 

@@ -30,6 +30,7 @@ constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sum
 constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
+constexpr long long kWeighScores = 16 << 20;   // scores that single tokens' first pass may leave for the second
 
 struct WeighArgs {
     KvCache c;
@@ -47,6 +48,8 @@ struct WeighArgs {
     int workers;          // workgroups, or waves, that share the items of a launch
     int block, spans_most;   // tokens of a block; spans of a sequence at most
     int* span;               // the blocks of a span, at least, for the kernel of the logs
+    float* scores;           // [blocks of all sequences and heads][rows of a sequence][64], of weigh_few_kernel
+    int score_rows;          // rows of a sequence and cache head at most
 };
 
 // What a sequence asks for.
@@ -77,6 +80,7 @@ struct WeighItem {
     int seq, head, block, blocks, tile, tiles;      // blocks `block` .. block + blocks - 1, tiles likewise
     int chunks;                                     // of the block
     int slot;                                       // of the item's part, where there are several chunks
+    int before;                                     // slots of the sequences before
     WeighSeq q;
 };
 
@@ -87,6 +91,7 @@ enum WeighPass { kWeighSpanSums, kWeighTokens, kWeighJoin };
 struct WeighPlan {
     int chunk, total;             // row tiles of a chunk; items
     int span;                     // blocks of a span, at least
+    bool keep;                    // there is room for all scores
     int lane_items, lane_slots;   // of a lane's sequence, the first 64
 
     __device__ __forceinline__ static int span_blocks(const WeighArgs& a, const WeighSeq& q, int least) {
@@ -123,18 +128,20 @@ struct WeighPlan {
         }
         steps = wave_all(Sum(), steps);
         span = 1;
+        keep = false;
         if (FEW) {
             // an item a wave, of equal spans: each sequence and head may have one that is not full
             const long long ends = static_cast<long long>(wave_all(Sum(), live)) * a.c.kv_heads;
             const long long room = max(static_cast<long long>(a.workers) - ends, static_cast<long long>(a.workers / 2));
             blocks = wave_all(Sum(), blocks) * a.c.kv_heads;
             span = static_cast<int>(max(1ll, min((static_cast<long long>(blocks) + room - 1) / room, 1ll << 24)));
+            keep = static_cast<long long>(blocks) <= kWeighScores / 64 / a.score_rows;
         }
         const unsigned long long most = static_cast<unsigned long long>(kWeighItems) * a.workers;
         chunk = static_cast<int>(max(1ull, min((steps + most - 1) / most, 1ull << 26)));
         if (PASS == kWeighSpanSums) chunk = min(chunk, kWeighMostTiles);
         lane_items = items_of<PASS>(a, mine);
-        lane_slots = slots_of(a, mine);
+        lane_slots = FEW ? mine.blocks * a.c.kv_heads : slots_of(a, mine);
         total = wave_all(Sum(), lane_items);
         for (int i0 = 64; i0 < a.c.seqs; i0 += 64) {
             int n = 0;
@@ -144,9 +151,10 @@ struct WeighPlan {
     }
 
     // item x of all; the sequences a lane each
-    template <WeighPass PASS>
+    template <WeighPass PASS, bool FEW = false>
     __device__ __forceinline__ WeighItem find(const WeighArgs& a, const WeighSeq& first, int x,
-                                              std::integral_constant<WeighPass, PASS>) const {
+                                              std::integral_constant<WeighPass, PASS>,
+                                              std::integral_constant<bool, FEW> = {}) const {
         const int lane = threadIdx.x & 63;
         WeighItem w;
         w.seq = -1;
@@ -158,7 +166,7 @@ struct WeighPlan {
                 q = WeighSeq();
                 if (i0 + lane < a.c.seqs) q = WeighSeq(a, i0 + lane);
                 n = items_of<PASS>(a, q);
-                m = slots_of(a, q);
+                m = FEW ? q.blocks * a.c.kv_heads : slots_of(a, q);
             }
             const int upto = wave_upto(Sum(), n) + before, slots_upto = wave_upto(Sum(), m) + slots;
             const unsigned long long has = __ballot(upto > x);
@@ -184,7 +192,8 @@ struct WeighPlan {
                 }
                 w.tile = part * chunk;
                 w.tiles = min(chunk, w.q.tiles - w.tile);
-                w.slot = lane_of(slots_upto - m, l) + (place * w.chunks) + part;
+                w.before = lane_of(slots_upto - m, l);
+                w.slot = w.before + (place * w.chunks) + part;
                 return w;
             }
             before = lane_of(upto, 63);
@@ -476,10 +485,42 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
     const WeighPlan plan(a, first, pass, std::true_type());
     if (PASS == kWeighSpanSums && wave == 0 && lane == 0) *a.span = plan.span;
     for (int x = wave; x < plan.total; x += a.workers) {
-        const WeighItem w = plan.find(a, first, x, pass);
+        const WeighItem w = plan.find(a, first, x, pass, std::true_type());
         const Span& s = w.q.s;
         const int* table = a.c.pages + static_cast<size_t>(w.seq) * a.c.max_pages;
         const int blocks_end = w.block + w.blocks;
+        // the block's scores: a row after another, a token a lane
+        auto scores_of = [&](int block) {
+            return a.scores + (static_cast<size_t>(w.before) + static_cast<size_t>(w.head) * w.q.blocks + block) * a.score_rows * 64;
+        };
+        if (PASS == kWeighTokens && plan.keep) {
+            // the rows' sums a lane each; eight rows' scores of a block at once, the first of the next on their way
+            constexpr int kAhead = 8;
+            const int rows = s.n * a.group, token = lane / a.group;
+            float logs = INFINITY, z[kAhead];
+            if (lane < rows) logs = a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + w.head * a.group + lane - token * a.group];
+            auto load = [&](int block, int i0) {
+                const float* p = scores_of(block) + lane;
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) z[j] = rows > 0 ? p[64 * min(i0 + j, rows - 1)] : -INFINITY;
+            };
+            load(w.block, 0);
+            for (int block = w.block; block < blocks_end; ++block) {
+                float sum = 0.f;
+                for (int i0 = 0; i0 < max(rows, 1); i0 += kAhead) {
+                    float now[kAhead];
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j) now[j] = z[j];
+                    if (i0 + kAhead < rows) load(block, i0 + kAhead);
+                    else if (block + 1 < blocks_end) load(block + 1, 0);
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)      // of rows past the last L is infinite
+                        sum += now[j] == -INFINITY ? 0.f : fast_exp2(now[j] - lane_of(logs, min(i0 + j, 63)));
+                }
+                weigh_write(a, w, block * 64 + lane, sum);
+            }
+            continue;
+        }
         auto page_at = [&](int t) { return t < w.q.end ? table[t >> a.c.page_shift] : -1; };
         struct Keys {
             u32x4 raw[4][C];
@@ -569,6 +610,11 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
                     float sum = 0.f;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) sum += fast_exp2(total[e] - top);
+                    if (plan.keep && is[n])
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<f32x4*>(scores_of(block) + (16 * n + r) * 64 + 16 * g + e) =
+                                f32x4{total[e], total[e + 1], total[e + 2], total[e + 3]};
                     l[n] = l[n] * fast_exp2(m[n] - top) + sum;      // of this lane's tokens
                     m[n] = top;
                 } else {
