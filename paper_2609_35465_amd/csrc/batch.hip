@@ -137,7 +137,8 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.logs = a.spans + space.spans;
     a.parts = a.scores = a.logs + space.logs;
     a.q_stride = q_stride;
-    a.scale = scale * 1.44269504f;
+    a.scale = std::fabs(scale) * 1.44269504f;
+    a.q_flip = scale < 0.f ? 0x80008000u : 0u;
     a.decay = decay;
     a.rows = rows;
     a.max_new = max_new;

@@ -23,11 +23,11 @@
 namespace tetra_dev {
 
 constexpr int kWeighBlock = 256;          // tokens of a workgroup
-constexpr int kWeighTiles = 2;            // of 32 tokens, of a wave
+constexpr int kWeighTiles = 1;            // of 32 tokens, of a wave
 constexpr int kWeighWaves = kWeighBlock / (32 * kWeighTiles);
 constexpr int kWeighRows = 32;            // rows of a tile
 constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sums, at most
-constexpr int kWeighMostTiles = 32;       // row tiles whose sums a workgroup holds in LDS
+constexpr int kWeighMostTiles = 16;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
 constexpr long long kWeighScores = 16 << 20;   // scores that single tokens' first pass may leave for the second
@@ -42,7 +42,8 @@ struct WeighArgs {
     float* logs;          // [rows][q_heads]: L, +inf where a row sees nothing
     float* parts;         // [2 kWeighItems workers][kWeighBlock]: a block's sums over some of its rows
     long long q_stride;
-    float scale;          // scale log2(e)
+    float scale;          // |scale| log2(e)
+    uint32_t q_flip;      // 0x80008000 if the scale is negative: turns q instead
     float decay;
     int rows, max_new, q_heads, group, window, mass_tokens;
     int workers;          // workgroups, or waves, that share the items of a launch
@@ -239,10 +240,11 @@ __device__ __forceinline__ void weigh_write(const WeighArgs& a, const WeighItem&
 }
 
 template <int D, WeighPass PASS>
-__global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a) {
+__global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_kernel(WeighArgs a) {
     constexpr int TT = kWeighTiles, kThreads = 64 * kWeighWaves, kSlices = D / 8;
-    constexpr int kPer = kSlices * kWeighRows / kThreads;       // a thread's pieces (8 dimensions) of a tile of rows
-    static_assert(kPer * kThreads == kSlices * kWeighRows, "whole pieces a thread");
+    constexpr int kPieces = kSlices * kWeighRows;               // of 8 dimensions, of a tile of rows
+    constexpr int kPer = (kPieces + kThreads - 1) / kThreads;   // and of a thread
+    static_assert(kPieces % kThreads == 0 || kPer == 1, "all of a thread's or none");
     constexpr std::integral_constant<WeighPass, PASS> pass;
     constexpr bool kSums = PASS == kWeighSpanSums;
     // a slice's rows, and one row more, so that neither a slice's rows nor a row's slices meet in a bank
@@ -338,13 +340,28 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a)
             ahead.g = tile0 * kWeighRows - ahead.t * a.group;
             TileAt now = ahead;
             const int pc = tid % kSlices;
+            // where the heads of a cache head divide a tile, a thread's pieces of a tile are step_t tokens after those before
+            const uint16_t* from[kPer];
+            int from_token[kPer];
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                const int h = row_of(ahead, (tid + u * kThreads) / kSlices, from_token[u]);
+                from[u] = a.q + (s.row0 + from_token[u]) * a.q_stride + h * D + pc * 8;
+            }
             auto load = [&] {
                 int token;
 #pragma unroll
                 for (int u = 0; u < kPer; ++u) {
-                    const int h = row_of(ahead, (tid + u * kThreads) / kSlices, token);
                     piece[u] = u32x4{0, 0, 0, 0};
-                    if (token < s.n) piece[u] = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + pc * 8);
+                    if (kPieces < kThreads && tid >= kPieces) continue;
+                    if (step_g == 0) {
+                        if (from_token[u] < s.n) piece[u] = *reinterpret_cast<const u32x4*>(from[u]);
+                        from_token[u] += step_t;
+                        from[u] += step_t * a.q_stride;
+                    } else {
+                        const int h = row_of(ahead, (tid + u * kThreads) / kSlices, token);
+                        if (token < s.n) piece[u] = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + pc * 8);
+                    }
                 }
                 if (!kSums && wave == 0) {
                     const int h = row_of(ahead, lrow, token);
@@ -355,7 +372,8 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a)
             auto store = [&](int b) {
 #pragma unroll
                 for (int u = 0; u < kPer; ++u)
-                    *reinterpret_cast<f16x8*>(rows[b][pc][(tid + u * kThreads) / kSlices]) = query8(piece[u], 0);
+                    if (kPieces >= kThreads || tid < kPieces)
+                        *reinterpret_cast<f16x8*>(rows[b][pc][(tid + u * kThreads) / kSlices]) = query8(piece[u], a.q_flip);
                 if (!kSums && wave == 0) row_logs[b][lrow] = next_log;
             };
             load();
@@ -404,15 +422,19 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a)
                         return static_cast<unsigned>(32 * t + 8 * (e / 4) + e % 4) - lo >= n || !(there >> (2 * t + e / 8) & 1);
                     };
                     if constexpr (kSums) {
+                        // the largest before the scale, which is the same for 8 of a lane and not below 0
                         float top = kWeighNone;
 #pragma unroll
                         for (int t = 0; t < TT; ++t)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float v = z[t][e] * unit[t][e / 8];
-                                if constexpr (masked) v = unseen(t, e) ? -INFINITY : v;
-                                z[t][e] = v;
-                                top = fmaxf(top, v);
+                            for (int g = 0; g < 2; ++g) {
+                                float most = -INFINITY;
+#pragma unroll
+                                for (int e = 8 * g; e < 8 * g + 8; ++e) {
+                                    if constexpr (masked) z[t][e] = unseen(t, e) ? -INFINITY : z[t][e];
+                                    most = fmaxf(most, z[t][e]);
+                                }
+                                top = fmaxf(top, most > -INFINITY ? most * unit[t][g] : -INFINITY);
                             }
                         float* at_row = sums[wave][(tile - w.tile) * kWeighRows + lrow];
                         const float m0 = at_row[0], l0 = at_row[1];
@@ -421,7 +443,11 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighArgs a)
 #pragma unroll
                         for (int t = 0; t < TT; ++t)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) l += fast_exp2(z[t][e] - m);
+                            for (int e = 0; e < 16; ++e) {
+                                float v = fast_exp2(__builtin_fmaf(z[t][e], unit[t][e / 8], -m));
+                                if constexpr (masked) v = z[t][e] == -INFINITY ? 0.f : v;
+                                l += v;
+                            }
                         l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
                         if (half == 0) {
                             at_row[0] = m;
@@ -559,7 +585,7 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
                 u32x4 v = {0, 0, 0, 0};
                 if (is[n])
                     v = *reinterpret_cast<const u32x4*>(a.q + (s.row0 + token) * a.q_stride + h * D + 64 * (c / 2) + 16 * g + 8 * (c % 2));
-                q[n][c] = query8(v, 0);
+                q[n][c] = query8(v, a.q_flip);
             }
             m[n] = kWeighNone;
             l[n] = 0.f;

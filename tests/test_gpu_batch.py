@@ -358,6 +358,12 @@ def test_weigh_fewer_or_more_places_than_tokens(places):
     _check_weigh(Cache(26, [300, 77, 0, 256], 2, 32, 64), [1, 20, 0, 40], 4, places=places)
 
 
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1.0])
+@pytest.mark.parametrize("news", [(1, 3), (90, 70)])
+def test_weigh_scale_argument(scale, news):
+    _check_weigh(Cache(32, [300, 77], 2, 32, 64), list(news), 6, scale=scale, q_size=0.5)
+
+
 def test_weigh_many_sequences():
     rng = np.random.default_rng(0)
     news = rng.integers(0, 4, 300)
