@@ -602,7 +602,7 @@ def kv_evict(cache: KVCache, to: KVCache, mass, mass_out, workspace, recent: int
 
 
 def log_probs_workspace(rows: int, vocab: int, top: int = 0):
-    """A workspace for log_probs over rows of vocab logits with `top` alternatives (a torch uint8 tensor)."""
+    """A workspace for log_probs over up to `rows` rows of vocab logits with `top` alternatives (a torch uint8 tensor)."""
     return _space("tetra_log_probs_workspace_bytes", rows, vocab, top)
 
 
@@ -618,7 +618,7 @@ def log_probs(logits, tokens, out, workspace, entropy=None, top_tokens=None, top
     ok = (half or logits.dtype is f32) and (logits.stride(1) == 1 or vocab == 1) and workspace.is_contiguous() and rows > 0
     given = top = 0
     for t, kind in ((tokens, i32), (out, f32), (entropy, f32), (top_tokens, i32), (top_out, f32), (temperature, f32)):
-        ok = ok and (t is None or (t.dtype is kind and t.is_contiguous()))
+        ok = ok and (t is None or (t.dtype is kind and t.is_contiguous() and t.dim() > 0))
     for t in (entropy, temperature):
         ok = ok and (t is None or t.numel() == rows)
     ok = ok and (tokens is None) == (out is None) and (top_tokens is None) == (top_out is None)

@@ -166,6 +166,7 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
     if (!mass || !workspace || mass_tokens < 1 || recent < 0 || (mass_out && out_tokens < 1) || mass_out == mass)
         return TETRA_EINVAL;
     if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(workspace, 256)) return TETRA_EALIGN;
+    if (from->pages == to->pages && from->k == to->k) return TETRA_EINVAL;      // into the pages that it reads
     const EvictSpace space(from, to);
     if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     const long long units = static_cast<long long>(a.from.seqs) * a.from.kv_heads;
@@ -199,8 +200,7 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
 size_t tetra_log_probs_workspace_bytes(int rows, int vocab, int top) {
     int cus = 0;
     if (rows < 1 || vocab < 1 || vocab > kMaxVocab || top < 0 || top > tetra_dev::kMostTop || device_cus(&cus)) return 0;
-    const int parts = tetra_dev::score_shape(rows, vocab, cus).parts;
-    return parts > 1 ? rounded(static_cast<size_t>(rows) * parts * (16 + 8 * top)) : kMinWorkspace;
+    return rounded(tetra_dev::score_entries(rows, vocab, cus) * (16 + 8 * static_cast<size_t>(top)));
 }
 
 int tetra_log_probs(const void* logits, int half, long long stride, int rows, int vocab, const float* temperature,

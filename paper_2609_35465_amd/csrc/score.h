@@ -511,18 +511,26 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
     }
 }
 
-// parts of a row, and the bytes that they leave
+// Parts of a row, so that there are four workgroups a CU over all rows and each wave has
+// a batch; and the most that this many rows, or fewer, leave for the join.
 struct ScoreShape {
     int parts, part;
 };
+inline int score_batches(int vocab) { return (vocab + kScoreBatch - 1) / kScoreBatch; }
+inline int score_most_parts(int vocab) {
+    const int most = (score_batches(vocab) + 3) / 4;
+    return most < kMostScoreParts ? most : kMostScoreParts;
+}
 inline ScoreShape score_shape(int rows, int vocab, int cus) {
-    const int batches = (vocab + kScoreBatch - 1) / kScoreBatch;
     int parts = 4 * cus / rows;
-    parts = parts < kMostScoreParts ? parts : kMostScoreParts;
-    parts = parts < (batches + 3) / 4 ? parts : (batches + 3) / 4;
-    if (parts < 1) parts = 1;
+    const int most = score_most_parts(vocab), batches = score_batches(vocab);
+    parts = parts < 1 ? 1 : parts < most ? parts : most;
     const int part = (batches + parts - 1) / parts;
     return {(batches + part - 1) / part, part * kScoreBatch};
+}
+inline size_t score_entries(int rows, int vocab, int cus) {
+    const size_t n = static_cast<size_t>(rows) * score_most_parts(vocab), most = 4 * static_cast<size_t>(cus);
+    return n < most ? n : most;
 }
 
 }  // namespace tetra_dev

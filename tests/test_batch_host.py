@@ -92,6 +92,7 @@ def test_evict_validation():
         assert _evict(**args) == tt.EINVAL, args
     for args in (dict(mass=FAKE + 2), dict(out=FAKE + 1), dict(ws=FAKE + 16)):
         assert _evict(**args) == tt.EALIGN, args
+    assert _evict(to=_cache(lens=FAKE + 64, num_pages=9)) == tt.EINVAL            # into the pages that it reads
     for change in (dict(kv_heads=1), dict(head_dim=128), dict(page_tokens=32), dict(seqs=2)):
         assert _evict(to=_cache(**change)) == tt.EINVAL, change
     size, c = tt.library().tetra_kv_evict_workspace_bytes, _cache()
@@ -166,7 +167,7 @@ def test_binding_refuses_other_shapes_types_and_places():
                      ((x, torch.zeros((1, 3), dtype=i32), torch.zeros((1, 3)), ws), {}),
                      ((x, t1, out, ws), dict(entropy=f[:2])), ((x, t1, out, ws), dict(temperature=f.half())),
                      ((x, t1, out, ws), dict(top_tokens=top)), ((x, t1, out, ws), dict(top_tokens=top, top_out=f)),
-                     ((x[:0], t1, out, ws), {})):
+                     ((x[:0], t1, out, ws), {}), ((x, t1, out, ws), dict(entropy=f[0])), ((x[:1], t1[0, 0], out[0, 0], ws), {})):
         _refused(tt.log_probs, *args, **kw)
     k = torch.zeros((3, 2, 64))
     for shifts in (torch.zeros(2, dtype=i32), torch.zeros(3), torch.zeros((3, 2), dtype=i32)[:, 0]):

@@ -774,6 +774,19 @@ def test_score_large_logits():
     _check_score(x, top=5)
 
 
+def test_score_workspace_serves_fewer_rows():
+    """One for the largest batch serves every smaller one, whose rows are cut in more parts."""
+    vocab, top = 30000, 7
+    x = _dev(np.random.default_rng(0).standard_normal((900, vocab)).astype(np.float32))
+    space = tt.log_probs_workspace(900, vocab, top)
+    for rows in (900, 513, 300, 64, 5, 1):
+        ids, logs = torch.zeros((rows, top), dtype=torch.int32, device="cuda"), torch.zeros((rows, top), device="cuda")
+        tt.log_probs(x[:rows], None, None, space, top_tokens=ids, top_out=logs)
+        torch.cuda.synchronize()
+        want = torch.log_softmax(x[:rows].double(), -1).topk(top)
+        assert torch.equal(ids.long(), want.indices) and torch.allclose(logs.double(), want.values, atol=1e-4)
+
+
 def test_score_nothing_but_what_is_asked_for():
     x = _dev(np.random.default_rng(0).standard_normal((3, 400)).astype(np.float32))
     space, ent = tt.log_probs_workspace(3, 400), torch.zeros(3, device="cuda")
