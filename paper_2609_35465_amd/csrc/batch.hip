@@ -28,10 +28,15 @@ bool sizes_ok(const tetra_kv_cache* c) {
     return c->max_pages <= kMaxTokens / c->page_tokens && (c->head_dim == 64 || c->head_dim == 128);
 }
 
+// As many as a CU holds by their registers.
 constexpr int kWeighGroupsPerCU = 2, kWeighFewGroupsPerCU = 4;
 
-// sequences of at most one row tile each: known from max_new
-bool weigh_few(int max_new, int group) { return static_cast<long long>(max_new) * group <= tetra_dev::kWeighRows; }
+// Sequences whose rows a wave holds in registers beside its keys: 16 of a cache head of 128, 32
+// of one of 64.  Then the keys are what is read: 64 sequences of up to 4,096 tokens, 5 rows
+// 39 us by weigh_few_kernel and 73 by weigh_kernel, whose rows go through LDS with a barrier; 16
+// rows 22-41 and 30-73 by batch; heads of 64, 32 rows 14-43 and 16-62.  With heads of
+// 128, 20 rows took 28 and 22 (8 sequences) to 62 and 73 (64), 32 rows 37 and 30 (16).
+bool weigh_few(int max_new, int group, int head_dim) { return static_cast<long long>(max_new) * group * head_dim <= 2048; }
 
 // floats of kv_weigh's workspace
 struct WeighSpace {
@@ -49,15 +54,15 @@ struct WeighSpace {
 
 template <int D>
 int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
-    const bool few = weigh_few(a.max_new, a.group);
+    const bool few = weigh_few(a.max_new, a.group, D);
     const dim3 b(256), m(64 * tetra_dev::kWeighWaves), g(static_cast<unsigned>(cus * (few ? kWeighFewGroupsPerCU : kWeighGroupsPerCU)));
     a.workers = static_cast<int>(few ? 4 * g.x : g.x);
     a.block = few ? 64 : tetra_dev::kWeighBlock;
     a.spans_most = few ? tetra_dev::kWeighSpans : tetra_dev::kWeighSpans / 4;
-    const bool one = static_cast<long long>(a.max_new) * a.group <= 16;
+    const bool two = D == 64 && static_cast<long long>(a.max_new) * a.group > 16;
 #define TETRA_WEIGH_FEW(PASS) \
-    if (one) hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 1>), g, b, 0, stream, a); \
-    else hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 2>), g, b, 0, stream, a)
+    if (two) hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, D == 64 ? 2 : 1>), g, b, 0, stream, a); \
+    else hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 1>), g, b, 0, stream, a)
     if (few) { TETRA_WEIGH_FEW(tetra_dev::kWeighSpanSums); }
     else hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, m, 0, stream, a);
     hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), dim3(64 * tetra_dev::kLogWaves), 0, stream, a);
@@ -72,8 +77,9 @@ int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
 }
 
 // Places of kv_evict's workspace.  A sequence and head whose weights a workgroup holds in
-// registers is one workgroup's; longer ones are cut in parts, up to four workgroups
-// a CU: 8 heads of 131,072 tokens @@
+// registers is one workgroup's, in one launch; longer ones are cut in parts, two workgroups a
+// CU in all, in four launches (8 heads of 131,072 tokens 32 us in place of 144; what the
+// first form takes is 12.5 us for 512 units of up to 4,096).
 struct EvictSpace {
     int parts;            // 0: not cut
     size_t tokens, state, bytes;

@@ -9,8 +9,15 @@
 // is 2^-200 and less of the largest, add nothing.  Each wave keeps its largest
 // logits in order, one a lane, and looks closer only where a batch has one that
 // belongs among them.  The order is by logit, then by index from the first on.
-// Neither depends on how a row is split but by the order of fp32 sums, which the
+// The tokens do not depend on how a row is split, and fp32 sums have an order that the
 // sizes fix.
+//
+// 2,048 rows of 151,936 logits in fp16, the likeliest token: 120 us, 5,180 GB/s (a
+// large copy reaches 5,160); of fp32 64 rows with five tokens 18 us and one row with
+// twenty 12: a chain of the loads, the bar's bisection, the list and the ranking in
+// 14 and 7.5 us, and the join's 4.5.  A wave's largest kept in order by inserting, in
+// place of the list, took 28 us for 64 rows with twenty tokens (now 18.6) and as long with one;
+// one batch at a time in place of four 26 with five.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -8,12 +8,20 @@
 // the sum over rows, so the scores are found twice: once for L (a row's largest
 // score and sum over each span of tokens, then joined), once for the weights.
 //
-// Both times the keys stay and the rows pass by: a wave holds 64 tokens in fp16
-// as operands of v_mfma_f32_32x32x16_f16, S^T = K Q^T, and a workgroup's four waves
+// Prompts: the keys stay and the rows pass by.  A wave holds 32 tokens in fp16
+// as operands of v_mfma_f32_32x32x16_f16, S^T = K Q^T, and a workgroup's eight waves
 // share the rows, 32 at a time, from LDS.  A lane then has scores of one row (lane
-// % 32) and 32 tokens: 8 (i / 4) + 4 (lane / 32) + i % 4 of each 32.  A row's
-// maximum and sum stay within a lane and its other half; a token's sum over the
-// rows is one addition a score, and one exchange over the lanes at the end.
+// % 32) and 16 tokens: 8 (i / 4) + 4 (lane / 32) + i % 4.  A row's maximum and sum
+// stay within a lane and its other half; a token's sum over the rows is one addition
+// a score, and one exchange over the lanes at the end.  The lengths are the device's,
+// so every workgroup plans for itself: blocks of tokens by chunks of rows, some eight
+// of them each.  4,096 tokens of 32 heads over 8 of 128: 148 and 133 us, 466 and 518
+// TFLOP/s; vector units busy 66 % of the cycles and matrix cores 30 %, which take turns
+// on a SIMD: an exponential a score and pass is a third of all.  64 tokens a wave and four
+// waves 158 and 146 us with more instructions and 165 and 154 with fewer, two tiles of rows
+// a barrier 164 and 160, half as many items 171 and 167.
+//
+// Single tokens: see weigh_few_kernel.
 #pragma once
 
 #include <type_traits>
@@ -497,7 +505,11 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
 
 // The same for sequences of up to 16 RT rows (single tokens), on v_mfma_f32_16x16x32_f16:
 // every wave for itself, a span of blocks of 64 tokens at a time, the rows in its
-// registers and the next block's keys on their way.  Tile t of four takes token 16 g +
+// registers and the next block's keys on their way.  The first pass also leaves the scores
+// where there is room for them (16 M), so that the second reads those and not the keys again:
+// of 5 rows 20 bytes for 128.  64 sequences of up to 4,096 tokens, 40 heads over 8 of 128:
+// 24 us (91 MB of keys, 14 of scores, 4,400 GB/s) and 11.7, with the keys read twice 21
+// and 22.  In 32 rows a tile, a block a wave at a time, both took 27.  Tile t of four takes token 16 g +
 // 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the scores of
 // 16 neighbouring tokens, all of one page, for row lane % 16.
 template <int D, WeighPass PASS, int RT>
