@@ -19,6 +19,8 @@ generator with the HIP path. It is deliberately plain and slow:
   (Eq. 2; Sec. 4.1 for the unquantised row tail; Sec. 5.1 for the product).
 * ``int4``   - the secondary int4 projection record and the 4-bit embedding
   row gather (Sec. 4.3, Sec. 4.4).
+* ``batch``  - attention weights of cached tokens, eviction by them, log
+  probabilities, all in 64 bits; not from the paper.
 
 Parity status of every function is stated in its module header.
 """

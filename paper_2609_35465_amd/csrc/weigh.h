@@ -509,9 +509,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
 // where there is room for them (16 M), so that the second reads those and not the keys again:
 // of 5 rows 20 bytes for 128.  64 sequences of up to 4,096 tokens, 40 heads over 8 of 128:
 // 24 us (91 MB of keys, 14 of scores, 4,400 GB/s) and 11.7, with the keys read twice 21
-// and 22.  In 32 rows a tile, a block a wave at a time, both took 27.  Tile t of four takes token 16 g +
-// 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the scores of
-// 16 neighbouring tokens, all of one page, for row lane % 16.
+// and 22.  In 32 rows a tile, a block a wave at a time, both took 27.  Tile t of four takes
+// token 16 g + 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the
+// scores of 16 neighbouring tokens, all of one page, for row lane % 16.
 template <int D, WeighPass PASS, int RT>
 __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
     constexpr std::integral_constant<WeighPass, kWeighSpanSums> pass;       // spans are the items both times
