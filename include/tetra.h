@@ -614,7 +614,8 @@ size_t tetra_kv_attend_shared_workspace_bytes(void);
  *   workspace: as for tetra_kv_attend, at least
  *             tetra_kv_weigh_workspace_bytes(cache, rows, q_heads)
  * Sums are fp32 of fp32 weights, in an order that the sizes fix: the result does not
- * change from run to run.  Asynchronous; errors as for tetra_kv_attend.
+ * change from run to run.  rows is less than 2^24.  Asynchronous; errors as for
+ * tetra_kv_attend.
  */
 int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
                    int max_new, int q_heads, float scale, int window, const float* mass, float* mass_out,
@@ -646,7 +647,9 @@ size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int
  *   workspace: as for tetra_kv_attend, at least
  *         tetra_kv_evict_workspace_bytes(from, to)
  * Tokens without a page go in as zeros, and kept tokens that `to` has no page
- * for are dropped.  Asynchronous; errors as for tetra_kv_append.
+ * for are dropped.  Asynchronous; errors as for tetra_kv_append, TETRA_EINVAL
+ * also where `to` has room for 2^29 tokens or more, over all sequences and
+ * cache heads (what a launch holds).
  */
 int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const float* mass, int mass_tokens, int recent,
                    float* mass_out, int out_tokens, void* workspace, size_t workspace_bytes, hipStream_t stream);
@@ -677,8 +680,8 @@ size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv
  *   workspace: as for tetra_kv_attend, at least
  *           tetra_log_probs_workspace_bytes(rows, vocab, top)
  * Sums are fp32; the result does not change from run to run.  vocab is at most
- * 2^22.  Asynchronous; TETRA_EINVAL / TETRA_EALIGN / TETRA_EDEVICE as for
- * tetra_sample.
+ * 2^22, rows less than 2^24.  Asynchronous; TETRA_EINVAL / TETRA_EALIGN /
+ * TETRA_EDEVICE as for tetra_sample.
  */
 int tetra_log_probs(const void* logits, int half, long long stride, int rows, int vocab, const float* temperature,
                     const int* tokens, int given, float* out, float* entropy, int top, int* top_tokens, float* top_out,

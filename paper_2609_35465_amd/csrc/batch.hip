@@ -96,7 +96,6 @@ struct EvictSpace {
 
 template <class T, bool TOP>
 int score_launch(const tetra_dev::ScoreArgs& a, hipStream_t stream) {
-    if (static_cast<long long>(a.rows) * a.parts > kMaxGrid) return TETRA_EINVAL;
     hipLaunchKernelGGL((tetra_dev::score_kernel<T, TOP>), dim3(static_cast<unsigned>(a.rows * a.parts)), dim3(256), 0, stream, a);
     if (a.parts > 1)
         hipLaunchKernelGGL((tetra_dev::score_join_kernel<T, TOP>), dim3(static_cast<unsigned>(a.rows)), dim3(256), 0, stream, a);
@@ -122,7 +121,8 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     if (!q || !starts || !mass_out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
     if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale) || mass_tokens < 1) return TETRA_EINVAL;
     if (!(decay >= 0.f && decay <= 1.f)) return TETRA_EINVAL;
-    if (q_stride < static_cast<long long>(q_heads) * cache->head_dim || rows > kMaxGrid / q_heads) return TETRA_EINVAL;
+    if (q_stride < static_cast<long long>(q_heads) * cache->head_dim || rows > kMaxGrid / q_heads || rows > kMaxGroups)
+        return TETRA_EINVAL;
     if (!aligned(q, 16) || q_stride % 8 || !aligned(starts, 4) || !aligned(mass, 4) || !aligned(mass_out, 4) ||
         !aligned(workspace, 256))
         return TETRA_EALIGN;
@@ -176,7 +176,9 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
     const EvictSpace space(from, to);
     if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     const long long units = static_cast<long long>(a.from.seqs) * a.from.kv_heads;
-    if (units > kMaxGrid / 16 / a.to.max_pages) return TETRA_EINVAL;
+    const long long moves = 2 * (to->page_tokens / tetra_dev::kGroupTokens);         // waves of a page and head
+    if (units > kMaxGrid / 16 / a.to.max_pages || (units * a.to.max_pages * moves + 3) / 4 > kMaxGroups) return TETRA_EINVAL;
+    if (units * std::max(space.parts, 1) > kMaxGroups * 256 / tetra_dev::kEvictThreads) return TETRA_EINVAL;
     a.mass = mass;
     a.out = mass_out;
     a.tokens = static_cast<int*>(workspace);
@@ -197,7 +199,7 @@ int tetra_kv_evict(const tetra_kv_cache* from, const tetra_kv_cache* to, const f
         hipLaunchKernelGGL(tetra_dev::evict_part_kernel<2>, p, t, 0, stream, a);
         hipLaunchKernelGGL(tetra_dev::evict_part_kernel<3>, p, t, 0, stream, a);
     }
-    const dim3 g(static_cast<unsigned>((units * a.to.max_pages * 2 * (to->page_tokens / tetra_dev::kGroupTokens) + 3) / 4)), m(256);
+    const dim3 g(static_cast<unsigned>((units * a.to.max_pages * moves + 3) / 4)), m(256);
     if (from->head_dim == 64) hipLaunchKernelGGL((tetra_dev::evict_move_kernel<64>), g, m, 0, stream, a);
     else hipLaunchKernelGGL((tetra_dev::evict_move_kernel<128>), g, m, 0, stream, a);
     return launch_status();
@@ -214,7 +216,7 @@ int tetra_log_probs(const void* logits, int half, long long stride, int rows, in
                     void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (!logits || !workspace || (half != 0 && half != 1) || rows < 1 || vocab < 1 || vocab > kMaxVocab || stride < vocab)
         return TETRA_EINVAL;
-    if (given < 0 || top < 0 || top > tetra_dev::kMostTop) return TETRA_EINVAL;
+    if (given < 0 || top < 0 || top > tetra_dev::kMostTop || rows > kMaxGroups) return TETRA_EINVAL;
     if ((given && (!tokens || !out)) || (top && (!top_tokens || !top_out))) return TETRA_EINVAL;
     if (!given && !top && !entropy) return TETRA_EINVAL;
     if (!aligned(logits, half ? 2 : 4) || !aligned(temperature, 4) || !aligned(tokens, 4) || !aligned(out, 4) ||

@@ -12,6 +12,7 @@
 namespace tetra_host {
 
 constexpr long long kMaxGrid = 0x7FFFFFFFll;
+constexpr long long kMaxGroups = 0xFFFFFFFFll / 256;     // of 256 threads: a launch holds less than 2^32
 constexpr int kMaxVocab = 1 << 22;     // so that a row's sum of weights, 2^62 at most, fits 64 bits
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

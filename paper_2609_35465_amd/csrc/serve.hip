@@ -172,8 +172,9 @@ int attend_args(const tetra_kv_cache* cache, const uint16_t* q, long long q_stri
 }
 
 // What a call with shared prefixes may be to go by its groups: rows of a sequence and cache
-// head, rows times q heads, and groups and sequences.
-constexpr int kSharedMost = 64, kSharedRows = 65536, kSharedList = 131072;
+// head, rows times q heads, groups and sequences, and these times cache heads (at most 8
+// workgroups of the join for each).
+constexpr int kSharedMost = 64, kSharedRows = 65536, kSharedList = 131072, kSharedHeads = 1 << 20;
 
 // bytes of kv_attend_shared's workspace, behind those of kv_attend
 struct SharedSpace {
@@ -200,6 +201,7 @@ constexpr long long kSharedBytes = 160ll << 20;
 bool shared_pays(const tetra_dev::AttendArgs& a, int dim) {
     const long long most = static_cast<long long>(a.max_new) * a.group;
     if (most > kSharedMost || a.rows > kSharedRows / a.q_heads || a.num_seqs > kSharedList) return false;
+    if (a.num_seqs > kSharedHeads / a.c.kv_heads) return false;
     const double tokens = static_cast<double>(static_cast<long long>(a.c.max_pages) << a.c.page_shift) * a.c.seqs;
     const long long tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
     return tokens * a.c.kv_heads * 2 * dim * tiles >= kSharedBytes;

@@ -126,6 +126,16 @@ def test_score_validation():
     assert size(0, 5, 0) == size(5, 0, 0) == size(1, (1 << 22) + 1, 0) == size(1, 5, 65) == size(1, 5, -1) == 0
 
 
+def test_launches_past_the_thread_limit_are_refused():
+    """A launch holds less than 2^32 threads: calls that need one more are refused before their first launch."""
+    wide = _cache(kv_heads=8, page_tokens=128, max_pages=1 << 23, seqs=1)
+    for pages in (1 << 19, 1 << 20, 1 << 23):             # 2^24 workgroups of 256 threads from the first on
+        to = _cache(kv_heads=8, page_tokens=128, max_pages=pages, seqs=1, k=FAKE + 4096)
+        assert _evict(wide, to, ws_bytes=1 << 62) == tt.EINVAL, pages
+    assert _weigh(rows=1 << 24, max_new=1) == tt.EINVAL
+    assert _score(rows=1 << 24) == tt.EINVAL
+
+
 def _refused(call, *args, **kw):
     with pytest.raises(tt.TetraError) as e:
         call(*args, **kw)
