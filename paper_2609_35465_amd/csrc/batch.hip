@@ -33,7 +33,7 @@ constexpr int kWeighGroupsPerCU = 2, kWeighFewGroupsPerCU = 4;
 
 // Sequences whose rows a wave holds in registers beside its keys: 16 of a cache head of 128, 32
 // of one of 64.  Then the keys are what is read: 64 sequences of up to 4,096 tokens, 5 rows
-// 39 us by weigh_few_kernel and 73 by weigh_kernel, whose rows go through LDS with a barrier; 16
+// 37 us by weigh_few_kernel and 73 by weigh_kernel, whose rows go through LDS with a barrier; 16
 // rows 22-41 and 30-73 by batch; heads of 64, 32 rows 14-43 and 16-62.  With heads of
 // 128, 20 rows took 28 and 22 (8 sequences) to 62 and 73 (64), 32 rows 37 and 30 (16).
 bool weigh_few(int max_new, int group, int head_dim) { return static_cast<long long>(max_new) * group * head_dim <= 2048; }
@@ -65,7 +65,8 @@ int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
     else hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, 1>), g, b, 0, stream, a)
     if (few) { TETRA_WEIGH_FEW(tetra_dev::kWeighSpanSums); }
     else hipLaunchKernelGGL((tetra_dev::weigh_kernel<D, tetra_dev::kWeighSpanSums>), g, m, 0, stream, a);
-    hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), dim3(64 * tetra_dev::kLogWaves), 0, stream, a);
+    if (!few || two)                  // one tile of rows is joined by the second pass
+        hipLaunchKernelGGL(tetra_dev::weigh_logs_kernel, dim3(static_cast<unsigned>(a.rows)), dim3(64 * tetra_dev::kLogWaves), 0, stream, a);
     if (few) {
         TETRA_WEIGH_FEW(tetra_dev::kWeighTokens);
     } else {

@@ -17,7 +17,7 @@
 // so every workgroup plans for itself: blocks of tokens by chunks of rows, some eight
 // of them each.  4,096 tokens of 32 heads over 8 of 128: 148 and 133 us, 466 and 518
 // TFLOP/s; vector units busy 66 % of the cycles and matrix cores 30 %, which take turns
-// on a SIMD: an exponential a score and pass is a third of all.  64 tokens a wave and four
+// on a SIMD: an exponential a score and pass is 45 % of the former.  64 tokens a wave and four
 // waves 158 and 146 us with more instructions and 165 and 154 with fewer, two tiles of rows
 // a barrier 164 and 160, half as many items 171 and 167.
 //
@@ -503,12 +503,43 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
     }
 }
 
+// L of row `lane` of a sequence's `rows` (64 at most) of a cache head, from its spans' largest
+// scores and sums: 64 / R lanes a row, R the next power of two.  Every wave that asks
+// joins them in the same order.  With up to 16 rows this costs less than the launch of
+// weigh_logs_kernel: 4 rows over 203 tokens 11.0 and 12.5 us, 64 sequences of 5 rows over up to
+// 4,096 37 and 40, 5 rows over 131,072 (256 spans) 49 and 54.  With 32 over 65,536 it took 51
+// and the launch 44.
+__device__ __forceinline__ float weigh_log(const WeighArgs& a, const WeighItem& w, int rows, int spans) {
+    const int lane = threadIdx.x & 63;
+    int R = 1;
+    while (R < rows) R *= 2;
+    const int i = lane & (R - 1), token = i / a.group;
+    const size_t step = static_cast<size_t>(a.rows) * a.q_heads;
+    const f32x2* p = reinterpret_cast<const f32x2*>(a.spans) + static_cast<size_t>(w.q.s.row0 + token) * a.q_heads + w.head * a.group + i -
+                     token * a.group;
+    float m = kWeighNone, l = 0.f;
+    if (i < rows)
+#pragma unroll 4
+        for (int k = lane / R; k < spans; k += 64 / R) {
+            const f32x2 x = p[k * step];
+            const float n = fmaxf(m, x[0]);
+            l = l * fast_exp2(m - n) + x[1] * fast_exp2(x[0] - n);
+            m = n;
+        }
+    for (int k = R; k < 64; k *= 2) {
+        const float m1 = __shfl_xor(m, k, 64), l1 = __shfl_xor(l, k, 64), n = fmaxf(m, m1);
+        l = l * fast_exp2(m - n) + l1 * fast_exp2(m1 - n);
+        m = n;
+    }
+    return lane >= rows || l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+}
+
 // The same for sequences of up to 16 RT rows (single tokens), on v_mfma_f32_16x16x32_f16:
 // every wave for itself, a span of blocks of 64 tokens at a time, the rows in its
 // registers and the next block's keys on their way.  The first pass also leaves the scores
 // where there is room for them (16 M), so that the second reads those and not the keys again:
 // of 5 rows 20 bytes for 128.  64 sequences of up to 4,096 tokens, 40 heads over 8 of 128:
-// 24 us (91 MB of keys, 14 of scores, 4,400 GB/s) and 11.7, with the keys read twice 21
+// 24 us (91 MB of keys, 14 of scores, 4,400 GB/s) and 13, with the keys read twice 21
 // and 22.  In 32 rows a tile, a block a wave at a time, both took 27.  Tile t of four takes
 // token 16 g + 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the
 // scores of 16 neighbouring tokens, all of one page, for row lane % 16.
@@ -516,6 +547,7 @@ template <int D, WeighPass PASS, int RT>
 __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
     constexpr std::integral_constant<WeighPass, kWeighSpanSums> pass;       // spans are the items both times
     constexpr int C = D / 64;
+    constexpr bool kJoins = RT == 1;              // the rows' spans itself
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x + gridDim.x * (threadIdx.x >> 6));
     const size_t stride = static_cast<size_t>(a.c.page_tokens) * D;
@@ -536,7 +568,8 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
             constexpr int kAhead = 8;
             const int rows = s.n * a.group, token = lane / a.group;
             float logs = INFINITY, z[kAhead];
-            if (lane < rows) logs = a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + w.head * a.group + lane - token * a.group];
+            if (kJoins && rows > 0) logs = weigh_log(a, w, rows, WeighPlan::spans_of(a, w.q, plan.span));
+            if (!kJoins && lane < rows) logs = a.logs[static_cast<size_t>(s.row0 + token) * a.q_heads + w.head * a.group + lane - token * a.group];
             auto load = [&](int block, int i0) {
                 const float* p = scores_of(block) + lane;
 #pragma unroll
@@ -583,7 +616,8 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
         bool is[RT];
         size_t row[RT];
         int see_all[RT], see_begin[RT];
-        float m[RT], l[RT], log[RT];
+        float m[RT], l[RT], log[RT], logs = INFINITY;
+        if (PASS == kWeighTokens && kJoins && s.n > 0) logs = weigh_log(a, w, s.n * a.group, WeighPlan::spans_of(a, w.q, plan.span));
 #pragma unroll
         for (int n = 0; n < RT; ++n) {
             const int i = 16 * n + r, token = i / a.group, h = w.head * a.group + i - token * a.group;
@@ -602,7 +636,10 @@ __global__ __launch_bounds__(256, 4) void weigh_few_kernel(WeighArgs a) {
             m[n] = kWeighNone;
             l[n] = 0.f;
             log[n] = INFINITY;
-            if (PASS == kWeighTokens && is[n]) log[n] = a.logs[row[n]];
+            if (PASS == kWeighTokens) {
+                if (kJoins) log[n] = __shfl(logs, 16 * n + r, 64);
+                else if (is[n]) log[n] = a.logs[row[n]];
+            }
         }
         for (int block = w.block; block < blocks_end; ++block) {
             const int t0 = block * 64, mine = t0 + 16 * g;
