@@ -422,6 +422,8 @@ def kv_append(cache: KVCache, q, k, v, starts, max_new: int, rope, q_out, q_norm
         size = q_out.numel()
         q_heads = size // (rows * dim) if rows else 0
         ok = ok and q.dtype is kind and size == q_heads * rows * dim and q_out.dtype is f16 and q_out.is_contiguous()
+    if shifts is not None:
+        ok = ok and _here(shifts, q, k, v, starts, rope, q_out, q_norm, k_norm, *cache.tensors)
     _expect(ok, what)
     if q is not None:
         q_stride = _row_stride(q, rows, q_heads, dim, what)

@@ -210,3 +210,24 @@ def test_oracle_of_the_choice_keeps_order_and_the_last():
     assert ref.choose(m, 5, 9, 1).tolist() == [0, 1, 2, 3, 4]
     q, s = ref.moved(np.array([[10, -7], [100, 3]], np.int8), np.array([1.0, 4.0], np.float32))
     assert s == 4 and q.tolist() == [[2, -2], [100, 3]]
+
+
+def test_shifts_on_the_host_do_not_reach_the_library(monkeypatch):
+    """What kv_append takes with shifts lies on the current GPU, all of it: an address of host memory never gets to a
+    kernel."""
+    cache, i32 = _tensors(), torch.int32
+    calls, call = [], tt._call
+    monkeypatch.setattr(tt, "_call", lambda name, *a: calls.append(name) or tt.OK if name.startswith("tetra_kv") else call(name, *a))
+    k, q, starts, shifts = torch.zeros((3, 2, 64)), torch.zeros((3, 4, 64)), torch.zeros(4, dtype=i32), torch.zeros(3, dtype=i32)
+    _refused(tt.kv_append, cache, None, k, k, starts, 1, None, None, shifts=shifts, stream=0)
+    _refused(tt.kv_append, cache, q, k, k, starts, 1, torch.zeros((9, 64)), q.half(), torch.zeros(64), torch.zeros(64),
+             shifts=shifts, stream=0)
+    assert calls == []
+
+    # each of them by itself: the others as if on the current GPU
+    seen = []
+    monkeypatch.setattr(tt, "_here", lambda *t: bool(seen.append(t)))
+    rope, out, norms = torch.zeros((9, 64)), q.half(), [torch.zeros(64), torch.zeros(64)]
+    _refused(tt.kv_append, cache, q, k, k, starts, 1, rope, out, *norms, shifts=shifts, stream=0)
+    for t in (q, k, starts, rope, out, *norms, shifts, *cache.tensors):
+        assert any(t is x for x in seen[0])
