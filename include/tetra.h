@@ -585,7 +585,9 @@ int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_input* in, co
  *   workspace: as for tetra_kv_attend, at least
  *        tetra_kv_attend_shared_workspace_bytes()
  * The result does not change from run to run.  Asynchronous; errors as for
- * tetra_kv_attend, TETRA_EINVAL also for num_groups < 1 or > seqs.
+ * tetra_kv_attend, TETRA_EINVAL also for num_groups < 1 or > seqs, and where the
+ * tables of groups and sequences have room for 2^31 tiles of 256 tokens or more,
+ * over all cache heads and 16 rows of each.
  */
 int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
                            int max_new, int q_heads, float scale, const int* groups, const int* shared, int num_groups,

@@ -142,7 +142,7 @@ int attend_launch(tetra_dev::AttendArgs& a, int cus, hipStream_t stream) {
 // the arguments of tetra_kv_attend, checked
 int attend_args(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
                 int max_new, int q_heads, float scale, int window, uint16_t* out, long long out_stride,
-                void* workspace, size_t workspace_bytes, tetra_dev::AttendArgs& a, int& cus) {
+                void* workspace, size_t workspace_bytes, tetra_dev::AttendArgs& a) {
     if (int st = cache_of(cache, &a.c)) return st;
     if (!q || !starts || !out || !workspace || rows < 1 || max_new < 1 || max_new > rows || window < 0) return TETRA_EINVAL;
     if (q_heads < 1 || q_heads % a.c.kv_heads || !std::isfinite(scale)) return TETRA_EINVAL;
@@ -152,13 +152,10 @@ int attend_args(const tetra_kv_cache* cache, const uint16_t* q, long long q_stri
         !aligned(workspace, 256))
         return TETRA_EALIGN;
     if (workspace_bytes < kMinAttendWorkspace) return TETRA_EINVAL;
-    if (int st = device_cus(&cus)) return st;
-    if (workspace_bytes < attend_workspace(cus)) return TETRA_EINVAL;
     a.q = q;
     a.starts = starts;
     a.out = out;
     a.partials = static_cast<float*>(workspace);
-    a.pieces = a.partials + few_parts(cus);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.scale = std::fabs(scale) * 1.44269504f;
@@ -168,6 +165,14 @@ int attend_args(const tetra_kv_cache* cache, const uint16_t* q, long long q_stri
     a.q_heads = q_heads;
     a.group = q_heads / a.c.kv_heads;
     a.window = window;
+    return TETRA_OK;
+}
+
+// the device's part of them
+int attend_device(tetra_dev::AttendArgs& a, size_t workspace_bytes, int& cus) {
+    if (int st = device_cus(&cus)) return st;
+    if (workspace_bytes < attend_workspace(cus)) return TETRA_EINVAL;
+    a.pieces = a.partials + few_parts(cus);
     return TETRA_OK;
 }
 
@@ -198,10 +203,10 @@ struct SharedSpace {
 // group 64 and 179.
 constexpr long long kSharedBytes = 160ll << 20;
 
-bool shared_pays(const tetra_dev::AttendArgs& a, int dim) {
-    const long long most = static_cast<long long>(a.max_new) * a.group;
-    if (most > kSharedMost || a.rows > kSharedRows / a.q_heads || a.num_seqs > kSharedList) return false;
-    if (a.num_seqs > kSharedHeads / a.c.kv_heads) return false;
+bool shared_pays(const tetra_dev::AttendArgs& a, int num_groups, int dim) {
+    const long long most = static_cast<long long>(a.max_new) * a.group, seqs = static_cast<long long>(num_groups) + a.c.seqs;
+    if (most > kSharedMost || a.rows > kSharedRows / a.q_heads || seqs > kSharedList) return false;
+    if (seqs > kSharedHeads / a.c.kv_heads) return false;
     const double tokens = static_cast<double>(static_cast<long long>(a.c.max_pages) << a.c.page_shift) * a.c.seqs;
     const long long tiles = (most + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows;
     return tokens * a.c.kv_heads * 2 * dim * tiles >= kSharedBytes;
@@ -214,12 +219,24 @@ bool shared_pays(const tetra_dev::AttendArgs& a, int dim) {
 // 32,768 tokens in common 74 us, two workgroups a CU 83, one 77.
 constexpr int kSharedFew = 32;
 
+int shared_few(const tetra_dev::AttendArgs& a) { return std::max(a.max_new * a.group, kSharedFew); }
+constexpr int kSharedTile = 256;
+
+// Tiles of attend_few where groups and sequences all fill the table: the device counts them in an int.
+double shared_tiles(const tetra_dev::AttendArgs& a, int num_groups) {
+    auto row_tiles = [](int rows) { return (rows + tetra_dev::kFewRows - 1) / tetra_dev::kFewRows; };
+    const double units = static_cast<double>(num_groups) * row_tiles(shared_few(a)) +
+                         static_cast<double>(a.c.seqs) * row_tiles(a.max_new * a.group);
+    const long long kept = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
+    return units * a.c.kv_heads * static_cast<double>((kept + kSharedTile - 1) / kSharedTile);
+}
+
 template <int D>
 int shared_launch(tetra_dev::SharedArgs& x, int cus, hipStream_t stream) {
     tetra_dev::AttendArgs& a = x.a;
     const int slots = cus + cus / 2, few = kFewGroupsPerCU * cus;
-    a.few_most = std::max(a.max_new * a.group, kSharedFew);
-    a.few_tile = 256;
+    a.few_most = shared_few(a);
+    a.few_tile = kSharedTile;
     const long long all = static_cast<long long>(a.rows) * a.group;
     const long long units = (all / 128 + std::min<long long>(x.num_groups, all / (a.few_most + 1))) * a.c.kv_heads;   // at most
     const long long blocks = units ? std::max<long long>(units, slots) : 0;
@@ -344,8 +361,9 @@ int tetra_kv_attend(const tetra_kv_cache* cache, const uint16_t* q, long long q_
     tetra_dev::AttendArgs a;
     int cus = 0;
     if (int st = attend_args(cache, q, q_stride, starts, rows, max_new, q_heads, scale, window, out, out_stride, workspace,
-                             workspace_bytes, a, cus))
+                             workspace_bytes, a))
         return st;
+    if (int st = attend_device(a, workspace_bytes, cus)) return st;
     return cache->head_dim == 64 ? attend_launch<64>(a, cus, stream) : attend_launch<128>(a, cus, stream);
 }
 
@@ -364,8 +382,11 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long 
     if (cache && (!groups || !shared || num_groups < 1 || num_groups > cache->seqs)) return TETRA_EINVAL;
     if (!aligned(groups, 4) || !aligned(shared, 4)) return TETRA_EALIGN;
     if (int st = attend_args(cache, q, q_stride, starts, rows, max_new, q_heads, scale, 0, out, out_stride, workspace,
-                             workspace_bytes, x.a, cus))
+                             workspace_bytes, x.a))
         return st;
+    const bool pays = shared_pays(x.a, num_groups, cache->head_dim);
+    if (pays && shared_tiles(x.a, num_groups) > kMaxGrid) return TETRA_EINVAL;
+    if (int st = attend_device(x.a, workspace_bytes, cus)) return st;
     const SharedSpace space(cus);
     if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     x.groups = groups;
@@ -375,11 +396,11 @@ int tetra_kv_attend_shared(const tetra_kv_cache* cache, const uint16_t* q, long 
     x.list = reinterpret_cast<tetra_dev::SharedSeq*>(at + space.list);
     x.group = reinterpret_cast<tetra_dev::SharedGroup*>(at + space.group);
     x.a.seqs = x.list;
-    x.a.num_seqs = num_groups + cache->seqs;
     x.a.results = reinterpret_cast<float*>(at + space.results);
     x.a.stats = reinterpret_cast<float*>(at + space.stats);
-    if (!shared_pays(x.a, cache->head_dim))
+    if (!pays)
         return cache->head_dim == 64 ? attend_launch<64>(x.a, cus, stream) : attend_launch<128>(x.a, cus, stream);
+    x.a.num_seqs = num_groups + cache->seqs;
     return cache->head_dim == 64 ? shared_launch<64>(x, cus, stream) : shared_launch<128>(x, cus, stream);
 }
 

@@ -231,3 +231,18 @@ def test_shifts_on_the_host_do_not_reach_the_library(monkeypatch):
     _refused(tt.kv_append, cache, q, k, k, starts, 1, rope, out, *norms, shifts=shifts, stream=0)
     for t in (q, k, starts, rope, out, *norms, shifts, *cache.tensors):
         assert any(t is x for x in seen[0])
+
+
+def test_shared_tables_of_more_tiles_than_an_int_counts():
+    """Room for 2^31 tiles and more, over groups, sequences, cache heads and row tiles, is refused as kv_attend refuses it:
+    the kernels count them in an int.  The workspace is too small for a launch in any case."""
+    def call(pages, seqs=1024, n=1024, heads=64, new=1):
+        wide = _cache(kv_heads=heads, page_tokens=128, max_pages=pages, seqs=seqs)
+        return _shared(wide, q_stride=heads * 64, rows=1024, max_new=new, heads=heads, n=n, out_stride=heads * 64, ws_bytes=4096)
+
+    # row tiles of 1,024 groups of up to 32 rows (two) and of as many sequences, by 64 heads, of pages / 2 tiles each
+    for new, row_tiles in ((1, 3), (20, 4)):
+        least = 2 * -(-(1 << 31) // (row_tiles * 1024 * 64))
+        assert call(least, new=new) == call(1 << 23, new=new) == tt.EINVAL
+        if not torch.cuda.is_available():
+            assert call(least - 2, new=new) == tt.EDEVICE                    # on to the device, which is none
