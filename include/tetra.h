@@ -623,8 +623,16 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
                    int max_new, int q_heads, float scale, int window, const float* mass, float* mass_out,
                    int mass_tokens, float decay, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of tetra_kv_weigh (host only; only the cache's sizes are
- * looked at; 0 if they are out of range or the device cannot be queried). */
+/*
+ * Workspace bytes of tetra_kv_weigh for caches of these sizes and up to `rows`
+ * rows (host only; only the cache's sizes are looked at; 0 if they are out of
+ * range or the device cannot be queried).  They hold, for each row and q head,
+ * 8 bytes a span of tokens: as many spans as the table has 256 tokens, 64 at most,
+ * or for single tokens (rows of a sequence and cache head times head_dim at most
+ * 2,048) as it has 64, 256 at most.  Beside that single tokens' scores, 4 bytes
+ * for each of the table's tokens and such rows, 64 MiB at most, or prompts' sums,
+ * 32 KiB a CU at most.
+ */
 size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int q_heads);
 
 /*

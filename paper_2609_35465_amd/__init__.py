@@ -558,7 +558,7 @@ def kv_attend_shared(cache: KVCache, q, starts, max_new: int, groups, shared, ou
 
 
 def kv_weigh_workspace(cache: KVCache, rows: int, q_heads: int):
-    """A workspace for kv_weigh of up to `rows` rows (a torch uint8 tensor)."""
+    """A workspace for kv_weigh of up to `rows` rows over caches of this one's sizes (a torch uint8 tensor)."""
     return _space("tetra_kv_weigh_workspace_bytes", ctypes.addressof(cache), rows, q_heads)
 
 

@@ -36,29 +36,49 @@ constexpr int kWeighGroupsPerCU = 2, kWeighFewGroupsPerCU = 4;
 // 37 us by weigh_few_kernel and 73 by weigh_kernel, whose rows go through LDS with a barrier; 16
 // rows 22-41 and 30-73 by batch; heads of 64, 32 rows 14-43 and 16-62.  With heads of
 // 128, 20 rows took 28 and 22 (8 sequences) to 62 and 73 (64), 32 rows 37 and 30 (16).
-bool weigh_few(int max_new, int group, int head_dim) { return static_cast<long long>(max_new) * group * head_dim <= 2048; }
+constexpr long long kWeighFew = 2048;
+bool weigh_few(int max_new, int group, int head_dim) { return static_cast<long long>(max_new) * group * head_dim <= kWeighFew; }
 
-// floats of kv_weigh's workspace
+// Places of kv_weigh's workspace, in floats, for up to `rows` rows: what full tables ask for.  A sequence that goes by
+// weigh_few_kernel has few_rows rows at most; a batch of more rows than those, as where there are rows past the last
+// start, has longer spans.  Lengths past the table make spans and chunks longer too, so nothing depends on the lengths.
 struct WeighSpace {
-    int workers;
-    size_t spans, logs, bytes;
-    WeighSpace(int rows, int q_heads, int cus) {
-        workers = cus * kWeighGroupsPerCU;
+    int few_spans, many_spans;      // of a sequence at most, in weigh_few_kernel and in weigh_kernel
+    int items;                      // of weigh_kernel, whose parts there is room for
+    size_t spans, logs, scores, bytes;
+    WeighSpace(const tetra_kv_cache& c, int rows, int q_heads, int cus) {
+        using namespace tetra_dev;
+        const long long tokens = static_cast<long long>(c.max_pages) * c.page_tokens, group = q_heads / c.kv_heads;
+        const long long few_blocks = (tokens + 63) / 64, blocks = (tokens + kWeighBlock - 1) / kWeighBlock;
+        few_spans = static_cast<int>(std::min<long long>(kWeighSpans, few_blocks));
+        many_spans = static_cast<int>(std::min<long long>(kWeighSpans / 4, blocks));
+        const long long few_rows = std::min<long long>(rows, kWeighFew / (group * c.head_dim));
+        const long long few = std::min<long long>(rows, few_rows * c.seqs);
         logs = (static_cast<size_t>(rows) * q_heads + 63) / 64 * 64;
-        spans = logs * tetra_dev::kWeighSpans * 2;
-        // single tokens' scores, or prompts' parts
-        const size_t parts = 2 * static_cast<size_t>(tetra_dev::kWeighItems) * workers * tetra_dev::kWeighBlock;
-        bytes = rounded(256 + sizeof(float) * (spans + logs + std::max<size_t>(parts, tetra_dev::kWeighScores)));
+        spans = std::max(2 * logs * many_spans, (2 * static_cast<size_t>(few) * q_heads * few_spans + 63) / 64 * 64);
+        // and single tokens' scores, or prompts' parts: blocks of each sequence by row tiles of all
+        const long long units = static_cast<long long>(c.seqs) * c.kv_heads, block_scores = 64 * few_rows * group;
+        scores = 0;
+        if (few_rows) scores = few_blocks > kWeighScores / block_scores / units ? kWeighScores : few_blocks * units * block_scores;
+        const long long tiles = rows * group / kWeighRows + std::min(rows, c.seqs);
+        const double steps = static_cast<double>(blocks) * c.kv_heads * static_cast<double>(tiles);
+        items = static_cast<int>(std::min<double>(kWeighItems * kWeighGroupsPerCU * cus, steps));
+        bytes = rounded(256 + sizeof(float) * (spans + logs + std::max(scores, 2 * static_cast<size_t>(items) * kWeighBlock)));
+    }
+    int spans_most(bool few, int rows, int q_heads) const {
+        return static_cast<int>(std::min<size_t>(few ? few_spans : many_spans, spans / (2 * static_cast<size_t>(rows) * q_heads)));
     }
 };
 
 template <int D>
-int weigh_launch(tetra_dev::WeighArgs& a, int cus, hipStream_t stream) {
+int weigh_launch(tetra_dev::WeighArgs& a, const WeighSpace& space, int cus, hipStream_t stream) {
     const bool few = weigh_few(a.max_new, a.group, D);
     const dim3 b(256), m(64 * tetra_dev::kWeighWaves), g(static_cast<unsigned>(cus * (few ? kWeighFewGroupsPerCU : kWeighGroupsPerCU)));
     a.workers = static_cast<int>(few ? 4 * g.x : g.x);
     a.block = few ? 64 : tetra_dev::kWeighBlock;
-    a.spans_most = few ? tetra_dev::kWeighSpans : tetra_dev::kWeighSpans / 4;
+    a.spans_most = space.spans_most(few, a.rows, a.q_heads);
+    a.items_most = space.items;
+    a.scores_most = static_cast<long long>(space.scores);
     const bool two = D == 64 && static_cast<long long>(a.max_new) * a.group > 16;
 #define TETRA_WEIGH_FEW(PASS) \
     if (two) hipLaunchKernelGGL((tetra_dev::weigh_few_kernel<D, PASS, D == 64 ? 2 : 1>), g, b, 0, stream, a); \
@@ -111,7 +131,7 @@ size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int
     int cus = 0;
     if (!sizes_ok(cache) || rows < 1 || q_heads < 1 || q_heads % cache->kv_heads || rows > kMaxGrid / q_heads || device_cus(&cus))
         return 0;
-    return WeighSpace(rows, q_heads, cus).bytes;
+    return WeighSpace(*cache, rows, q_heads, cus).bytes;
 }
 
 int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_stride, const int* starts, int rows,
@@ -133,7 +153,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     int cus = 0;
     if (workspace_bytes < kMinWorkspace) return TETRA_EINVAL;
     if (int st = device_cus(&cus)) return st;
-    const WeighSpace space(rows, q_heads, cus);
+    const WeighSpace space(*cache, rows, q_heads, cus);
     if (workspace_bytes < space.bytes) return TETRA_EINVAL;
     a.q = q;
     a.starts = starts;
@@ -154,7 +174,7 @@ int tetra_kv_weigh(const tetra_kv_cache* cache, const uint16_t* q, long long q_s
     a.window = window;
     a.mass_tokens = mass_tokens;
     a.score_rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_new) * a.group, tetra_dev::kWeighRows));
-    return cache->head_dim == 64 ? weigh_launch<64>(a, cus, stream) : weigh_launch<128>(a, cus, stream);
+    return cache->head_dim == 64 ? weigh_launch<64>(a, space, cus, stream) : weigh_launch<128>(a, space, cus, stream);
 }
 
 size_t tetra_kv_evict_workspace_bytes(const tetra_kv_cache* from, const tetra_kv_cache* to) {

@@ -38,7 +38,7 @@ constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sum
 constexpr int kWeighMostTiles = 16;       // row tiles whose sums a workgroup holds in LDS
 constexpr int kWeighItems = 8;            // of a workgroup, where there are enough
 constexpr float kWeighNone = -3e38f;      // a maximum over no score
-constexpr long long kWeighScores = 16 << 20;   // scores that single tokens' first pass may leave for the second
+constexpr long long kWeighScores = 16 << 20;   // scores that single tokens' first pass leaves for the second, at most
 
 struct WeighArgs {
     KvCache c;
@@ -46,9 +46,9 @@ struct WeighArgs {
     const int* starts;
     const float* mass;
     float* out;
-    float* spans;         // [kWeighSpans][rows][q_heads][2]: largest score and sum of a row over a span
+    float* spans;         // [spans_most][rows][q_heads][2]: largest score and sum of a row over a span
     float* logs;          // [rows][q_heads]: L, +inf where a row sees nothing
-    float* parts;         // [2 kWeighItems workers][kWeighBlock]: a block's sums over some of its rows
+    float* parts;         // [2 items_most][kWeighBlock]: a block's sums over some of its rows
     long long q_stride;
     float scale;          // |scale| log2(e)
     uint32_t q_flip;      // 0x80008000 if the scale is negative: turns q instead
@@ -57,7 +57,9 @@ struct WeighArgs {
     int workers;          // workgroups, or waves, that share the items of a launch
     int block, spans_most;   // tokens of a block; spans of a sequence at most
     int* span;               // the blocks of a span, at least, for the kernel of the logs
+    int items_most;          // chunks of rows are so long that no more items than this have one
     float* scores;           // [blocks of all sequences and heads][rows of a sequence][64], of weigh_few_kernel
+    long long scores_most;   // that there is room for
     int score_rows;          // rows of a sequence and cache head at most
 };
 
@@ -95,8 +97,9 @@ struct WeighItem {
 
 enum WeighPass { kWeighSpanSums, kWeighTokens, kWeighJoin };
 
-// Row tiles of a chunk, so that there are some kWeighItems items a workgroup: then no
-// more than twice that many have a part of a block's sums to leave.
+// Row tiles of a chunk, so that there are some items_most items (kWeighItems a workgroup,
+// where a full table has as many): then no more than twice that many have a part of a
+// block's sums to leave.
 struct WeighPlan {
     int chunk, total;             // row tiles of a chunk; items
     int span;                     // blocks of a span, at least
@@ -144,9 +147,9 @@ struct WeighPlan {
             const long long room = max(static_cast<long long>(a.workers) - ends, static_cast<long long>(a.workers / 2));
             blocks = wave_all(Sum(), blocks) * a.c.kv_heads;
             span = static_cast<int>(max(1ll, min((static_cast<long long>(blocks) + room - 1) / room, 1ll << 24)));
-            keep = static_cast<long long>(blocks) <= kWeighScores / 64 / a.score_rows;
+            keep = static_cast<long long>(blocks) * 64 * a.score_rows <= a.scores_most;
         }
-        const unsigned long long most = static_cast<unsigned long long>(kWeighItems) * a.workers;
+        const unsigned long long most = a.items_most;
         chunk = static_cast<int>(max(1ull, min((steps + most - 1) / most, 1ull << 26)));
         if (PASS == kWeighSpanSums) chunk = min(chunk, kWeighMostTiles);
         lane_items = items_of<PASS>(a, mine);

@@ -1,5 +1,5 @@
 """Weights of cached tokens over the plans that the device makes for them: items of several row tiles, spans of several
-blocks, scores that find no room, more items than waves (run on an MI355X).
+blocks, scores that find no room, more items than waves; and the workspace (run on an MI355X).
 
 Which of these a call meets goes by its sizes, so every case asks a copy of the plan on the host whether it meets what it
 is for.  The pages of a small pool are shared by all tables, in any order and more than once.
@@ -204,3 +204,48 @@ def test_prompts_of_more_sequences_than_lanes(group):
     lens = [n + int(rng.integers(0, 600)) for n in news]
     plan = _check(lens, news, 2, group, 128, page=16, slack=9)
     assert not plan.few
+
+
+# ------------------------------------------------------------------ the workspace
+
+def _sizes(seqs, kv_heads, dim, tokens, page=64):
+    c = tt.KVCache()
+    c.num_pages, c.page_tokens, c.kv_heads, c.head_dim, c.seqs, c.max_pages = 10, page, kv_heads, dim, seqs, _up(tokens, page)
+    return c
+
+
+def test_workspace_is_what_a_call_can_use():
+    """Not the most that any call could: a prompt's 64 spans of the table's blocks, a short sequence's scores."""
+    import ctypes
+
+    def size(rows, q_heads, *sizes):
+        cache = _sizes(*sizes)
+        return tt.library().tetra_kv_weigh_workspace_bytes(ctypes.addressof(cache), rows, q_heads)
+
+    assert 0 < size(1, 32, 1, 8, 128, 203) <= 1 << 17
+    # 64 MiB of scores (the rows may be three a sequence: 8 * 64 * 64 blocks * 64 * 15 are more), and the spans of 64 rows
+    assert size(64, 40, 64, 8, 128, 4096) <= (64 << 20) + 64 * 40 * (64 * 8 + 4) + 512
+    assert size(64, 40, 64, 8, 128, 131072) <= (64 << 20) + 64 * 40 * (256 * 8 + 4) + 512
+    assert size(16, 40, 16, 8, 128, 2048) <= 16 * 8 * 32 * 64 * 15 * 4 + 16 * 40 * (32 * 8 + 4) + 512
+    assert size(4096, 32, 1, 8, 128, 4096) <= 32 << 20
+    # scores of three rows of five heads over the table: 15.7 MB
+    assert size(32768, 40, 1, 8, 128, 32768) <= 32768 * 40 * (64 * 8 + 4) + 8 * 32768 * 15 * 4 + 512
+    # one for many rows serves fewer
+    for cache in ((1, 8, 128, 203), (3, 2, 64, 100000), (64, 8, 128, 4096)):
+        for q_heads in (8, 40, 320):
+            sizes = [size(n, q_heads, *cache) for n in (1, 2, 3, 4, 5, 15, 16, 17, 31, 32, 33, 64, 200, 1000, 5000)]
+            assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("dim,group", [(128, 5), (64, 20)])
+def test_rows_far_past_the_last_start(dim, group):
+    """As in a graph captured for a larger batch: the spans of the rows that count are longer then."""
+    plan = _check([40000, 33], [1, 1], 2, group, dim, extra_rows=700)
+    assert plan.few
+
+
+@pytest.mark.parametrize("news", [(1, 1), (60, 300)])
+def test_lengths_and_places_far_past_the_table(news):
+    """What the table does not hold gets no weight and keeps what it had, in a workspace of the table's size."""
+    _check([90000, 5000], list(news), 2, 4, 128, table_tokens=700, places=100000)
+    _check([300000, 200], list(news), 1, 3, 64, table_tokens=400, places=200000, in_place=True)
