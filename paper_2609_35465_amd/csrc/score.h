@@ -274,7 +274,9 @@ struct ScoreRow {
     __device__ __forceinline__ ScoreRow(const ScoreScale& scale, const ScoreSum& sum) : scale(scale), sum(sum), log_l(logf(sum.l)) {}
     __device__ __forceinline__ float log_of(float x) const {
         if (sum.m == -INFINITY || !(x > -INFINITY)) return -INFINITY;
-        return (x == sum.m ? 0.f : (x - sum.m) * scale.inverse) - log_l;
+        float t = x == sum.m ? 0.f : (x - sum.m) * scale.inverse;
+        if (t == -INFINITY) t = 2.f * ((0.5f * x - 0.5f * sum.m) * scale.inverse);     // x - m past the type's end
+        return t - log_l;
     }
     __device__ __forceinline__ void write(const ScoreArgs& a, int row, const ScoreGiven& given) const {
         for (int g = threadIdx.x; g < a.given; g += 256)

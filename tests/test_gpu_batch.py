@@ -774,6 +774,14 @@ def test_score_large_logits():
     _check_score(x, top=5)
 
 
+@pytest.mark.parametrize("temperature", [1.0, 1.5, 4.0, 1e30])
+def test_score_differences_past_the_type(temperature):
+    """Logits that lie further apart than the type reaches, at temperatures that bring them back into it."""
+    x = np.random.default_rng(0).uniform(-3.4e38, 3.4e38, (2, 3000)).astype(np.float32)
+    x[0, 7], x[0, 8], x[1, 9] = np.finfo(np.float32).min, np.finfo(np.float32).max, np.inf
+    _check_score(x, [[7, 8, 5], [9, 5, 6]], top=64, temperature=temperature)
+
+
 def test_score_workspace_serves_fewer_rows():
     """One for the largest batch serves every smaller one, whose rows are cut in more parts."""
     vocab, top = 30000, 7
