@@ -50,20 +50,74 @@ __device__ __forceinline__ EvictShape evict_shape(const EvictArgs& a, int seq) {
     return s;
 }
 
-// rises with the weight; NaN counts as -inf, and the zeros are equal
-__device__ __forceinline__ uint32_t evict_key(float x) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, x == 0.f ? 0.f : x);
-    return x != x ? 0x007FFFFFu : b >> 31 ? ~b : b | 0x80000000u;
-}
+// What the two forms of the choice have in common: a workgroup's bins and its waves' counts.
+struct EvictLds {
+    unsigned count[kEvictBins], above[kEvictWaves], equal[kEvictWaves];
+    int found[2];
 
+    // found: the bin in which the count from the last bin down reaches `need`, and what it has to give; a thread has two
+    // neighbouring bins, hi of the last but 2 tid and lo below it
+    __device__ __forceinline__ void find(unsigned hi, unsigned lo, unsigned need) {
+        const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = kEvictBins - 2 - 2 * tid;
+        const unsigned upto = wave_upto(Sum(), hi + lo);
+        if ((tid & 63) == 63) above[wave] = upto;
+        __syncthreads();
+        unsigned before = upto - hi - lo;
+        for (int w = 0; w < wave; ++w) before += above[w];
+        if (before < need && before + hi >= need) {
+            found[0] = b + 1;
+            found[1] = need - before;
+        } else if (before + hi < need && before + hi + lo >= need) {
+            found[0] = b;
+            found[1] = need - before - hi;
+        }
+        __syncthreads();
+    }
+
+    // Puts the tokens of `each` above the cut, and as many at it that `left` are put with the `equals` before them, in
+    // their order from `place` + min(equals, left) on.
+    template <class Each, class Put>
+    __device__ __forceinline__ void select(Each each, uint32_t cut, int left, int place, int equals, Put put) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        unsigned n_above = 0, n_equal = 0;
+        each([&](int, float x, bool is) {
+            const uint32_t k = rising_key(x);
+            n_above += is && k > cut;
+            n_equal += is && k == cut;
+        });
+        n_above = wave_all(Sum(), n_above);
+        n_equal = wave_all(Sum(), n_equal);
+        if (lane == 0) {
+            above[wave] = n_above;
+            equal[wave] = n_equal;
+        }
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) {
+            place += above[w];
+            equals += equal[w];
+        }
+        place += min(equals, left);
+        const unsigned long long below = (1ull << lane) - 1;
+        each([&](int t, float x, bool is) {
+            const uint32_t k = rising_key(x);
+            const unsigned long long same = __ballot(is && k == cut);
+            const bool stays = is && (k > cut || (k == cut && equals + static_cast<int>(__popcll(same & below)) < left));
+            const unsigned long long staying = __ballot(stays);
+            if (stays) put(place + static_cast<int>(__popcll(staying & below)), t, x);
+            place += __popcll(staying);
+            equals += __popcll(same);
+        });
+    }
+};
 
 // The smallest key that stays is found eleven bits at a time from the histogram of the
 // keys that agree so far; then every wave writes its part of the tokens.  64 sequences
 // of up to 4,096 tokens, 8 heads: 12.5 us, three rounds of LDS atomics and scans.  A wave's part
-// is in line, a token a lane, the first kEvictHeld of a lane in registers from the start.
+// is in line, a token a lane, kEvictHeld of a lane in registers from the start: all of them,
+// as tables with room for more than kEvictHeld kEvictThreads tokens take the form below.
 __global__ __launch_bounds__(kEvictThreads) void evict_choose_kernel(EvictArgs a) {
-    __shared__ unsigned count[kEvictBins], above[kEvictWaves], equal[kEvictWaves];
-    __shared__ int found[2];
+    __shared__ EvictLds sh;
+    unsigned(&count)[kEvictBins] = sh.count;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int seq = blockIdx.x / a.from.kv_heads, head = blockIdx.x % a.from.kv_heads;
     const EvictShape s = evict_shape(a, seq);
@@ -89,7 +143,6 @@ __global__ __launch_bounds__(kEvictThreads) void evict_choose_kernel(EvictArgs a
 #pragma unroll
         for (int j = 0; j < kEvictHeld; ++j)
             if (t0 + 64 * j < t1) f(t0 + 64 * j + lane, held[j], t0 + 64 * j + lane < t1);
-        for (int i = t0 + 64 * kEvictHeld; i < t1; i += 64) f(i + lane, i + lane < t1 ? mass_of(i + lane) : 0.f, i + lane < t1);
     };
     uint32_t cut = 0;
     int left = pick;                                            // of the keys that begin like `cut`
@@ -99,61 +152,18 @@ __global__ __launch_bounds__(kEvictThreads) void evict_choose_kernel(EvictArgs a
         for (int i = tid; i < kEvictBins; i += kEvictThreads) count[i] = 0;
         __syncthreads();
         each([&](int, float x, bool is) {
-            const uint32_t k = evict_key(x);
+            const uint32_t k = rising_key(x);
             if (is && (pass == 0 || (k >> (shift + bits)) == (cut >> (shift + bits))))
                 atomicAdd(&count[k >> shift & ((1u << bits) - 1)], 1u);
         });
         __syncthreads();
-        // the bin in which the count from the last bin down reaches `left`: two bins a thread
         const int b = kEvictBins - 2 - 2 * tid;
-        const unsigned hi = count[b + 1], lo = count[b];
-        const unsigned upto = wave_upto(Sum(), hi + lo);
-        if (lane == 63) above[wave] = upto;
-        __syncthreads();
-        unsigned before = upto - hi - lo;
-        for (int w = 0; w < wave; ++w) before += above[w];
-        const unsigned need = left;
-        if (before < need && before + hi >= need) {
-            found[0] = b + 1;
-            found[1] = need - before;
-        } else if (before + hi < need && before + hi + lo >= need) {
-            found[0] = b;
-            found[1] = need - before - hi;
-        }
-        __syncthreads();
-        cut |= static_cast<uint32_t>(found[0]) << shift;
-        left = found[1];
+        sh.find(count[b + 1], count[b], left);
+        cut |= static_cast<uint32_t>(sh.found[0]) << shift;
+        left = sh.found[1];
         __syncthreads();
     }
-    unsigned n_above = 0, n_equal = 0;
-    each([&](int, float x, bool is) {
-        const uint32_t k = evict_key(x);
-        n_above += is && k > cut;
-        n_equal += is && k == cut;
-    });
-    n_above = wave_all(Sum(), n_above);
-    n_equal = wave_all(Sum(), n_equal);
-    if (lane == 0) {
-        above[wave] = n_above;
-        equal[wave] = n_equal;
-    }
-    __syncthreads();
-    int place = 0, equals = 0;                                  // before this wave: above the cut, and at it
-    for (int w = 0; w < wave; ++w) {
-        place += above[w];
-        equals += equal[w];
-    }
-    place += min(equals, left);
-    const unsigned long long below = (1ull << lane) - 1;
-    each([&](int t, float x, bool is) {
-        const uint32_t k = evict_key(x);
-        const unsigned long long same = __ballot(is && k == cut);
-        const bool stays = is && (k > cut || (k == cut && equals + static_cast<int>(__popcll(same & below)) < left));
-        const unsigned long long staying = __ballot(stays);
-        if (stays) put(place + static_cast<int>(__popcll(staying & below)), t, x);
-        place += __popcll(staying);
-        equals += __popcll(same);
-    });
+    sh.select(each, cut, left, 0, 0, put);
 }
 
 // The same for long sequences, in parts of a row: a launch for each eleven bits, which
@@ -164,8 +174,8 @@ __global__ __launch_bounds__(kEvictThreads) void evict_choose_kernel(EvictArgs a
 
 template <int PASS>
 __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a) {
-    __shared__ unsigned count[kEvictBins], above[kEvictWaves], equal[kEvictWaves];
-    __shared__ int found[2];
+    __shared__ EvictLds sh;
+    unsigned(&count)[kEvictBins] = sh.count;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int units = a.from.seqs * a.from.kv_heads, unit = blockIdx.x / a.parts, mine = blockIdx.x - unit * a.parts;
     const int seq = unit / a.from.kv_heads;
@@ -220,33 +230,20 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a) 
             hi_before += p < mine ? c[p][1] : 0;
             lo_before += p < mine ? c[p][0] : 0;
         }
-        const unsigned upto = wave_upto(Sum(), hi + lo);
-        if (lane == 63) above[wave] = upto;
-        __syncthreads();
-        unsigned before = upto - hi - lo;
-        for (int w = 0; w < wave; ++w) before += above[w];
-        const unsigned need = left;
-        if (before < need && before + hi >= need) {
-            found[0] = b + 1;
-            found[1] = need - before;
-        } else if (before + hi < need && before + hi + lo >= need) {
-            found[0] = b;
-            found[1] = need - before - hi;
-        }
-        __syncthreads();
-        const int bin = found[0];
-        left = found[1];
+        sh.find(hi, lo, left);
+        const int bin = sh.found[0];
+        left = sh.found[1];
         cut |= static_cast<uint32_t>(bin) << shift;
         const unsigned over = wave_all(Sum(), (b + 1 > bin ? hi_before : 0) + (b > bin ? lo_before : 0));
         const unsigned same = wave_all(Sum(), (b + 1 == bin ? hi_before : 0) + (b == bin ? lo_before : 0));
         if (lane == 0) {
-            above[wave] = over;
-            equal[wave] = same;
+            sh.above[wave] = over;
+            sh.equal[wave] = same;
         }
         __syncthreads();
         for (int w = 0; w < kEvictWaves; ++w) {
-            before_part += above[w];
-            equals_before += equal[w];
+            before_part += sh.above[w];
+            equals_before += sh.equal[w];
         }
         __syncthreads();
         if (PASS < 3 && tid == 0) {
@@ -262,7 +259,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a) 
         for (int i = tid; i < kEvictBins; i += kEvictThreads) count[i] = 0;
         __syncthreads();
         each([&](int, float x, bool is) {
-            const uint32_t k = evict_key(x);
+            const uint32_t k = rising_key(x);
             if (is && (PASS == 0 || (k >> (shift + bits)) == (cut >> (shift + bits))))
                 atomicAdd(&count[k >> shift & ((1u << bits) - 1)], 1u);
         });
@@ -277,35 +274,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a) 
         };
         for (int i = mine * kEvictThreads + tid; i < s.last; i += a.parts * kEvictThreads) put(pick + i, old + i, mass_of(old + i));
         if (pick == 0) return;
-        unsigned n_above = 0, n_equal = 0;
-        each([&](int, float x, bool is) {
-            const uint32_t k = evict_key(x);
-            n_above += is && k > cut;
-            n_equal += is && k == cut;
-        });
-        n_above = wave_all(Sum(), n_above);
-        n_equal = wave_all(Sum(), n_equal);
-        if (lane == 0) {
-            above[wave] = n_above;
-            equal[wave] = n_equal;
-        }
-        __syncthreads();
-        int place = before_part, equals = equals_before;
-        for (int w = 0; w < wave; ++w) {
-            place += above[w];
-            equals += equal[w];
-        }
-        place += min(equals, left);
-        const unsigned long long below = (1ull << lane) - 1;
-        each([&](int t, float x, bool is) {
-            const uint32_t k = evict_key(x);
-            const unsigned long long same = __ballot(is && k == cut);
-            const bool stays = is && (k > cut || (k == cut && equals + static_cast<int>(__popcll(same & below)) < left));
-            const unsigned long long staying = __ballot(stays);
-            if (stays) put(place + static_cast<int>(__popcll(staying & below)), t, x);
-            place += __popcll(staying);
-            equals += __popcll(same);
-        });
+        sh.select(each, cut, left, before_part, equals_before, put);
     }
 }
 

@@ -1,5 +1,5 @@
 // Sums and maxima over the lanes of a wave by DPP moves, which take a few cycles
-// each where a shuffle goes through LDS.
+// each where a shuffle goes through LDS; the order of floats as whole numbers.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -90,6 +90,12 @@ __device__ __forceinline__ float with_row(F f, float v) {
     const uint32_t u = __builtin_bit_cast(uint32_t, v);
     const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     return f(__builtin_bit_cast(float, static_cast<uint32_t>(r[0])), __builtin_bit_cast(float, static_cast<uint32_t>(r[1])));
+}
+
+// whole numbers that rise with x; NaN counts as -inf, and the zeros are equal
+__device__ __forceinline__ uint32_t rising_key(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x == 0.f ? 0.f : x);
+    return x != x ? 0x007FFFFFu : b >> 31 ? ~b : b | 0x80000000u;
 }
 
 }  // namespace tetra_dev

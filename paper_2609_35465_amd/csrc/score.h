@@ -47,17 +47,12 @@ struct ScoreArgs {
     uint64_t* places;                        // [rows][parts][top]: the parts' largest, falling
 };
 
-__device__ __forceinline__ uint32_t score_key(float x) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, x == 0.f ? 0.f : x);
-    return x != x ? 0x007FFFFFu : b >> 31 ? ~b : b | 0x80000000u;
-}
-
 __device__ __forceinline__ float score_logit(uint32_t key) {
     return __builtin_bit_cast(float, key >> 31 ? key ^ 0x80000000u : ~key);
 }
 
 __device__ __forceinline__ uint64_t score_place(float x, int index) {
-    return static_cast<uint64_t>(score_key(x)) << 32 | static_cast<uint32_t>(~index);
+    return static_cast<uint64_t>(rising_key(x)) << 32 | static_cast<uint32_t>(~index);
 }
 
 // 1 / T, and c.  Temperatures end at 2^100, so that `least` is a number and -inf stays out.
@@ -117,7 +112,7 @@ struct ScoreTop {
     // a key that at least n of the groups' reach, near the largest such; a lane's groups
     // count as one where 64 are enough
     __device__ __forceinline__ static uint32_t reached(const float (&groups)[4], int n) {
-        const uint32_t key = score_key(fmaxf(fmaxf(groups[0], groups[1]), fmaxf(groups[2], groups[3])));
+        const uint32_t key = rising_key(fmaxf(fmaxf(groups[0], groups[1]), fmaxf(groups[2], groups[3])));
         uint32_t lo = ~wave_all(Max(), ~key), hi = wave_all(Max(), key);
         if (n <= kMostTop / 2) {
             for (int step = 0; step < 10 && lo < hi; ++step) {
@@ -127,7 +122,7 @@ struct ScoreTop {
             }
         } else {
             uint32_t k[4];
-            for (int i = 0; i < 4; ++i) k[i] = score_key(groups[i]);
+            for (int i = 0; i < 4; ++i) k[i] = rising_key(groups[i]);
             for (int step = 0; step < 10 && lo < hi; ++step) {
                 const uint32_t mid = hi - (hi - lo) / 2;
                 const int c = __popcll(__ballot(k[0] >= mid)) + __popcll(__ballot(k[1] >= mid)) +
