@@ -31,8 +31,7 @@
 namespace tetra_dev {
 
 constexpr int kWeighBlock = 256;          // tokens of a workgroup
-constexpr int kWeighTiles = 1;            // of 32 tokens, of a wave
-constexpr int kWeighWaves = kWeighBlock / (32 * kWeighTiles);
+constexpr int kWeighWaves = kWeighBlock / 32;
 constexpr int kWeighRows = 32;            // rows of a tile
 constexpr int kWeighSpans = 256;          // of a sequence's tokens, for the sums, at most
 constexpr int kWeighMostTiles = 16;       // row tiles whose sums a workgroup holds in LDS
@@ -252,7 +251,7 @@ __device__ __forceinline__ void weigh_write(const WeighArgs& a, const WeighItem&
 
 template <int D, WeighPass PASS>
 __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_kernel(WeighArgs a) {
-    constexpr int TT = kWeighTiles, kThreads = 64 * kWeighWaves, kSlices = D / 8;
+    constexpr int kThreads = 64 * kWeighWaves, kSlices = D / 8;
     constexpr int kPieces = kSlices * kWeighRows;               // of 8 dimensions, of a tile of rows
     constexpr int kPer = (kPieces + kThreads - 1) / kThreads;   // and of a thread
     static_assert(kPieces % kThreads == 0 || kPer == 1, "all of a thread's or none");
@@ -285,10 +284,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
                 sums[wave][i][1] = 0.f;
             }
         }
-        float total[TT][16];
+        float total[16];
         if constexpr (!kSums)
-            for (auto& t : total)
-                for (float& v : t) v = 0.f;
+            for (float& v : total) v = 0.f;
         for (int block = w.block; block < w.block + w.blocks; ++block) {
             // the rows that see something of the block: tiles tile0 .. tile1 - 1
             const int t_begin = block * kWeighBlock, t_end = min(t_begin + kWeighBlock, w.q.end);
@@ -300,13 +298,12 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
             if (t_end <= t_begin) tile1 = tile0;
             if (tile0 >= tile1) continue;
             // the wave's tokens
-            const int mine = t_begin + 32 * TT * wave;
-            f16x8 k[TT][D / 16];
-            float unit[TT][2];                    // of 16 tokens each: scale of the scores
+            const int mine = t_begin + 32 * wave;
+            f16x8 k[D / 16];
+            float unit[2];                        // of 16 tokens each: scale of the scores
             unsigned there = 0;                   // which of those have a page
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int token = mine + 32 * t + lrow;
+            {
+                const int token = mine + lrow;
                 const int page = token < t_end ? table[token >> a.c.page_shift] : -1;
                 const bool is = page >= 0 && page < a.c.num_pages;
                 const size_t ph = static_cast<size_t>(is ? page : 0) * a.c.kv_heads + w.head;
@@ -317,13 +314,13 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
                 const float scale = a.c.scales[2 * ph] * a.scale;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
-                    k[t][2 * c] = to_half8(raw[c][0], raw[c][1]);
-                    k[t][2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
+                    k[2 * c] = to_half8(raw[c][0], raw[c][1]);
+                    k[2 * c + 1] = to_half8(raw[c][2], raw[c][3]);
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    unit[t][g] = lane_of(scale, 16 * g);
-                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << (2 * t + g);
+                    unit[g] = lane_of(scale, 16 * g);
+                    there |= static_cast<unsigned>(__builtin_amdgcn_readlane(is, 16 * g)) << g;
                 }
             }
             // Row r of the sequence is token r / group, head r % group; a tile's first row as both, uniform.
@@ -399,22 +396,18 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
                     if (tile + 2 < tile1) load();
                 }
                 const float my_log = kSums ? 0.f : row_logs[b][lrow];
-                f32x16 z[TT];
+                f32x16 z;
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+                for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const f16x8 q = *reinterpret_cast<const f16x8*>(rows[b][4 * c + 2 * half + u][lrow]);
-#pragma unroll
-                        for (int t = 0; t < TT; ++t) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][2 * c + u], q, z[t], 0, 0, 0);
-                    }
+                    for (int u = 0; u < 2; ++u)
+                        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            k[2 * c + u], *reinterpret_cast<const f16x8*>(rows[b][4 * c + 2 * half + u][lrow]), z, 0, 0, 0);
                 // do all of the tile's rows see all of the wave's tokens (rows past the last matter to none)?
                 const int position0 = s.first + now.t, position1 = position0 + step_t + 1;
-                const bool all = there == (1u << 2 * TT) - 1 && mine + 32 * TT <= min(position0 + 1, t_end) &&
+                const bool all = there == 3u && mine + 32 <= min(position0 + 1, t_end) &&
                                  (a.window == 0 || position1 - a.window < mine);
                 const TileAt at = now;
                 step(now);
@@ -429,36 +422,30 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
                         lo = static_cast<unsigned>(see_begin - mine - 4 * half);
                         n = static_cast<unsigned>(max(see_end - see_begin, 0));
                     }
-                    auto unseen = [&](int t, int e) {
-                        return static_cast<unsigned>(32 * t + 8 * (e / 4) + e % 4) - lo >= n || !(there >> (2 * t + e / 8) & 1);
-                    };
+                    auto unseen = [&](int e) { return static_cast<unsigned>(8 * (e / 4) + e % 4) - lo >= n || !(there >> (e / 8) & 1); };
                     if constexpr (kSums) {
                         // the largest before the scale, which is the same for 8 of a lane and not below 0
                         float top = kWeighNone;
 #pragma unroll
-                        for (int t = 0; t < TT; ++t)
+                        for (int g = 0; g < 2; ++g) {
+                            float most = -INFINITY;
 #pragma unroll
-                            for (int g = 0; g < 2; ++g) {
-                                float most = -INFINITY;
-#pragma unroll
-                                for (int e = 8 * g; e < 8 * g + 8; ++e) {
-                                    if constexpr (masked) z[t][e] = unseen(t, e) ? -INFINITY : z[t][e];
-                                    most = fmaxf(most, z[t][e]);
-                                }
-                                top = fmaxf(top, most > -INFINITY ? most * unit[t][g] : -INFINITY);
+                            for (int e = 8 * g; e < 8 * g + 8; ++e) {
+                                if constexpr (masked) z[e] = unseen(e) ? -INFINITY : z[e];
+                                most = fmaxf(most, z[e]);
                             }
+                            top = fmaxf(top, most > -INFINITY ? most * unit[g] : -INFINITY);
+                        }
                         float* at_row = sums[wave][(tile - w.tile) * kWeighRows + lrow];
                         const float m0 = at_row[0], l0 = at_row[1];
                         const float m = fmaxf(with_half(Larger(), top), m0);
                         float l = 0.f;
 #pragma unroll
-                        for (int t = 0; t < TT; ++t)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float v = fast_exp2(__builtin_fmaf(z[t][e], unit[t][e / 8], -m));
-                                if constexpr (masked) v = z[t][e] == -INFINITY ? 0.f : v;
-                                l += v;
-                            }
+                        for (int e = 0; e < 16; ++e) {
+                            float v = fast_exp2(__builtin_fmaf(z[e], unit[e / 8], -m));
+                            if constexpr (masked) v = z[e] == -INFINITY ? 0.f : v;
+                            l += v;
+                        }
                         l = with_half(Sum(), l) + l0 * fast_exp2(m0 - m);
                         if (half == 0) {
                             at_row[0] = m;
@@ -466,13 +453,11 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
                         }
                     } else {
 #pragma unroll
-                        for (int t = 0; t < TT; ++t)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float v = fast_exp2(__builtin_fmaf(z[t][e], unit[t][e / 8], -my_log));
-                                if constexpr (masked) v = unseen(t, e) ? 0.f : v;
-                                total[t][e] += v;
-                            }
+                        for (int e = 0; e < 16; ++e) {
+                            float v = fast_exp2(__builtin_fmaf(z[e], unit[e / 8], -my_log));
+                            if constexpr (masked) v = unseen(e) ? 0.f : v;
+                            total[e] += v;
+                        }
                     }
                 };
                 if (all) finish(std::false_type());
@@ -494,11 +479,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2 * kWeighWaves / 4) void weigh_k
             }
         } else {
             // lane e of 16 gets the sum of total[e] over them, then over the other 16 of the half
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const float sum = with_row(Sum(), weigh_scatter(total[t]));
-                const int place = 32 * (TT * wave + t) + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
-                if (lrow >= 16) continue;
+            const float sum = with_row(Sum(), weigh_scatter(total));
+            const int place = 32 * wave + 8 * ((lrow & 15) >> 2) + 4 * half + (lrow & 3);
+            if (lrow < 16) {
                 if (w.chunks == 1) weigh_write(a, w, w.block * kWeighBlock + place, sum);
                 else a.parts[static_cast<size_t>(w.slot) * kWeighBlock + place] = sum;
             }
