@@ -573,7 +573,13 @@ int tetra_kv_append_at(const tetra_kv_cache* cache, const tetra_kv_input* in, co
 /*
  * tetra_kv_attend for a batch in which groups of sequences begin with the same
  * pages (a system prompt, a document, several answers to one prompt): the
- * pages that a group shares are read once for all of its rows.
+ * pages that a group shares are read once for all of its rows, in calls that
+ * are large enough for that and not too large.  That is told by sizes alone: the
+ * tables of all sequences have room for 160 MiB of keys and values or more
+ * (counted for each 16 rows of a sequence and cache head), a sequence and cache
+ * head has up to 64 rows (max_new * q_heads / kv_heads), rows * q_heads is up to
+ * 65,536, and groups and sequences are up to 131,072, times kv_heads up to 2^20.
+ * Other calls go by tetra_kv_attend, which reads pages for each sequence.
  * Group g is the sequences groups[g] .. groups[g + 1] - 1; their first
  * shared[g] tokens lie in the same pages, which all their tables name (of a
  * page that shared[g] ends inside, nothing counts as shared).  Sequences of
@@ -608,7 +614,9 @@ size_t tetra_kv_attend_shared_workspace_bytes(void);
  * rows themselves have no past: mass is not read there.  Sequences without
  * rows keep what they have (mass_out = mass).  Rows are a sequence's last
  * tokens, so a prompt can be weighed by its last few rows alone.  A q with a
- * NaN or an infinity makes the weights that its row gives NaN.
+ * NaN or an infinity makes the weights that its row gives NaN.  Where the rows
+ * of a sequence and cache head, times head_dim, are 2,048 at most, all of its keys
+ * are read, with a window as without.
  *   mass:     device fp32 [seqs][kv_heads][mass_tokens], or NULL: all 0
  *   mass_out: the same, may be mass itself; tokens from mass_tokens on have no
  *             place in either
@@ -656,6 +664,8 @@ size_t tetra_kv_weigh_workspace_bytes(const tetra_kv_cache* cache, int rows, int
  *   recent: 0 or more
  *   workspace: as for tetra_kv_attend, at least
  *         tetra_kv_evict_workspace_bytes(from, to)
+ * Tables of `from` with room for more than 8,192 tokens take four launches for the
+ * choice in place of one, whatever the lengths.
  * Tokens without a page go in as zeros, and kept tokens that `to` has no page
  * for are dropped.  Asynchronous; errors as for tetra_kv_append, TETRA_EINVAL
  * also where `to` has room for 2^29 tokens or more, over all sequences and

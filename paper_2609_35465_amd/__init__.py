@@ -541,8 +541,9 @@ def kv_attend_shared_workspace():
 def kv_attend_shared(cache: KVCache, q, starts, max_new: int, groups, shared, out, workspace, scale: float = None,
                      stream=None):
     """kv_attend (without a window) of a batch whose sequences groups[g] .. groups[g + 1] - 1 (int32 [n + 1])
-    begin with the same shared[g] tokens (int32 [n]) in the same pages, which are read once for all of them;
-    workspace from kv_attend_shared_workspace(), one per stream."""
+    begin with the same shared[g] tokens (int32 [n]) in the same pages, which are read once for all of them where
+    the call's sizes are such that it pays (include/tetra.h); workspace from kv_attend_shared_workspace(), one per
+    stream."""
     what = "tetra_kv_attend_shared"
     rows, heads, stride = _rows_of(cache, q, starts, what)
     _, f16, i32 = _kinds

@@ -35,7 +35,8 @@ constexpr int kWeighGroupsPerCU = 2, kWeighFewGroupsPerCU = 4;
 // of one of 64.  Then the keys are what is read: 64 sequences of up to 4,096 tokens, 5 rows
 // 37 us by weigh_few_kernel and 73 by weigh_kernel, whose rows go through LDS with a barrier; 16
 // rows 22-41 and 30-73 by batch; heads of 64, 32 rows 14-43 and 16-62.  With heads of
-// 128, 20 rows took 28 and 22 (8 sequences) to 62 and 73 (64), 32 rows 37 and 30 (16).
+// 128, 20 rows took 28 and 22 (8 sequences) to 62 and 73 (64), 32 rows 37 and 30 (16): the rule
+// is for batches of up to some 32 sequences there and does not look at their count.
 constexpr long long kWeighFew = 2048;
 bool weigh_few(int max_new, int group, int head_dim) { return static_cast<long long>(max_new) * group * head_dim <= kWeighFew; }
 
@@ -100,7 +101,9 @@ int weigh_launch(tetra_dev::WeighArgs& a, const WeighSpace& space, int cus, hipS
 // Places of kv_evict's workspace.  A sequence and head whose weights a workgroup holds in
 // registers is one workgroup's, in one launch; longer ones are cut in parts, two workgroups a
 // CU in all, in four launches (8 heads of 131,072 tokens 32 us in place of 144; what the
-// first form takes is 12.5 us for 512 units of up to 4,096).
+// first form takes is 12.5 us for 512 units of up to 4,096).  The host does not know the
+// lengths, so the table's width decides: 64 sequences of 300 tokens, 8 heads, cut to 150
+// take 23 us with tables of up to 8,192 tokens and 48 with wider ones.
 struct EvictSpace {
     int parts;            // 0: not cut
     size_t tokens, state, bytes;

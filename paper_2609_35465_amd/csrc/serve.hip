@@ -178,7 +178,10 @@ int attend_device(tetra_dev::AttendArgs& a, size_t workspace_bytes, int& cus) {
 
 // What a call with shared prefixes may be to go by its groups: rows of a sequence and cache
 // head, rows times q heads, groups and sequences, and these times cache heads (at most 8
-// workgroups of the join for each).
+// workgroups of the join for each).  The first is what was measured to pay, the others are
+// what the workspace holds, whose size does not depend on the call: 1,600 sequences of 1,044
+// tokens with 1,024 in common, 40 heads over 8 of 128, take 280 us by groups and 472 by
+// kv_attend, 1,700 go by kv_attend and take 507.
 constexpr int kSharedMost = 64, kSharedRows = 65536, kSharedList = 131072, kSharedHeads = 1 << 20;
 
 // bytes of kv_attend_shared's workspace, behind those of kv_attend
@@ -197,7 +200,8 @@ struct SharedSpace {
 // memory, some 14 us, and saves what kv_attend reads of keys and values more than once: of
 // pages that sequences share it has much from the caches.  What it may read is told by the
 // table's width, for the host does not know the lengths, and it reads it for each 16 rows
-// of a sequence.  Measured (40 heads over 8 of 128, us by groups and by kv_attend): 8
+// of a sequence.  So short sequences in wide tables take the four launches: 4 sequences of
+// 1,056 tokens 15.7 us with tables of 20,480 tokens and more, 10.7 by kv_attend.  Measured (40 heads over 8 of 128, us by groups and by kv_attend): 8
 // sequences of 4,196 tokens (69 MB) 28 and 22, 64 of 1,124 (151 MB) 29 and 27, 12 of 8,292
 // (204 MB) 33 and 39, 64 of 4,196 in 8 groups (554 MB) 43 and 56, with four rows each in one
 // group 64 and 179.

@@ -524,7 +524,10 @@ __device__ __forceinline__ float weigh_log(const WeighArgs& a, const WeighItem& 
 // every wave for itself, a span of blocks of 64 tokens at a time, the rows in its
 // registers and the next block's keys on their way.  The first pass also leaves the scores
 // where there is room for them (16 M), so that the second reads those and not the keys again:
-// of 5 rows 20 bytes for 128.  64 sequences of up to 4,096 tokens, 40 heads over 8 of 128:
+// of 5 rows 20 bytes for 128.  64 sequences of 6,528 tokens, whose scores fit, take 144 us, of
+// 6,656, whose do not, 185.  All blocks of a sequence are gone through, also those before a
+// window: one token of 131,072, 40 heads over 8, 48 us with a window of 1,024 as without.
+// 64 sequences of up to 4,096 tokens, 40 heads over 8 of 128:
 // 24 us (91 MB of keys, 14 of scores, 4,400 GB/s) and 13, with the keys read twice 21
 // and 22.  In 32 rows a tile, a block a wave at a time, both took 27.  Tile t of four takes
 // token 16 g + 4 t + i as its row 4 g + i, so that a lane of group g = lane / 16 gets the
