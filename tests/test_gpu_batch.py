@@ -635,6 +635,26 @@ def test_append_shifted_is_the_append_further_on(dim, news):
             assert torch.equal(a[pages], b[pages])
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_append_shifted_from_fp16_with_norms(dim):
+    """fp16 rows, strided, with norms: the bytes of an append whose table of the rotation begins at the shift."""
+    lens, news, shift = [40, 23, 130], [1, 17, 70], 333
+    starts, rows = _starts(news), sum(news)
+    rng = np.random.default_rng(3)
+    wide = _dev(rng.standard_normal((rows, 8 * dim + 16)).astype(np.float16))
+    q, k, v = (wide[:, 8 + a * dim:8 + b * dim] for a, b in ((0, 4), (4, 6), (6, 8)))
+    norms = [_dev(rng.uniform(0.5, 1.5, dim).astype(np.float32)) for _ in range(2)]
+    rope, got = tt.rope_table(600, dim), []
+    for table, shifts in ((rope, torch.full((3,), shift, dtype=torch.int32, device="cuda")), (rope[shift:].contiguous(), None)):
+        c = Cache(50, lens, 2, 16, dim)
+        out = torch.zeros((rows, 4, dim), dtype=torch.float16, device="cuda")
+        tt.kv_append(c.upload(), q, k, v, _dev(starts), max(news), table, out, *norms, shifts=shifts)
+        torch.cuda.synchronize()
+        got.append([*c.d[:3], out])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_append_shifts_are_clamped():
     c = Cache(49, [40, 21], 1, 16, 64)
     x, rope = _dev(np.random.default_rng(2).standard_normal((2, 1, 64)).astype(np.float32)), tt.rope_table(50, 64)
